@@ -414,6 +414,95 @@ hap_status hap_self_check(uint64_t *host_sites);
  * the general kernel; the two reduction kernels).  Host value, no device work. */
 hap_status hap_launches_per_pass(hap_problem *, uint32_t *host_count);
 
+/* ---- Training operators --------------------------------------------------------------------------------------------
+ * The planner's times are those of operators: an expert's feed-forward products (t_ffn, eta, gamma), the output head
+ * (t_post), the optimizer's step (c_opt).  These calls are the operators, and hap_measure_profile times them on the current
+ * device, which so becomes a device type of a plan.
+ *  - They need no handle.  Pointers are device memory of the current device, matrices are row-major with the distance of
+ *    two rows (ld*, in elements) given, and elements of a row side by side.  Outputs may not overlap inputs unless a
+ *    function says so.
+ *  - They are asynchronous on `stream`, allocate nothing, and may be captured: a captured call replays with the addresses
+ *    and numbers it was given.  Calls on different streams may run at the same time; each has its own workspace then.
+ *  - Sums are kept in fp32 and rounded once to the output's type.  The order of additions is fixed: the same call gives the
+ *    same bits.
+ *  - Operands whose addresses and row distances are multiples of 16 bytes run on the tensor cores; others on a plain
+ *    kernel with the same results up to the order of additions, at a small part of the speed. */
+enum { HAP_BF16 = 0, HAP_FP16 = 1, HAP_FP32 = 2 };   /* element types */
+enum { HAP_EXPERT_FORWARD = 0, HAP_EXPERT_GRAD_INPUT = 1, HAP_EXPERT_GRAD_WEIGHT = 2 };
+
+/* Products of rows that are sorted by expert with their expert's matrix.  Rows dev_offsets[e] .. dev_offsets[e+1] of the
+ * `rows` rows belong to expert e (int64 [E+1] on the device, ascending; values outside of 0 .. rows are clamped, one that is
+ * below its predecessor counts as that).  An expert may have no rows.
+ *   HAP_EXPERT_FORWARD      out[i] = a[i] w_e^T          a [rows][K], b = w [E][N][K], out [rows][N]
+ *   HAP_EXPERT_GRAD_INPUT   out[i] = a[i] w_e            a [rows][N], b = w [E][N][K], out [rows][K]
+ *   HAP_EXPERT_GRAD_WEIGHT  out_e = sum_i a[i]^T b[i]    a [rows][N], b [rows][K], out [E][N][K]; 0 without rows
+ * Matrices of two experts are N * ldb (out of the third form: N * ldo) elements apart.  Rows of `out` before the first and
+ * behind the last expert's are left as they are, and what such rows of a and b hold does not matter.  dtype: HAP_BF16 or
+ * HAP_FP16; out_dtype: dtype or HAP_FP32.  accumulate: the product is added to what `out` holds.  1 <= E <= 1024. */
+hap_status hap_expert_matmul(int32_t form, int32_t dtype, int32_t out_dtype, int32_t accumulate, int32_t E, int64_t rows,
+                             int32_t N, int32_t K, const int64_t *dev_offsets, const void *dev_a, int64_t lda,
+                             const void *dev_b, int64_t ldb, void *dev_out, int64_t ldo, void *stream);
+
+/* First half of a gated feed-forward block: [g | u]_i = x[i] w_e^T with x [rows][H], w [E][2F][H] (the gate's F rows, then
+ * the other F), h_i = g_i / (1 + exp(-g_i)) * u_i, h [rows][F].  dev_gu [rows][2F] keeps g and u for the backward pass
+ * (nullable).  h is formed from g and u before they are rounded.  Offsets and rows as in hap_expert_matmul. */
+hap_status hap_expert_gated(int32_t dtype, int32_t E, int64_t rows, int32_t H, int32_t F, const int64_t *dev_offsets,
+                            const void *dev_x, int64_t ldx, const void *dev_w, int64_t ldw, void *dev_gu, int64_t ldgu,
+                            void *dev_h, int64_t ldh, void *stream);
+/* Its backward pass with the product in front of it: dh_i = dy[i] w2_e with dy [rows][H], w2 [E][H][F], and from the kept
+ * g and u dgu [rows][2F] = [dg | du], dg = dh u (s + g s (1 - s)), du = dh g s, s = 1 / (1 + exp(-g)), and h [rows][F] = g s u
+ * again (nullable), which the gradient of w2 needs.  dh is not rounded in between.  dev_dgu may be dev_gu. */
+hap_status hap_expert_gated_backward(int32_t dtype, int32_t E, int64_t rows, int32_t H, int32_t F, const int64_t *dev_offsets,
+                                     const void *dev_dy, int64_t ldy, const void *dev_w2, int64_t ldw, const void *dev_gu,
+                                     int64_t ldgu, void *dev_dgu, int64_t lddgu, void *dev_h, int64_t ldh, void *stream);
+
+/* Cross entropy of the output head without keeping the logits z = x w^T (x [rows][H], w [V][H]): lse_i = log sum_j exp z_ij
+ * and loss_i = lse_i - z_i,target(i), fp32 [rows]; loss_i = 0 where target(i) = ignore (lse_i is that of the logits all the
+ * same), NaN where a target is neither that nor in 0 .. V-1.  target: int64 [rows].
+ * The backward pass gives the gradients of grad * sum_i loss_i (dev_grad: fp32 scalar on the device) from the lse of the
+ * forward pass: dx [rows][H], dw [V][H], either nullable; a row without a valid target adds nothing, but must be finite.
+ * It computes the logits again, in pieces of the vocabulary; softmax - one-hot is rounded to `dtype` before the products
+ * with w and x, not the gradient's scale.
+ * Workspace: hap_linear_cross_entropy_workspace bytes of 256-byte aligned device memory, needed during a call only. */
+hap_status hap_linear_cross_entropy_workspace(int64_t rows, int32_t H, int64_t V, uint64_t *host_bytes);
+hap_status hap_linear_cross_entropy(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *dev_x, int64_t ldx,
+                                    const void *dev_w, int64_t ldw, const int64_t *dev_target, int64_t ignore,
+                                    float *dev_loss, float *dev_lse, void *dev_workspace, uint64_t bytes, void *stream);
+hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *dev_x,
+                                             int64_t ldx, const void *dev_w, int64_t ldw, const int64_t *dev_target,
+                                             int64_t ignore, const float *dev_lse, const float *dev_grad, void *dev_dx,
+                                             int64_t lddx, void *dev_dw, int64_t lddw, void *dev_workspace, uint64_t bytes,
+                                             void *stream);
+
+/* One AdamW step over n tensors: with g = grad * (*dev_grad_scale, 1 if null), m = beta1 m + (1 - beta1) g,
+ * v = beta2 v + (1 - beta2) g^2, param = param (1 - lr weight_decay) - lr (m / (1 - beta1^step)) /
+ * (sqrt(v / (1 - beta2^step)) + eps).  `tensors` is host memory, read during the call.  Tensors may not overlap.
+ * param_dtype: any; grad_dtype: param's, HAP_FP32, or any under HAP_FP32 parameters.  `copy`, nullable: the new parameter
+ * rounded to copy_dtype (HAP_BF16, HAP_FP16), the weights that a model computes with while `param` is kept in 32 bits.
+ * state_bits 32: m and v are fp32.  state_bits 8: m is int8, v uint8, and m_scale, v_scale are fp32 [ceil(count / 256)]:
+ * blocks of 256 values share a scale s, the largest magnitude in the block.  m stands for s t |t| with t = m / 127, v for
+ * s t^4 with t = v / 255; the codes are the nearest to 127 sqrt(|m| / s) and 255 sqrt(sqrt(v / s)), ties to even, and that
+ * of a v above 0 is at least 1.  The step uses the moments before they are rounded.  All zeros is the start in either form.
+ * A block of 8-bit states that a gradient which is not finite has reached reads as not finite from then on.
+ * hap_adamw_state writes what 8-bit states stand for: host_m[i], host_v[i] point to fp32 [count] on the device (nullable). */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;  /* state_bits 8 */
+    void *copy;                /* nullable */
+    uint64_t count;
+} hap_adamw_tensor;
+typedef struct { double lr, beta1, beta2, eps, weight_decay; int64_t step; } hap_adamw_options;   /* step: 1 for the first */
+hap_status hap_adamw_step(const hap_adamw_tensor *tensors, int32_t n, int32_t param_dtype, int32_t grad_dtype,
+                          int32_t copy_dtype, int32_t state_bits, const hap_adamw_options *options,
+                          const float *dev_grad_scale, void *stream);
+hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *const *host_m, float *const *host_v, void *stream);
+
+/* Waits inside the operators' kernels are bounded; one that runs out ends its kernel early and sets a bit in a device word.
+ * Waits for the current device, returns that word in *host_bits (0: none, results are whole) and clears it. */
+hap_status hap_operator_status(uint32_t *host_bits);
+
 const char *hap_status_str(hap_status);
 const char *hap_last_error(const hap_problem *);
 

@@ -11,3 +11,6 @@ from .binding import (HapError, HapProblem, hap_problem_create, hap_enumerate, h
                       hap_search_range, hap_argmin, hap_argmin_static, hap_joint_bottleneck, hap_count_cells, hap_get_timings, hap_launches_per_pass, hap_eval_appendix_b, hap_simulate_1f1b, hap_release_cached_memory, hap_self_check, hap_problem_save, hap_problem_load, hap_problem_dims, hap_problem_destroy, load_library, EXPORTS, INF, COEF,
                       NCOEF, MAX_PP, OPT_NO_MAPTAB, OPT_REFINE, OPT_EXACT, OPT_UNIFORM, OPT_NO_TRIE, OPT_NO_FUSE, OPT_COUNT_SPLITS,
                       OPT_HETERO_DISPATCH)
+from .operators import (EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, HapAdamWTensors, hap_expert_matmul,  # noqa: F401,E402
+                        hap_expert_gated, hap_expert_gated_backward, hap_linear_cross_entropy_workspace, hap_linear_cross_entropy,
+                        hap_linear_cross_entropy_backward, hap_adamw_tensors, hap_adamw_step, hap_adamw_state, hap_operator_status)

@@ -1,0 +1,284 @@
+// Host side of the training operators: checks of arguments, choice of variant, launches.
+#include "hap_adamw.cuh"
+#include "hap_products.cuh"
+
+#include <math.h>
+
+using namespace hapop;
+
+static hap_status launched() { return cudaGetLastError() == cudaSuccess ? HAP_OK : HAP_E_CUDA; }
+
+static int sm_count()
+{
+    int dev = 0, n = 0;
+    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0 ? n : 0;
+}
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (!sms) return HAP_E_CUDA;
+    const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
+    const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, PM) : ceil_div(p.rows, PM) + p.groups);
+    if (most > INT32_MAX) return HAP_E_RANGE;
+    plain_product_kernel<T, FORM, EPI><<<(unsigned)(most < 4 * sms ? most : 4 * sms), 256, 0, stream>>>(p);
+    return launched();
+}
+
+static bool dtype16(int32_t t) { return t == HAP_BF16 || t == HAP_FP16; }
+static int64_t size_of(int32_t t) { return t == HAP_FP32 ? 4 : 2; }
+static bool aligned(const void *p, int64_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+// sizes that the kernels' 32-bit indexes hold
+static bool sizes_fit(int64_t rows, int64_t n, int64_t k) { return rows >= 0 && rows < (1ll << 30) && n >= 1 && n < (1 << 28) && k >= 1 && k < (1 << 28); }
+
+extern "C" hap_status hap_expert_matmul(int32_t form, int32_t dtype, int32_t out_dtype, int32_t accumulate, int32_t E, int64_t rows, int32_t N, int32_t K,
+                                        const int64_t *offsets, const void *a, int64_t lda, const void *b, int64_t ldb, void *out, int64_t ldo, void *stream)
+{
+    if (form < HAP_EXPERT_FORWARD || form > HAP_EXPERT_GRAD_WEIGHT || !dtype16(dtype) || (out_dtype != dtype && out_dtype != HAP_FP32)) return HAP_E_INVALID;
+    if (E < 1 || E > MAX_GROUPS || !sizes_fit(rows, N, K)) return HAP_E_INVALID;
+    const bool grad_w = form == HAP_EXPERT_GRAD_WEIGHT;
+    if (!offsets || (!out && (rows > 0 || grad_w)) || (rows > 0 && (!a || !b))) return HAP_E_INVALID;
+    if (lda < (form == HAP_EXPERT_FORWARD ? K : N) || ldb < K || ldo < (form == HAP_EXPERT_FORWARD ? N : K)) return HAP_E_INVALID;
+    if (!aligned(a, 2) || !aligned(b, 2) || !aligned(out, size_of(out_dtype)) || !aligned(offsets, 8)) return HAP_E_INVALID;
+    if (rows == 0 && (!grad_w || accumulate)) return HAP_OK;
+    Args p{};
+    p.offsets = offsets, p.groups = E, p.rows = (int)rows;
+    p.mdim = N, p.ncols = form == HAP_EXPERT_FORWARD ? N : K, p.kdim = form == HAP_EXPERT_FORWARD ? K : N;
+    p.a = a, p.b = b, p.lda = lda, p.ldb = ldb, p.bgroup = (int64_t)N * ldb;
+    p.out = out, p.ldo = ldo, p.ogroup = grad_w ? (int64_t)N * ldo : 0;
+    p.out32 = out_dtype == HAP_FP32, p.accumulate = accumulate != 0;
+    cudaStream_t s = (cudaStream_t)stream;
+#define HAP_BY_TYPE(FORM, EPI) (dtype == HAP_BF16 ? launch_product<__nv_bfloat16, FORM, EPI>(p, s) : launch_product<__half, FORM, EPI>(p, s))
+    return form == HAP_EXPERT_FORWARD ? HAP_BY_TYPE(NT, STORE) : grad_w ? HAP_BY_TYPE(TN, STORE) : HAP_BY_TYPE(NN, STORE);
+}
+
+extern "C" hap_status hap_expert_gated(int32_t dtype, int32_t E, int64_t rows, int32_t H, int32_t F, const int64_t *offsets, const void *x, int64_t ldx,
+                                       const void *w, int64_t ldw, void *gu, int64_t ldgu, void *h, int64_t ldh, void *stream)
+{
+    if (!dtype16(dtype) || E < 1 || E > MAX_GROUPS || !sizes_fit(rows, 2ll * F, H)) return HAP_E_INVALID;
+    if (!offsets || (rows > 0 && (!x || !w || !h))) return HAP_E_INVALID;
+    if (ldx < H || ldw < H || ldh < F || (gu && ldgu < 2ll * F)) return HAP_E_INVALID;
+    if (!aligned(x, 2) || !aligned(w, 2) || !aligned(gu, 2) || !aligned(h, 2) || !aligned(offsets, 8)) return HAP_E_INVALID;
+    if (rows == 0) return HAP_OK;
+    Args p{};
+    p.offsets = offsets, p.groups = E, p.rows = (int)rows, p.ncols = F, p.kdim = H;
+    p.a = x, p.b = w, p.lda = ldx, p.ldb = ldw, p.bgroup = 2ll * F * ldw;
+    p.out = gu, p.ldo = ldgu, p.h = h, p.ldh = ldh;
+    cudaStream_t s = (cudaStream_t)stream;
+    return HAP_BY_TYPE(NT, GATED);
+}
+
+extern "C" hap_status hap_expert_gated_backward(int32_t dtype, int32_t E, int64_t rows, int32_t H, int32_t F, const int64_t *offsets, const void *dy,
+                                                int64_t ldy, const void *w2, int64_t ldw, const void *gu, int64_t ldgu, void *dgu, int64_t lddgu,
+                                                void *h, int64_t ldh, void *stream)
+{
+    if (!dtype16(dtype) || E < 1 || E > MAX_GROUPS || !sizes_fit(rows, 2ll * F, H)) return HAP_E_INVALID;
+    if (!offsets || (rows > 0 && (!dy || !w2 || !gu || !dgu))) return HAP_E_INVALID;
+    if (ldy < H || ldw < F || ldgu < 2ll * F || lddgu < 2ll * F || (h && ldh < F)) return HAP_E_INVALID;
+    if (!aligned(dy, 2) || !aligned(w2, 2) || !aligned(gu, 2) || !aligned(dgu, 2) || !aligned(h, 2) || !aligned(offsets, 8)) return HAP_E_INVALID;
+    if (gu == dgu && ldgu != lddgu) return HAP_E_INVALID;
+    if (rows == 0) return HAP_OK;
+    Args p{};
+    p.offsets = offsets, p.groups = E, p.rows = (int)rows, p.ncols = F, p.kdim = H;
+    p.a = dy, p.b = w2, p.lda = ldy, p.ldb = ldw, p.bgroup = (int64_t)H * ldw;
+    p.out = dgu, p.ldo = lddgu, p.gu = gu, p.ldgu = ldgu, p.h = h, p.ldh = ldh;
+    cudaStream_t s = (cudaStream_t)stream;
+    return HAP_BY_TYPE(NN, GATED_BACK);
+}
+
+// ---- cross entropy of the output head ----------------------------------------------------------------------------------
+// Columns of the vocabulary per piece of the backward pass: the piece's softmax gradients (rows x columns x 2 bytes) stay in
+// about 96 MiB, most of L2.
+static int64_t piece_columns(int64_t rows, int64_t V)
+{
+    int64_t c = (96ll << 20) / (2 * (rows < 1 ? 1 : rows)) / TILE_N * TILE_N;
+    if (c < 8 * TILE_N) c = 8 * TILE_N;
+    const int64_t whole = ceil_div(V, TILE_N) * TILE_N;
+    return c < whole ? c : whole;
+}
+static uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
+
+static bool loss_sizes(int64_t rows, int64_t H, int64_t V) { return sizes_fit(rows, V, H); }
+
+extern "C" hap_status hap_linear_cross_entropy_workspace(int64_t rows, int32_t H, int64_t V, uint64_t *host_bytes)
+{
+    if (!host_bytes || !loss_sizes(rows, H, V)) return HAP_E_INVALID;
+    const uint64_t n = (uint64_t)rows, piece = (uint64_t)piece_columns(rows, V);
+    const uint64_t forward = up256(ceil_div(V, TILE_N) * n * 8) + up256(n * 4);
+    const uint64_t backward = up256(n * piece * 2) + ((int64_t)piece < V ? up256(n * H * 4) : 0);
+    *host_bytes = forward > backward ? forward : backward;
+    return HAP_OK;
+}
+
+static hap_status loss_args(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *x, int64_t ldx, const void *w, int64_t ldw, const int64_t *target,
+                            const void *workspace, uint64_t bytes)
+{
+    if (!dtype16(dtype) || !loss_sizes(rows, H, V) || ldx < H || ldw < H || !aligned(x, 2) || !aligned(w, 2) || !aligned(target, 8)) return HAP_E_INVALID;
+    if (rows > 0 && (!x || !w || !target)) return HAP_E_INVALID;
+    uint64_t need = 0;
+    hap_linear_cross_entropy_workspace(rows, H, V, &need);
+    return need && (!workspace || bytes < need || !aligned(workspace, 256)) ? HAP_E_INVALID : HAP_OK;
+}
+
+extern "C" hap_status hap_linear_cross_entropy(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *x, int64_t ldx, const void *w, int64_t ldw,
+                                               const int64_t *target, int64_t ignore, float *loss, float *lse, void *workspace, uint64_t bytes, void *stream)
+{
+    const hap_status bad = loss_args(dtype, rows, H, V, x, ldx, w, ldw, target, workspace, bytes);
+    if (bad != HAP_OK) return bad;
+    if (rows == 0) return HAP_OK;
+    if (!loss || !lse || !aligned(loss, 4) || !aligned(lse, 4)) return HAP_E_INVALID;
+    const int tiles = (int)ceil_div(V, TILE_N);
+    Args p{};
+    p.groups = 1, p.rows = (int)rows, p.ncols = (int)V, p.kdim = H;
+    p.a = x, p.b = w, p.lda = ldx, p.ldb = ldw;
+    p.target = target, p.ignore = ignore, p.vocab = V;
+    p.part = (float2 *)workspace, p.at_target = (float *)((char *)workspace + up256((uint64_t)tiles * rows * 8));
+    cudaStream_t s = (cudaStream_t)stream;
+    const hap_status st = HAP_BY_TYPE(NT, LSE);
+    if (st != HAP_OK) return st;
+    loss_rows_kernel<<<(unsigned)ceil_div(rows, 32), 256, 0, s>>>(p.part, tiles, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
+    return launched();
+}
+
+extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *x, int64_t ldx, const void *w,
+                                                        int64_t ldw, const int64_t *target, int64_t ignore, const float *lse, const float *grad, void *dx,
+                                                        int64_t lddx, void *dw, int64_t lddw, void *workspace, uint64_t bytes, void *stream)
+{
+    const hap_status bad = loss_args(dtype, rows, H, V, x, ldx, w, ldw, target, workspace, bytes);
+    if (bad != HAP_OK) return bad;
+    if (!grad || !aligned(grad, 4) || !aligned(dx, 2) || !aligned(dw, 2) || (dx && lddx < H) || (dw && lddw < H)) return HAP_E_INVALID;
+    if (rows > 0 && (!lse || !aligned(lse, 4))) return HAP_E_INVALID;
+    cudaStream_t s = (cudaStream_t)stream;
+    const int64_t piece = piece_columns(rows, V);
+    void *d = workspace;
+    float *acc = (float *)((char *)workspace + up256((uint64_t)rows * piece * 2));
+    for (int64_t c0 = 0; c0 < V; c0 += piece) {
+        const int64_t cols = V - c0 < piece ? V - c0 : piece;
+        const char *wc = (const char *)w + c0 * ldw * 2;
+        hap_status st = HAP_OK;
+        if (rows > 0) {
+            Args p{};
+            p.groups = 1, p.rows = (int)rows, p.ncols = (int)cols, p.kdim = H;
+            p.a = x, p.b = wc, p.lda = ldx, p.ldb = ldw;
+            p.target = target, p.ignore = ignore, p.vocab = V, p.col0 = (int)c0, p.lse = lse;
+            p.out = d, p.ldo = piece;
+            st = HAP_BY_TYPE(NT, DLOGIT);
+        }
+        if (st == HAP_OK && dx && rows > 0) {
+            Args p{};
+            p.groups = 1, p.rows = (int)rows, p.ncols = H, p.kdim = (int)cols;
+            p.a = d, p.b = wc, p.lda = piece, p.ldb = ldw;
+            p.out = dx, p.ldo = lddx, p.acc32 = acc, p.first = c0 == 0, p.last = c0 + cols == V;
+            p.scale = grad, p.scale_by = 1.0f / DLOGIT_SCALE;
+            st = HAP_BY_TYPE(NN, SUM32);
+        }
+        if (st == HAP_OK && dw) {
+            Args p{};
+            p.groups = 1, p.rows = (int)rows, p.mdim = (int)cols, p.ncols = H;
+            p.a = d, p.b = x, p.lda = piece, p.ldb = ldx;
+            p.out = (char *)dw + c0 * lddw * 2, p.ldo = lddw;
+            p.scale = grad, p.scale_by = 1.0f / DLOGIT_SCALE;
+            st = HAP_BY_TYPE(TN, STORE);
+        }
+        if (st != HAP_OK) return st;
+    }
+    return HAP_OK;
+}
+
+// ---- AdamW ------------------------------------------------------------------------------------------------------------
+// Descriptors of one launch: a short list for the usual call on few tensors, whose arguments are copied faster, and one that
+// fills most of the 32 KB that a launch may carry.
+constexpr int FEW = 32, MANY = 440;
+
+template <int N, typename F> static hap_status adamw_launches(const hap_adamw_tensor *tensors, int32_t n, float *const *m_out, float *const *v_out, F &&launch)
+{
+    AdamwList<N> list;
+    for (int i = 0; i < n;) {
+        list.n = 0;
+        uint64_t chunks = 0;
+        for (; i < n && list.n < N; i++) {
+            const hap_adamw_tensor &t = tensors[i];
+            if (!t.count) continue;
+            const uint64_t c = (t.count + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+            if (chunks + c > INT32_MAX) {
+                if (!list.n) return HAP_E_RANGE;
+                break;
+            }
+            list.t[list.n] = {m_out ? m_out[i] : t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, m_out || v_out ? (void *)(v_out ? v_out[i] : nullptr) : t.copy, t.count};
+            if (!m_out && v_out) list.t[list.n].p = nullptr;
+            list.first[list.n++] = (unsigned)chunks;
+            chunks += c;
+        }
+        if (!list.n) break;
+        launch(list, (unsigned)chunks);
+        const hap_status st = launched();
+        if (st != HAP_OK) return st;
+    }
+    return HAP_OK;
+}
+
+template <typename P, typename G> static hap_status adamw_run(const hap_adamw_tensor *tensors, int32_t n, int bits, const AdamwFactors &f, const float *grad_scale, cudaStream_t s)
+{
+    auto launch = [&](auto &list, unsigned chunks) {
+        constexpr int N = sizeof(list.t) / sizeof(AdamwTensor);
+        if (bits == 8) adamw8_kernel<P, G, N><<<chunks, 256, 0, s>>>(list, f, grad_scale);
+        else adamw_kernel<P, G, N><<<chunks, 256, 0, s>>>(list, f, grad_scale);
+    };
+    return n <= FEW ? adamw_launches<FEW>(tensors, n, nullptr, nullptr, launch) : adamw_launches<MANY>(tensors, n, nullptr, nullptr, launch);
+}
+
+extern "C" hap_status hap_adamw_step(const hap_adamw_tensor *tensors, int32_t n, int32_t pt, int32_t gt, int32_t ct, int32_t bits,
+                                     const hap_adamw_options *o, const float *grad_scale, void *stream)
+{
+    if (n < 0 || (n > 0 && !tensors) || !o || pt < HAP_BF16 || pt > HAP_FP32 || gt < HAP_BF16 || gt > HAP_FP32 || (bits != 32 && bits != 8)) return HAP_E_INVALID;
+    if (gt != pt && gt != HAP_FP32 && pt != HAP_FP32) return HAP_E_INVALID;
+    if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1 && o->eps >= 0 && o->step >= 1) || !isfinite(o->lr) || !isfinite(o->weight_decay) || !isfinite(o->eps) || !aligned(grad_scale, 4)) return HAP_E_INVALID;
+    for (int i = 0; i < n; i++) {
+        const hap_adamw_tensor &t = tensors[i];
+        if (!t.count) continue;
+        if (t.count > (1ull << 42)) return HAP_E_RANGE;
+        if (!t.param || !t.grad || !t.m || !t.v || !aligned(t.param, size_of(pt)) || !aligned(t.grad, size_of(gt))) return HAP_E_INVALID;
+        if (bits == 32 ? !aligned(t.m, 4) || !aligned(t.v, 4) : !t.m_scale || !t.v_scale || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4)) return HAP_E_INVALID;
+        if (t.copy && (!dtype16(ct) || pt != HAP_FP32 || !aligned(t.copy, 2))) return HAP_E_INVALID;
+    }
+    const double c1 = 1 - pow(o->beta1, (double)o->step), c2 = 1 - pow(o->beta2, (double)o->step);
+    const AdamwFactors f = {(float)o->beta1, (float)o->beta2, (float)(1 - o->beta1), (float)(1 - o->beta2), (float)(1 - o->lr * o->weight_decay),
+                            (float)(o->lr / c1), (float)(1 / sqrt(c2)), (float)o->eps, ct == HAP_FP16};
+    cudaStream_t s = (cudaStream_t)stream;
+    if (pt == HAP_BF16) return gt == HAP_FP32 ? adamw_run<__nv_bfloat16, float>(tensors, n, bits, f, grad_scale, s) : adamw_run<__nv_bfloat16, __nv_bfloat16>(tensors, n, bits, f, grad_scale, s);
+    if (pt == HAP_FP16) return gt == HAP_FP32 ? adamw_run<__half, float>(tensors, n, bits, f, grad_scale, s) : adamw_run<__half, __half>(tensors, n, bits, f, grad_scale, s);
+    return gt == HAP_FP32 ? adamw_run<float, float>(tensors, n, bits, f, grad_scale, s)
+         : gt == HAP_BF16 ? adamw_run<float, __nv_bfloat16>(tensors, n, bits, f, grad_scale, s) : adamw_run<float, __half>(tensors, n, bits, f, grad_scale, s);
+}
+
+extern "C" hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *const *host_m, float *const *host_v, void *stream)
+{
+    if (n < 0 || (n > 0 && !tensors)) return HAP_E_INVALID;
+    if (!host_m && !host_v) return HAP_OK;
+    for (int i = 0; i < n; i++) {
+        const hap_adamw_tensor &t = tensors[i];
+        if (!t.count) continue;
+        if (t.count > (1ull << 42)) return HAP_E_RANGE;
+        if (!t.m || !t.v || !t.m_scale || !t.v_scale || !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4)) return HAP_E_INVALID;
+        if ((host_m && !aligned(host_m[i], 4)) || (host_v && !aligned(host_v[i], 4))) return HAP_E_INVALID;
+    }
+    cudaStream_t s = (cudaStream_t)stream;
+    auto launch = [&](auto &list, unsigned chunks) {
+        constexpr int N = sizeof(list.t) / sizeof(AdamwTensor);
+        adamw_values_kernel<N><<<chunks, 256, 0, s>>>(list);
+    };
+    return n <= FEW ? adamw_launches<FEW>(tensors, n, host_m, host_v, launch) : adamw_launches<MANY>(tensors, n, host_m, host_v, launch);
+}
+
+__device__ unsigned operator_error;
+
+extern "C" hap_status hap_operator_status(uint32_t *host_bits)
+{
+    if (!host_bits) return HAP_E_INVALID;
+    *host_bits = 0;
+    const unsigned zero = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(host_bits, operator_error, sizeof zero) != cudaSuccess) return HAP_E_CUDA;
+    return cudaMemcpyToSymbol(operator_error, &zero, sizeof zero) == cudaSuccess ? HAP_OK : HAP_E_CUDA;
+}

@@ -1,0 +1,425 @@
+// Products of the training operators: tiles of grouped matrix products, their scheduling over the groups and what happens to
+// a finished tile.  Three forms share everything here:
+//   NT  out[i][n] = sum_k a[i][k] w_e[n][k]      rows i of group e (forward; logits)
+//   NN  out[i][n] = sum_k a[i][k] w_e[k][n]      (gradient of the input)
+//   TN  out_e[m][n] = sum over rows i of group e of a[i][m] b[i][n]   (gradient of the weight)
+// Group e holds rows offsets[e] .. offsets[e+1]; without offsets there is one group of all rows.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace hapop {
+
+enum Form { NT = 0, NN = 1, TN = 2 };
+enum Epilogue {
+    STORE = 0,      // out = scale * acc (+ out)
+    GATED = 1,      // tile columns are 128 of g and the same 128 of u: keep them, h = silu(g) u
+    GATED_BACK = 2, // acc is dh: dg, du and h from it and the kept g, u
+    LSE = 3,        // logits: the row's maximum and sum of exponentials over the tile's columns, the target's logit
+    DLOGIT = 4,     // logits again: (softmax - one-hot) * 2^15 in 16 bits
+    SUM32 = 5       // gradient of the loss's input over several pieces of the vocabulary: kept in 32 bits between them
+};
+
+constexpr int MAX_GROUPS = 1024;
+constexpr int TILE_N = 256;         // columns of a tile in every variant (the loss's partial results are per tile)
+constexpr int BAND = 16;            // row tiles of a group that are worked on side by side, for reuse in L2
+// softmax gradients are held in 16 bits times this: fp16's normal range ends at 6e-5, a probability of a large vocabulary
+// is smaller; 2^15 keeps 1 below 65504 and 2e-9 normal.  The factor is a power of two and leaves with the gradient's scale.
+constexpr float DLOGIT_SCALE = 32768.0f;
+
+struct Args {
+    const int64_t *offsets;         // [groups + 1] or null
+    int groups, rows;               // rows: of a (and of b in TN)
+    int mdim;                       // TN: rows of out_e
+    int ncols;                      // columns of out (GATED: columns of h)
+    int kdim;                       // contraction in NT, NN
+    const void *a, *b;              // operands as the plain variant reads them
+    int64_t lda, ldb, bgroup;       // bgroup: distance of two groups' w
+    // epilogue
+    void *out;
+    int64_t ldo, ogroup;            // ogroup: distance of two groups' out (TN)
+    int out32, accumulate;
+    const float *scale;             // device scalar, or null: 1
+    float scale_by;                 // times this
+    const void *gu;                 // GATED_BACK: kept g | u
+    int64_t ldgu;
+    void *h;
+    int64_t ldh;
+    const int64_t *target;          // LSE, DLOGIT
+    int64_t ignore;
+    int64_t vocab;
+    int col0;                       // first column's place in the vocabulary
+    float2 *part;                   // [column tiles][rows]
+    float *at_target;               // [rows]
+    const float *lse;
+    float *acc32;                   // SUM32: [rows][ncols]
+    int first, last;
+};
+
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_float(float x) { return x; }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ float from_float(float x) { return x; }
+__device__ __forceinline__ uint32_t pack2(float x, float y, __nv_bfloat16) { __nv_bfloat162 v = __floats2bfloat162_rn(x, y); return *(uint32_t *)&v; }
+__device__ __forceinline__ uint32_t pack2(float x, float y, __half) { __half2 v = __floats2half2_rn(x, y); return *(uint32_t *)&v; }
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) { return __bfloat1622float2(*(__nv_bfloat162 *)&w); }
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*(__half2 *)&w); }
+
+// 32 consecutive values of a row, as many as the row has: in 16-byte pieces where the address allows
+template <typename T> __device__ __forceinline__ void store32(T *p, const float (&v)[32], int n)
+{
+    if (n >= 32 && ((uintptr_t)p & 15) == 0) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) ((float4 *)p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                ((uint4 *)p)[i] = make_uint4(pack2(v[8 * i], v[8 * i + 1], T()), pack2(v[8 * i + 2], v[8 * i + 3], T()),
+                                             pack2(v[8 * i + 4], v[8 * i + 5], T()), pack2(v[8 * i + 6], v[8 * i + 7], T()));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; i++)
+        if (i < n) p[i] = from_float<T>(v[i]);
+}
+template <typename T> __device__ __forceinline__ void load32(const T *p, float (&v)[32], int n)
+{
+    if (n >= 32 && ((uintptr_t)p & 15) == 0) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float4 x = ((const float4 *)p)[i];
+                v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint4 x = ((const uint4 *)p)[i];
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float2 f = unpack2(w[j], T());
+                    v[8 * i + 2 * j] = f.x, v[8 * i + 2 * j + 1] = f.y;
+                }
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
+}
+
+// What happens to the 32 columns col .. of one output row.  `row`: row of out (in TN of out_e, and then e is its group);
+// v: the sums; v2: those of u in GATED.  The softmax statistics of a row over a tile are held in m (maximum) and s.
+template <typename T, int EPI> struct RowEpilogue {
+    const Args &p;
+    const int64_t row;
+    const int e;
+    float m = -INFINITY, s = 0.0f;
+    int64_t target = -1;            // LSE, DLOGIT: column of the row's target in this launch's columns, or outside of them
+    bool kept = true;
+    float lse = 0.0f;
+    __device__ RowEpilogue(const Args &args, int64_t row, int e, bool live) : p(args), row(row), e(e)
+    {
+        if constexpr (EPI == LSE || EPI == DLOGIT) {
+            if (live) {
+                const int64_t t = p.target[row];
+                kept = t != p.ignore && t >= 0 && t < p.vocab;
+                target = t - p.col0;
+                if constexpr (EPI == DLOGIT) lse = p.lse[row];
+            }
+        }
+    }
+    __device__ __forceinline__ void columns(int col, float (&v)[32], float (&v2)[32])
+    {
+        const int n = p.ncols - col;
+        if (n <= 0) return;
+        if constexpr (EPI == STORE) {
+            const float f = p.scale ? *p.scale * p.scale_by : 1.0f;
+            if (p.scale) {
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] *= f;
+            }
+            if (p.out32) {
+                float *o = (float *)p.out + e * p.ogroup + row * p.ldo + col;
+                if (p.accumulate) {
+                    load32(o, v2, n);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) v[i] += v2[i];
+                }
+                store32(o, v, n);
+            } else {
+                T *o = (T *)p.out + e * p.ogroup + row * p.ldo + col;
+                if (p.accumulate) {
+                    load32(o, v2, n);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) v[i] += v2[i];
+                }
+                store32(o, v, n);
+            }
+        }
+        if constexpr (EPI == GATED) {
+            if (p.out) {
+                store32((T *)p.out + row * p.ldo + col, v, n);
+                store32((T *)p.out + row * p.ldo + p.ncols + col, v2, n);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i++) v[i] = v[i] / (1.0f + __expf(-v[i])) * v2[i];
+            store32((T *)p.h + row * p.ldh + col, v, n);
+        }
+        if constexpr (EPI == GATED_BACK) {
+            float g[32];
+            load32((const T *)p.gu + row * p.ldgu + col, g, n);
+            load32((const T *)p.gu + row * p.ldgu + p.ncols + col, v2, n);
+#pragma unroll
+            for (int i = 0; i < 32; i++) {      // s = sigma(g): dg = dh u (s + g s (1 - s)), du = dh g s, h = g s u
+                const float s = 1.0f / (1.0f + __expf(-g[i]));
+                const float gs = g[i] * s, dh = v[i], u = v2[i];
+                v[i] = dh * u * fmaf(gs, 1.0f - s, s);
+                v2[i] = dh * gs;
+                g[i] = gs * u;
+            }
+            store32((T *)p.out + row * p.ldo + col, v, n);
+            store32((T *)p.out + row * p.ldo + p.ncols + col, v2, n);
+            if (p.h) store32((T *)p.h + row * p.ldh + col, g, n);
+        }
+        if constexpr (EPI == LSE) {
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 32; i++) {
+                if (i >= n) v[i] = -INFINITY;
+                top = fmaxf(top, v[i]);
+            }
+            const float from = top == -INFINITY ? 0.0f : top * 1.4426950408889634f;
+            float sum = m == -INFINITY ? 0.0f : s * exp2f(fmaf(m, 1.4426950408889634f, -from));
+#pragma unroll
+            for (int i = 0; i < 32; i++) sum += exp2f(fmaf(v[i], 1.4426950408889634f, -from));
+            m = top, s = sum;
+            if (target >= col && target < col + 32 && target < p.ncols) {
+                float z = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 32; i++) z = col + i == target ? v[i] : z;
+                p.at_target[row] = z;
+            }
+        }
+        if constexpr (EPI == DLOGIT) {
+            const float from = lse * 1.4426950408889634f;
+#pragma unroll
+            for (int i = 0; i < 32; i++) {
+                float d = exp2f(fmaf(v[i], 1.4426950408889634f, -from));
+                d = col + i == target ? d - 1.0f : d;
+                v[i] = kept ? d * DLOGIT_SCALE : 0.0f;
+            }
+            store32((T *)p.out + row * p.ldo + col, v, n);
+        }
+        if constexpr (EPI == SUM32) {
+            float *a = p.acc32 + row * (int64_t)p.ncols + col;
+            if (!p.first) {
+                load32(a, v2, n);
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] += v2[i];
+            }
+            if (p.last) {
+                const float f = *p.scale * p.scale_by;
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] *= f;
+                store32((T *)p.out + row * p.ldo + col, v, n);
+            } else {
+                store32(a, v, n);
+            }
+        }
+    }
+    __device__ __forceinline__ void end(int tile_n)
+    {
+        if constexpr (EPI == LSE) p.part[(int64_t)tile_n * p.rows + row] = make_float2(m, s);
+    }
+};
+
+// Tiles of all groups in one order.  Offsets come from device memory: they are clamped to the rows and made ascending here,
+// so that no offset can lead outside of the operands.
+template <int BM> struct Schedule {
+    int bound[MAX_GROUPS + 1];
+    int first[MAX_GROUPS + 1];      // first tile of each group (NT, NN)
+    struct Tile { int e, m, n, lo, hi; };
+
+    __device__ static int row_tiles(int n) { return (n + BM - 1) / BM; }
+    // by all threads of the first warp
+    __device__ void build(const Args &p, int form, int col_tiles, int lane)
+    {
+        if (!p.offsets) {
+            if (lane < 2) bound[lane] = lane ? p.rows : 0, first[lane] = lane ? row_tiles(p.rows) * col_tiles : 0;
+            __syncwarp();
+            return;
+        }
+        int below = 0, tiles = 0;   // carried over the blocks of 32
+        for (int i0 = 0; i0 <= p.groups; i0 += 32) {
+            const int i = i0 + lane;
+            int64_t o = i <= p.groups ? p.offsets[i] : 0;
+            int b = o < 0 ? 0 : o > p.rows ? p.rows : (int)o;
+            b = max(b, below);
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int x = __shfl_up_sync(~0u, b, d);
+                if (lane >= d) b = max(b, x);
+            }
+            int prev = __shfl_up_sync(~0u, b, 1);
+            if (lane == 0) prev = below;
+            int t = i > 0 && i <= p.groups ? row_tiles(b - prev) * col_tiles : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int x = __shfl_up_sync(~0u, t, d);
+                if (lane >= d) t += x;
+            }
+            t += tiles;
+            if (i <= p.groups) bound[i] = b, first[i] = t;
+            below = __shfl_sync(~0u, b, 31);
+            tiles = __shfl_sync(~0u, t, 31);
+        }
+        __syncwarp();
+    }
+    __device__ int total(const Args &p, int form, int col_tiles) const
+    {
+        return form == TN ? p.groups * row_tiles(p.mdim) * col_tiles : first[p.groups];
+    }
+    __device__ Tile tile(const Args &p, int form, int col_tiles, int t) const
+    {
+        Tile r;
+        int rows;
+        if (form == TN) {
+            rows = p.mdim;
+            const int per = row_tiles(rows) * col_tiles;
+            r.e = t / per;
+            t -= r.e * per;
+        } else {
+            int lo = 0, hi = p.groups - 1;                  // last group whose first tile is not behind t
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= t) lo = mid; else hi = mid - 1;
+            }
+            r.e = lo;
+            t -= first[lo];
+            rows = bound[lo + 1] - bound[lo];
+        }
+        r.lo = bound[r.e], r.hi = bound[r.e + 1];
+        const int mt = row_tiles(rows), band = min(mt, BAND);
+        const int which = t / (band * col_tiles);
+        t -= which * band * col_tiles;
+        const int high = min(band, mt - which * band);
+        r.n = t / high;
+        r.m = which * band + t - r.n * high;
+        return r;
+    }
+};
+
+// ---- plain variant ----------------------------------------------------------------------------------------------------
+// For operands that a tensor map cannot describe (addresses or row distances that are not multiples of 16 bytes).  Tiles of
+// 32 rows and 256 columns, a thread sums 4 x 8 of them in fp32 from shared memory.
+constexpr int PM = 32, PK = 16;
+
+template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) plain_product_kernel(const __grid_constant__ Args p)
+{
+    __shared__ Schedule<PM> sched;
+    __shared__ float shared[PM * (TILE_N + 1)];     // the tile's sums; before that the operands' slices, which are smaller
+    float (*sc)[TILE_N + 1] = (float (*)[TILE_N + 1])shared;
+    float (*sa)[PM + 1] = (float (*)[PM + 1])shared, (*sb)[TILE_N + 1] = (float (*)[TILE_N + 1])(shared + PK * (PM + 1));
+    const int tid = threadIdx.x;
+    constexpr int BN = EPI == GATED ? TILE_N / 2 : TILE_N;
+    const int col_tiles = (p.ncols + BN - 1) / BN;
+    if (tid < 32) sched.build(p, FORM, col_tiles, tid);
+    __syncthreads();
+    const int total = sched.total(p, FORM, col_tiles);
+    for (int t = blockIdx.x; t < total; t += gridDim.x) {
+        const auto tile = sched.tile(p, FORM, col_tiles, t);
+        const int m0 = tile.m * PM, n0 = tile.n * BN;
+        const int mrows = FORM == TN ? p.mdim - m0 : tile.hi - tile.lo - m0;        // rows of out from m0 on
+        const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
+        const T *a = (const T *)p.a, *b = (const T *)p.b + (FORM == TN ? 0 : tile.e * p.bgroup);
+        float acc[4][8] = {};
+        const int tm = (tid & 7) * 4, tn = (tid >> 3);                              // columns tn + 32 j
+        for (int k0 = 0; k0 < K; k0 += PK) {
+            for (int i = tid; i < PM * PK; i += 256) {
+                const int m = FORM == TN ? i % PM : i / PK, k = FORM == TN ? i / PM : i % PK;
+                const bool in = m < mrows && k0 + k < K;
+                sa[k][m] = !in ? 0.0f : to_float(FORM == TN ? a[(int64_t)(tile.lo + k0 + k) * p.lda + m0 + m] : a[(int64_t)(tile.lo + m0 + m) * p.lda + k0 + k]);
+            }
+            for (int i = tid; i < TILE_N * PK; i += 256) {
+                const int n = FORM == NT ? i / PK : i % TILE_N, k = FORM == NT ? i % PK : i / TILE_N;
+                const int col = n0 + (EPI == GATED ? n % BN : n);
+                const bool in = col < p.ncols && k0 + k < K;
+                const int64_t from = EPI == GATED && n >= BN ? col + p.ncols : col;
+                sb[k][n] = !in ? 0.0f : to_float(FORM == NT ? b[from * p.ldb + k0 + k] : b[(int64_t)((FORM == TN ? tile.lo : 0) + k0 + k) * p.ldb + col]);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < PK; k++) {
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) x[i] = sa[k][tm + i];
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const float y = sb[k][tn + 32 * j];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) acc[i][j] = fmaf(x[i], y, acc[i][j]);
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) sc[tm + i][tn + 32 * j] = acc[i][j];
+        __syncthreads();
+        // a row's columns stay with one thread where its statistics run over them; else 8 threads share the row
+        const int r = tid & 31, c = tid >> 5;
+        if (r < mrows && (EPI != LSE || c == 0)) {
+            RowEpilogue<T, EPI> row(p, (FORM == TN ? 0 : (int64_t)tile.lo) + m0 + r, FORM == TN ? tile.e : 0, true);
+            float v[32], v2[32];
+            for (int q = EPI == LSE ? 0 : c; q < BN / 32; q += 8 - 7 * (EPI == LSE)) {
+#pragma unroll
+                for (int i = 0; i < 32; i++) v[i] = sc[r][q * 32 + i], v2[i] = EPI == GATED ? sc[r][BN + q * 32 + i] : 0.0f;
+                row.columns(n0 + q * 32, v, v2);
+            }
+            row.end(tile.n);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- the loss from the tiles' statistics ------------------------------------------------------------------------------
+// lse = M + log(sum_t s_t exp(m_t - M)).  A block takes 32 rows, its warps every eighth tile; rows of one tile lie side by side.
+__global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int tiles, int rows, const float *at_target, const int64_t *target,
+                                                        int64_t ignore, int V, float *loss, float *lse)
+{
+    __shared__ float2 sh[8][32];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    float m = -INFINITY, s = 0.0f;
+    if (row < rows)
+        for (int t = w; t < tiles; t += 8) {
+            const float2 x = part[(int64_t)t * rows + row];
+            const float top = fmaxf(m, x.x);
+            const float from = top == -INFINITY ? 0.0f : top;
+            s = s * expf(m - from) + x.y * expf(x.x - from);
+            m = top;
+        }
+    sh[w][lane] = make_float2(m, s);
+    __syncthreads();
+    if (w || row >= rows) return;
+    float top = -INFINITY;
+    for (int i = 0; i < 8; i++) top = fmaxf(top, sh[i][lane].x);
+    const float from = top == -INFINITY ? 0.0f : top;
+    s = 0.0f;
+    for (int i = 0; i < 8; i++) s += sh[i][lane].y * expf(sh[i][lane].x - from);
+    const float l = top + logf(s);
+    lse[row] = l;
+    const int64_t t = target[row];
+    loss[row] = t == ignore ? 0.0f : t < 0 || t >= V ? NAN : l - at_target[row];
+}
+
+} // namespace hapop
