@@ -1,10 +1,14 @@
 // Host side of the training operators: checks of arguments, choice of variant, launches.
 #include "hap_adamw.cuh"
-#include "hap_products.cuh"
+#include "hap_products_tc.cuh"
 
 #include <math.h>
 
 using namespace hapop;
+
+#ifndef HAP_PAIR_ROWS
+#define HAP_PAIR_ROWS 128
+#endif
 
 static hap_status launched() { return cudaGetLastError() == cudaSuccess ? HAP_OK : HAP_E_CUDA; }
 
@@ -16,15 +20,75 @@ static int sm_count()
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
+// ---- tensor maps ------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encode_tiled()
 {
-    const int sms = sm_count();
-    if (!sms) return HAP_E_CUDA;
+    static const EncodeTiled f = [] {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) fn = nullptr;
+        return (EncodeTiled)fn;
+    }();
+    return f;
+}
+
+// `count` matrices [rows][cols] of 16-bit values, read in boxes of 64 columns and box_rows rows; what lies outside arrives as 0
+static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols, int64_t rows, int64_t count, int64_t ld, int64_t distance, int box_rows)
+{
+    if (count < 2) distance = ld * rows;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count}, strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)distance * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, each[3] = {1, 1, 1};
+    return encode_tiled()(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (void *)base, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// whether TMA can address an operand
+static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
+
+template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(const Args &p, int sms, cudaStream_t stream)
+{
+    using S = Shape<CG>;
+    const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
+    const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, S::BM) : ceil_div(p.rows, S::BM) + (p.offsets ? p.groups : 0));
+    if (most > INT32_MAX) return HAP_E_RANGE;
+    constexpr bool fp16 = TypeBits<T>::value == 0;
+    CUtensorMap ma, mb;
+    const int64_t wrows = FORM == NT ? (EPI == GATED ? 2ll * p.ncols : p.ncols) : p.kdim;
+    const bool good = FORM == TN ? make_map(&ma, fp16, p.a, p.mdim, p.rows, 1, p.lda, 0, BK) && make_map(&mb, fp16, p.b, p.ncols, p.rows, 1, p.ldb, 0, BK)
+                                 : make_map(&ma, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 128) &&
+                                       make_map(&mb, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK);
+    if (!good) return HAP_E_CUDA;
+    constexpr int smem = 1024 + S::STAGES * S::STAGE + sizeof(Shared<CG>);
+    auto kernel = product_kernel<T, FORM, EPI, CG>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HAP_E_CUDA;
+    cudaLaunchConfig_t c{};
+    const int64_t at_once = sms / CG;
+    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(192), c.dynamicSmemBytes = smem, c.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
+    c.attrs = attr, c.numAttrs = CG > 1;
+    return cudaLaunchKernelEx(&c, kernel, p, ma, mb) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+}
+
+template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
+{
     const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, PM) : ceil_div(p.rows, PM) + p.groups);
     if (most > INT32_MAX) return HAP_E_RANGE;
     plain_product_kernel<T, FORM, EPI><<<(unsigned)(most < 4 * sms ? most : 4 * sms), 256, 0, stream>>>(p);
     return launched();
+}
+
+template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (!sms) return HAP_E_CUDA;
+    if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, sms, stream);
+    const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output
+    return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, sms, stream) : launch_tensor<T, FORM, EPI, 1>(p, sms, stream);
 }
 
 static bool dtype16(int32_t t) { return t == HAP_BF16 || t == HAP_FP16; }
@@ -271,8 +335,6 @@ extern "C" hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n
     };
     return n <= FEW ? adamw_launches<FEW>(tensors, n, host_m, host_v, launch) : adamw_launches<MANY>(tensors, n, host_m, host_v, launch);
 }
-
-__device__ unsigned operator_error;
 
 extern "C" hap_status hap_operator_status(uint32_t *host_bits)
 {
