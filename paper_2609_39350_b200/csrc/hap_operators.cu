@@ -2,6 +2,7 @@
 #include "hap_adamw.cuh"
 #include "hap_products_tc.cuh"
 
+#include <atomic>
 #include <math.h>
 
 using namespace hapop;
@@ -12,10 +13,20 @@ using namespace hapop;
 
 static hap_status launched() { return cudaGetLastError() == cudaSuccess ? HAP_OK : HAP_E_CUDA; }
 
-static int sm_count()
+// The current device and its multiprocessors; 0 of them: no device.  What does not change is asked once for each device.
+struct Device { int id = 0, sms = 0; };
+constexpr int DEVICES = 64;
+
+static Device device()
 {
-    int dev = 0, n = 0;
-    return cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0 ? n : 0;
+    static std::atomic<int> known[DEVICES];
+    Device d;
+    if (cudaGetDevice(&d.id) != cudaSuccess || d.id < 0) return d;
+    if (d.id < DEVICES) d.sms = known[d.id].load(std::memory_order_relaxed);
+    if (d.sms) return d;
+    if (cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, d.id) != cudaSuccess) d.sms = 0;
+    if (d.id < DEVICES) known[d.id].store(d.sms, std::memory_order_relaxed);
+    return d;
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -42,35 +53,47 @@ static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count}, strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)distance * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, each[3] = {1, 1, 1};
     return encode_tiled()(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (void *)base, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // whether TMA can address an operand
 static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
 
-template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(const Args &p, int sms, cudaStream_t stream)
+template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(Args p, Device d, cudaStream_t stream)
 {
-    using S = Shape<CG>;
+    using S = Shape<EPI, CG>;
     const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, S::BM) : ceil_div(p.rows, S::BM) + (p.offsets ? p.groups : 0));
     if (most > INT32_MAX) return HAP_E_RANGE;
     constexpr bool fp16 = TypeBits<T>::value == 0;
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, mo{};
     const int64_t wrows = FORM == NT ? (EPI == GATED ? 2ll * p.ncols : p.ncols) : p.kdim;
     const bool good = FORM == TN ? make_map(&ma, fp16, p.a, p.mdim, p.rows, 1, p.lda, 0, BK) && make_map(&mb, fp16, p.b, p.ncols, p.rows, 1, p.ldb, 0, BK)
                                  : make_map(&ma, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 128) &&
                                        make_map(&mb, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK);
     if (!good) return HAP_E_CUDA;
-    constexpr int smem = 1024 + S::STAGES * S::STAGE + sizeof(Shared<CG>);
+    if (EPI == STORE32 && FORM == TN && ((uintptr_t)p.out & 15) == 0 && p.ldo % 4 == 0 && p.ldo < (1ll << 35) && p.ogroup < (1ll << 35)) {
+        const cuuint64_t dims[3] = {(cuuint64_t)p.ncols, (cuuint64_t)p.mdim, (cuuint64_t)p.groups};
+        const cuuint64_t strides[2] = {(cuuint64_t)p.ldo * 4, (cuuint64_t)(p.groups > 1 ? p.ogroup : p.ldo * p.mdim) * 4};
+        const cuuint32_t box[3] = {32, 32, 1}, each[3] = {1, 1, 1};
+        p.out_mapped = encode_tiled()(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, p.out, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
+    constexpr int smem = 1024 + S::STAGES * S::STAGE + 8 * S::OUT + sizeof(Shared<EPI, CG>);
     auto kernel = product_kernel<T, FORM, EPI, CG>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HAP_E_CUDA;
+    static std::atomic<uint64_t> allowed;                   // devices on which the kernel may have this much shared memory
+    const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HAP_E_CUDA;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t c{};
-    const int64_t at_once = sms / CG;
-    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(192), c.dynamicSmemBytes = smem, c.stream = stream;
+    const int64_t at_once = d.sms / CG;
+    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(320), c.dynamicSmemBytes = smem, c.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
     c.attrs = attr, c.numAttrs = CG > 1;
-    return cudaLaunchKernelEx(&c, kernel, p, ma, mb) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+    return cudaLaunchKernelEx(&c, kernel, p, ma, mb, mo) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
 }
 
 template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
@@ -84,11 +107,11 @@ template <typename T, int FORM, int EPI> static hap_status launch_plain(const Ar
 
 template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
 {
-    const int sms = sm_count();
-    if (!sms) return HAP_E_CUDA;
-    if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, sms, stream);
+    const Device d = device();
+    if (!d.sms) return HAP_E_CUDA;
+    if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, d.sms, stream);
     const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output
-    return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, sms, stream) : launch_tensor<T, FORM, EPI, 1>(p, sms, stream);
+    return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, d, stream) : launch_tensor<T, FORM, EPI, 1>(p, d, stream);
 }
 
 static bool dtype16(int32_t t) { return t == HAP_BF16 || t == HAP_FP16; }
@@ -112,9 +135,10 @@ extern "C" hap_status hap_expert_matmul(int32_t form, int32_t dtype, int32_t out
     p.mdim = N, p.ncols = form == HAP_EXPERT_FORWARD ? N : K, p.kdim = form == HAP_EXPERT_FORWARD ? K : N;
     p.a = a, p.b = b, p.lda = lda, p.ldb = ldb, p.bgroup = (int64_t)N * ldb;
     p.out = out, p.ldo = ldo, p.ogroup = grad_w ? (int64_t)N * ldo : 0;
-    p.out32 = out_dtype == HAP_FP32, p.accumulate = accumulate != 0;
+    p.accumulate = accumulate != 0;
     cudaStream_t s = (cudaStream_t)stream;
 #define HAP_BY_TYPE(FORM, EPI) (dtype == HAP_BF16 ? launch_product<__nv_bfloat16, FORM, EPI>(p, s) : launch_product<__half, FORM, EPI>(p, s))
+    if (out_dtype == HAP_FP32) return form == HAP_EXPERT_FORWARD ? HAP_BY_TYPE(NT, STORE32) : grad_w ? HAP_BY_TYPE(TN, STORE32) : HAP_BY_TYPE(NN, STORE32);
     return form == HAP_EXPERT_FORWARD ? HAP_BY_TYPE(NT, STORE) : grad_w ? HAP_BY_TYPE(TN, STORE) : HAP_BY_TYPE(NN, STORE);
 }
 
@@ -170,7 +194,7 @@ extern "C" hap_status hap_linear_cross_entropy_workspace(int64_t rows, int32_t H
 {
     if (!host_bytes || !loss_sizes(rows, H, V)) return HAP_E_INVALID;
     const uint64_t n = (uint64_t)rows, piece = (uint64_t)piece_columns(rows, V);
-    const uint64_t forward = up256(ceil_div(V, TILE_N) * n * 8) + up256(n * 4);
+    const uint64_t forward = up256(ceil_div(V, PART_N) * n * 8) + up256(n * 4);
     const uint64_t backward = up256(n * piece * 2) + ((int64_t)piece < V ? up256(n * H * 4) : 0);
     *host_bytes = forward > backward ? forward : backward;
     return HAP_OK;
@@ -193,16 +217,16 @@ extern "C" hap_status hap_linear_cross_entropy(int32_t dtype, int64_t rows, int3
     if (bad != HAP_OK) return bad;
     if (rows == 0) return HAP_OK;
     if (!loss || !lse || !aligned(loss, 4) || !aligned(lse, 4)) return HAP_E_INVALID;
-    const int tiles = (int)ceil_div(V, TILE_N);
+    const int pieces = (int)ceil_div(V, PART_N);
     Args p{};
     p.groups = 1, p.rows = (int)rows, p.ncols = (int)V, p.kdim = H;
     p.a = x, p.b = w, p.lda = ldx, p.ldb = ldw;
     p.target = target, p.ignore = ignore, p.vocab = V;
-    p.part = (float2 *)workspace, p.at_target = (float *)((char *)workspace + up256((uint64_t)tiles * rows * 8));
+    p.part = (float2 *)workspace, p.at_target = (float *)((char *)workspace + up256((uint64_t)pieces * rows * 8));
     cudaStream_t s = (cudaStream_t)stream;
     const hap_status st = HAP_BY_TYPE(NT, LSE);
     if (st != HAP_OK) return st;
-    loss_rows_kernel<<<(unsigned)ceil_div(rows, 32), 256, 0, s>>>(p.part, tiles, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
+    loss_rows_kernel<<<(unsigned)ceil_div(rows, 32), 256, 0, s>>>(p.part, pieces, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
     return launched();
 }
 

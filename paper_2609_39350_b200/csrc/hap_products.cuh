@@ -19,11 +19,13 @@ enum Epilogue {
     GATED_BACK = 2, // acc is dh: dg, du and h from it and the kept g, u
     LSE = 3,        // logits: the row's maximum and sum of exponentials over the tile's columns, the target's logit
     DLOGIT = 4,     // logits again: (softmax - one-hot) * 2^15 in 16 bits
-    SUM32 = 5       // gradient of the loss's input over several pieces of the vocabulary: kept in 32 bits between them
+    SUM32 = 5,      // gradient of the loss's input over several pieces of the vocabulary: kept in 32 bits between them
+    STORE32 = 6     // STORE to fp32
 };
 
 constexpr int MAX_GROUPS = 1024;
-constexpr int TILE_N = 256;         // columns of a tile in every variant (the loss's partial results are per tile)
+constexpr int TILE_N = 256;         // columns of a tile
+constexpr int PART_N = 128;         // columns that one partial result of the loss's statistics covers, in every variant
 constexpr int BAND = 16;            // row tiles of a group that are worked on side by side, for reuse in L2
 // softmax gradients are held in 16 bits times this: fp16's normal range ends at 6e-5, a probability of a large vocabulary
 // is smaller; 2^15 keeps 1 below 65504 and 2e-9 normal.  The factor is a power of two and leaves with the gradient's scale.
@@ -40,7 +42,7 @@ struct Args {
     // epilogue
     void *out;
     int64_t ldo, ogroup;            // ogroup: distance of two groups' out (TN)
-    int out32, accumulate;
+    int accumulate, out_mapped;     // out_mapped: a tensor map describes out (TN, STORE32)
     const float *scale;             // device scalar, or null: 1
     float scale_by;                 // times this
     const void *gu;                 // GATED_BACK: kept g | u
@@ -51,7 +53,7 @@ struct Args {
     int64_t ignore;
     int64_t vocab;
     int col0;                       // first column's place in the vocabulary
-    float2 *part;                   // [column tiles][rows]
+    float2 *part;                   // [pieces of PART_N columns][rows]
     float *at_target;               // [rows]
     const float *lse;
     float *acc32;                   // SUM32: [rows][ncols]
@@ -116,25 +118,97 @@ template <typename T> __device__ __forceinline__ void load32(const T *p, float (
     for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
 }
 
-// What happens to the 32 columns col .. of one output row.  `row`: row of out (in TN of out_e, and then e is its group);
-// v: the sums; v2: those of u in GATED.  The softmax statistics of a row over a tile are held in m (maximum) and s.
+// How a warp's 32 rows of 32 16-bit values (row = lane) go to and come from memory: through 2 KB of shared memory, so that four
+// lanes take a row's 64 bytes and whole sectors are moved.  From the rows directly a 16-byte piece of every row went at a time,
+// half sectors: 150 us instead of 111 at 64 experts, 32768 rows, 1024 -> 2048.  Pieces of 16 bytes are swizzled over the banks.
+struct WarpRows {
+    char *staged;                   // null: each lane moves its own row
+    int lane, live;                 // rows 0 .. live-1 exist
+    __device__ __forceinline__ uint4 *piece(int row, int c) const { return (uint4 *)(staged + row * 64 + ((c ^ (row >> 1 & 3)) << 4)); }
+    template <typename T> __device__ __forceinline__ bool whole(const T *first, int64_t ld, int n) const { return staged && n >= 32 && ((uintptr_t)first & 15) == 0 && ld % 8 == 0; }
+    // first: column col of row 0
+    template <typename T> __device__ __forceinline__ void store(T *first, int64_t ld, const float (&v)[32], int n) const
+    {
+        if (!whole(first, ld, n)) {
+            if (lane < live) store32(first + lane * ld, v, n);
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            *piece(lane, i) = make_uint4(pack2(v[8 * i], v[8 * i + 1], T()), pack2(v[8 * i + 2], v[8 * i + 3], T()), pack2(v[8 * i + 4], v[8 * i + 5], T()), pack2(v[8 * i + 6], v[8 * i + 7], T()));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int r = i * 8 + (lane >> 2);
+            if (r < live) *(uint4 *)(first + r * ld + (lane & 3) * 8) = *piece(r, lane & 3);
+        }
+    }
+    // in two steps, so that the loads are on their way while something else is waited for
+    template <typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[4], int n) const
+    {
+        if (!whole(first, ld, n)) return;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int r = i * 8 + (lane >> 2);
+            w[i] = r < live ? *(const uint4 *)(first + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[4], float (&v)[32], int n) const
+    {
+        if (!whole(first, ld, n)) {
+            load32(first + (lane < live ? lane : 0) * ld, v, lane < live ? n : 0);
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; i++) *piece(i * 8 + (lane >> 2), lane & 3) = w[i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint4 x = *piece(lane, i);
+            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float2 f = unpack2(y[j], T());
+                v[8 * i + 2 * j] = f.x, v[8 * i + 2 * j + 1] = f.y;
+            }
+        }
+    }
+};
+
+// What happens to the 32 columns col .. of 32 output rows, one for each lane of a warp, from `row0` on (in TN rows of out_e, and
+// then e is its group).  v: the sums; v2: those of u in GATED.  The softmax statistics of a row over a tile are held in m
+// (maximum) and s.  All lanes call, those of rows that do not exist too.
 template <typename T, int EPI> struct RowEpilogue {
     const Args &p;
-    const int64_t row;
+    const WarpRows w;
+    const int64_t row0;
     const int e;
+    const bool live;
     float m = -INFINITY, s = 0.0f;
     int64_t target = -1;            // LSE, DLOGIT: column of the row's target in this launch's columns, or outside of them
     bool kept = true;
     float lse = 0.0f;
-    __device__ RowEpilogue(const Args &args, int64_t row, int e, bool live) : p(args), row(row), e(e)
+    uint4 g4[EPI == GATED_BACK ? 4 : 1], u4[EPI == GATED_BACK ? 4 : 1];
+    __device__ __forceinline__ RowEpilogue(const Args &args, const WarpRows &w, int64_t row0, int e) : p(args), w(w), row0(row0), e(e), live(w.lane < w.live)
     {
         if constexpr (EPI == LSE || EPI == DLOGIT) {
             if (live) {
-                const int64_t t = p.target[row];
+                const int64_t t = p.target[row0 + w.lane];
                 kept = t != p.ignore && t >= 0 && t < p.vocab;
                 target = t - p.col0;
-                if constexpr (EPI == DLOGIT) lse = p.lse[row];
+                if constexpr (EPI == DLOGIT) lse = p.lse[row0 + w.lane];
             }
+        }
+    }
+    // what the columns need from memory, ahead of them
+    __device__ __forceinline__ void ahead(int col)
+    {
+        if constexpr (EPI == GATED_BACK) {
+            const T *gu = (const T *)p.gu + row0 * p.ldgu + col;
+            w.fetch(gu, p.ldgu, g4, p.ncols - col);
+            w.fetch(gu + p.ncols, p.ldgu, u4, p.ncols - col);
         }
     }
     __device__ __forceinline__ void columns(int col, float (&v)[32], float (&v2)[32])
@@ -142,42 +216,50 @@ template <typename T, int EPI> struct RowEpilogue {
         const int n = p.ncols - col;
         if (n <= 0) return;
         if constexpr (EPI == STORE) {
-            const float f = p.scale ? *p.scale * p.scale_by : 1.0f;
             if (p.scale) {
+                const float f = *p.scale * p.scale_by;
 #pragma unroll
                 for (int i = 0; i < 32; i++) v[i] *= f;
             }
-            if (p.out32) {
-                float *o = (float *)p.out + e * p.ogroup + row * p.ldo + col;
-                if (p.accumulate) {
-                    load32(o, v2, n);
+            T *o = (T *)p.out + e * p.ogroup + row0 * p.ldo + col;
+            if (p.accumulate) {
+                load32(o + w.lane * p.ldo, v2, live ? n : 0);
 #pragma unroll
-                    for (int i = 0; i < 32; i++) v[i] += v2[i];
+                for (int i = 0; i < 32; i++) v[i] += v2[i];
+            }
+            w.store(o, p.ldo, v, n);
+        }
+        if constexpr (EPI == STORE32) {         // four at a time: a whole tile's half row is in registers here
+            float *o = (float *)p.out + e * p.ogroup + (row0 + w.lane) * p.ldo + col;
+            if (!live) return;
+            if (n >= 32 && ((uintptr_t)o & 15) == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    float4 x = p.accumulate ? *(const float4 *)(o + i) : make_float4(0, 0, 0, 0);
+                    x.x += v[i], x.y += v[i + 1], x.z += v[i + 2], x.w += v[i + 3];
+                    *(float4 *)(o + i) = x;
                 }
-                store32(o, v, n);
             } else {
-                T *o = (T *)p.out + e * p.ogroup + row * p.ldo + col;
-                if (p.accumulate) {
-                    load32(o, v2, n);
 #pragma unroll
-                    for (int i = 0; i < 32; i++) v[i] += v2[i];
-                }
-                store32(o, v, n);
+                for (int i = 0; i < 32; i++)
+                    if (i < n) o[i] = p.accumulate ? o[i] + v[i] : v[i];
             }
         }
         if constexpr (EPI == GATED) {
             if (p.out) {
-                store32((T *)p.out + row * p.ldo + col, v, n);
-                store32((T *)p.out + row * p.ldo + p.ncols + col, v2, n);
+                T *o = (T *)p.out + row0 * p.ldo + col;
+                w.store(o, p.ldo, v, n);
+                w.store(o + p.ncols, p.ldo, v2, n);
             }
 #pragma unroll
             for (int i = 0; i < 32; i++) v[i] = v[i] / (1.0f + __expf(-v[i])) * v2[i];
-            store32((T *)p.h + row * p.ldh + col, v, n);
+            w.store((T *)p.h + row0 * p.ldh + col, p.ldh, v, n);
         }
         if constexpr (EPI == GATED_BACK) {
             float g[32];
-            load32((const T *)p.gu + row * p.ldgu + col, g, n);
-            load32((const T *)p.gu + row * p.ldgu + p.ncols + col, v2, n);
+            const T *gu = (const T *)p.gu + row0 * p.ldgu + col;
+            w.take(gu, p.ldgu, g4, g, n);
+            w.take(gu + p.ncols, p.ldgu, u4, v2, n);
 #pragma unroll
             for (int i = 0; i < 32; i++) {      // s = sigma(g): dg = dh u (s + g s (1 - s)), du = dh g s, h = g s u
                 const float s = 1.0f / (1.0f + __expf(-g[i]));
@@ -186,9 +268,10 @@ template <typename T, int EPI> struct RowEpilogue {
                 v2[i] = dh * gs;
                 g[i] = gs * u;
             }
-            store32((T *)p.out + row * p.ldo + col, v, n);
-            store32((T *)p.out + row * p.ldo + p.ncols + col, v2, n);
-            if (p.h) store32((T *)p.h + row * p.ldh + col, g, n);
+            T *o = (T *)p.out + row0 * p.ldo + col;
+            w.store(o, p.ldo, v, n);
+            w.store(o + p.ncols, p.ldo, v2, n);
+            if (p.h) w.store((T *)p.h + row0 * p.ldh + col, p.ldh, g, n);
         }
         if constexpr (EPI == LSE) {
             float top = m;
@@ -202,11 +285,11 @@ template <typename T, int EPI> struct RowEpilogue {
 #pragma unroll
             for (int i = 0; i < 32; i++) sum += exp2f(fmaf(v[i], 1.4426950408889634f, -from));
             m = top, s = sum;
-            if (target >= col && target < col + 32 && target < p.ncols) {
+            if (live && target >= col && target < col + 32 && target < p.ncols) {
                 float z = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 32; i++) z = col + i == target ? v[i] : z;
-                p.at_target[row] = z;
+                p.at_target[row0 + w.lane] = z;
             }
         }
         if constexpr (EPI == DLOGIT) {
@@ -217,12 +300,12 @@ template <typename T, int EPI> struct RowEpilogue {
                 d = col + i == target ? d - 1.0f : d;
                 v[i] = kept ? d * DLOGIT_SCALE : 0.0f;
             }
-            store32((T *)p.out + row * p.ldo + col, v, n);
+            w.store((T *)p.out + row0 * p.ldo + col, p.ldo, v, n);
         }
         if constexpr (EPI == SUM32) {
-            float *a = p.acc32 + row * (int64_t)p.ncols + col;
+            float *a = p.acc32 + (row0 + w.lane) * (int64_t)p.ncols + col;
             if (!p.first) {
-                load32(a, v2, n);
+                load32(a, v2, live ? n : 0);
 #pragma unroll
                 for (int i = 0; i < 32; i++) v[i] += v2[i];
             }
@@ -230,15 +313,16 @@ template <typename T, int EPI> struct RowEpilogue {
                 const float f = *p.scale * p.scale_by;
 #pragma unroll
                 for (int i = 0; i < 32; i++) v[i] *= f;
-                store32((T *)p.out + row * p.ldo + col, v, n);
-            } else {
+                w.store((T *)p.out + row0 * p.ldo + col, p.ldo, v, n);
+            } else if (live) {
                 store32(a, v, n);
             }
         }
     }
-    __device__ __forceinline__ void end(int tile_n)
+    __device__ __forceinline__ void end(int col)        // behind PART_N columns from col on
     {
-        if constexpr (EPI == LSE) p.part[(int64_t)tile_n * p.rows + row] = make_float2(m, s);
+        if constexpr (EPI == LSE)
+            if (live && col < p.ncols) p.part[(int64_t)(col / PART_N) * p.rows + row0 + w.lane] = make_float2(m, s);
     }
 };
 
@@ -376,32 +460,33 @@ template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) 
 #pragma unroll
             for (int j = 0; j < 8; j++) sc[tm + i][tn + 32 * j] = acc[i][j];
         __syncthreads();
-        // a row's columns stay with one thread where its statistics run over them; else 8 threads share the row
+        // 8 threads share a row; two where its statistics run over the columns
+        constexpr int SHARE = EPI == LSE ? TILE_N / PART_N : 8, EACH = BN / 32 / SHARE > 0 ? BN / 32 / SHARE : 1;
         const int r = tid & 31, c = tid >> 5;
-        if (r < mrows && (EPI != LSE || c == 0)) {
-            RowEpilogue<T, EPI> row(p, (FORM == TN ? 0 : (int64_t)tile.lo) + m0 + r, FORM == TN ? tile.e : 0, true);
+        if (c * EACH < BN / 32 && c < SHARE) {
+            RowEpilogue<T, EPI> row(p, WarpRows{nullptr, r, min(max(mrows, 0), 32)}, (FORM == TN ? 0 : (int64_t)tile.lo) + m0, FORM == TN ? tile.e : 0);
             float v[32], v2[32];
-            for (int q = EPI == LSE ? 0 : c; q < BN / 32; q += 8 - 7 * (EPI == LSE)) {
+            for (int q = c * EACH; q < (c + 1) * EACH; q++) {
 #pragma unroll
                 for (int i = 0; i < 32; i++) v[i] = sc[r][q * 32 + i], v2[i] = EPI == GATED ? sc[r][BN + q * 32 + i] : 0.0f;
                 row.columns(n0 + q * 32, v, v2);
             }
-            row.end(tile.n);
+            row.end(n0 + c * PART_N);
         }
         __syncthreads();
     }
 }
 
-// ---- the loss from the tiles' statistics ------------------------------------------------------------------------------
-// lse = M + log(sum_t s_t exp(m_t - M)).  A block takes 32 rows, its warps every eighth tile; rows of one tile lie side by side.
-__global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int tiles, int rows, const float *at_target, const int64_t *target,
+// ---- the loss from the pieces' statistics ------------------------------------------------------------------------------
+// lse = M + log(sum_t s_t exp(m_t - M)).  A block takes 32 rows, its warps every eighth piece; a piece's rows lie side by side.
+__global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int pieces, int rows, const float *at_target, const int64_t *target,
                                                         int64_t ignore, int V, float *loss, float *lse)
 {
     __shared__ float2 sh[8][32];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
     float m = -INFINITY, s = 0.0f;
     if (row < rows)
-        for (int t = w; t < tiles; t += 8) {
+        for (int t = w; t < pieces; t += 8) {
             const float2 x = part[(int64_t)t * rows + row];
             const float top = fmaxf(m, x.x);
             const float from = top == -INFINITY ? 0.0f : top;
