@@ -11,7 +11,8 @@ SOURCES = [os.path.join(_DIR, "csrc", "hap_api.cu"), os.path.join(_DIR, "csrc", 
 HEADERS = [os.path.join(_DIR, "csrc", "hap_device.cuh"), os.path.join(_DIR, "csrc", "hap_tree.cuh"),
            os.path.join(_DIR, "csrc", "hap_tree_host.h"), os.path.join(_DIR, "csrc", "hap_joint.cuh"),
            os.path.join(os.path.dirname(_DIR), "include", "hap.h")]
-OPERATOR_HEADERS = [os.path.join(_DIR, "csrc", "hap_products.cuh"), os.path.join(_DIR, "csrc", "hap_products_tc.cuh"), os.path.join(_DIR, "csrc", "hap_adamw.cuh"),
+OPERATOR_HEADERS = [os.path.join(_DIR, "csrc", "hap_products.cuh"), os.path.join(_DIR, "csrc", "hap_products_tc.cuh"),
+                    os.path.join(_DIR, "csrc", "hap_products_experts.cuh"), os.path.join(_DIR, "csrc", "hap_adamw.cuh"),
                     os.path.join(os.path.dirname(_DIR), "include", "hap.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "--fmad=false", "-std=c++17",

@@ -1,5 +1,6 @@
 // Host side of the training operators: checks of arguments, choice of variant, launches.
 #include "hap_adamw.cuh"
+#include "hap_products_experts.cuh"
 #include "hap_products_tc.cuh"
 
 #include <atomic>
@@ -59,15 +60,33 @@ static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols
 // whether TMA can address an operand
 static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
 
+// a persistent kernel of blocks or pairs of blocks, as many as fit and `most` tiles need
+template <auto KERNEL, int CG = 2, typename... A> static hap_status launch_pairs(int smem, int64_t most, Device d, cudaStream_t stream, const A &...args)
+{
+    static std::atomic<uint64_t> allowed;                   // devices on which the kernel may have this much shared memory
+    const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t c{};
+    const int64_t at_once = d.sms / CG;
+    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(320), c.dynamicSmemBytes = smem, c.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
+    c.attrs = attr, c.numAttrs = CG > 1;
+    return cudaLaunchKernelEx(&c, KERNEL, args...) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+}
+
 template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(Args p, Device d, cudaStream_t stream)
 {
     using S = Shape<EPI, CG>;
-    const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
+    const int64_t cols = ceil_div(p.ncols, TILE_N);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, S::BM) : ceil_div(p.rows, S::BM) + (p.offsets ? p.groups : 0));
     if (most > INT32_MAX) return HAP_E_RANGE;
     constexpr bool fp16 = TypeBits<T>::value == 0;
     CUtensorMap ma, mb, mo{};
-    const int64_t wrows = FORM == NT ? (EPI == GATED ? 2ll * p.ncols : p.ncols) : p.kdim;
+    const int64_t wrows = FORM == NT ? p.ncols : p.kdim;
     const bool good = FORM == TN ? make_map(&ma, fp16, p.a, p.mdim, p.rows, 1, p.lda, 0, BK) && make_map(&mb, fp16, p.b, p.ncols, p.rows, 1, p.ldb, 0, BK)
                                  : make_map(&ma, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 128) &&
                                        make_map(&mb, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK);
@@ -80,20 +99,22 @@ template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor
                                       CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
     constexpr int smem = 1024 + S::STAGES * S::STAGE + 8 * S::OUT + sizeof(Shared<EPI, CG>);
-    auto kernel = product_kernel<T, FORM, EPI, CG>;
-    static std::atomic<uint64_t> allowed;                   // devices on which the kernel may have this much shared memory
-    const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
-    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return HAP_E_CUDA;
-        allowed.fetch_or(bit, std::memory_order_relaxed);
-    }
-    cudaLaunchConfig_t c{};
-    const int64_t at_once = d.sms / CG;
-    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(320), c.dynamicSmemBytes = smem, c.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
-    c.attrs = attr, c.numAttrs = CG > 1;
-    return cudaLaunchKernelEx(&c, kernel, p, ma, mb, mo) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+    return launch_pairs<product_kernel<T, FORM, EPI, CG>, CG>(smem, most, d, stream, p, ma, mb, mo);
+}
+
+// experts' rows as columns of the products (NT, NN; out in 16 bits)
+template <typename T, int FORM, int EPI> static hap_status launch_experts(const Args &p, Device d, cudaStream_t stream)
+{
+    using S = Turned<EPI>;
+    const int64_t most = ceil_div(p.ncols, 256) * (ceil_div(p.rows, S::ROWS) + p.groups);
+    if (most > INT32_MAX) return HAP_E_RANGE;
+    constexpr bool fp16 = TypeBits<T>::value == 0;
+    CUtensorMap mw, mr, mf;
+    const int64_t wrows = FORM == NT ? (EPI == GATED ? 2ll * p.ncols : p.ncols) : p.kdim;
+    if (!make_map(&mw, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK) ||
+        !make_map(&mr, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, S::ROWS / 2) || !make_map(&mf, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 16))
+        return HAP_E_CUDA;
+    return launch_pairs<expert_kernel<T, FORM, EPI>>(1024 + S::STAGES * S::STAGE + 8 * 2048 + sizeof(TurnedShared<EPI>), most, d, stream, p, mw, mr, mf);
 }
 
 template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
@@ -110,8 +131,12 @@ template <typename T, int FORM, int EPI> static hap_status launch_product(const 
     const Device d = device();
     if (!d.sms) return HAP_E_CUDA;
     if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, d.sms, stream);
-    const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output
-    return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, d, stream) : launch_tensor<T, FORM, EPI, 1>(p, d, stream);
+    if constexpr (FORM != TN && (EPI == STORE || EPI == GATED || EPI == GATED_BACK)) {
+        return launch_experts<T, FORM, EPI>(p, d, stream);
+    } else {
+        const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output
+        return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, d, stream) : launch_tensor<T, FORM, EPI, 1>(p, d, stream);
+    }
 }
 
 static bool dtype16(int32_t t) { return t == HAP_BF16 || t == HAP_FP16; }

@@ -118,6 +118,17 @@ template <typename T> __device__ __forceinline__ void load32(const T *p, float (
     for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
 }
 
+// h = silu(g) u
+__device__ __forceinline__ float gate(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+// from g, u and dh: g becomes h, u becomes du, dh becomes dg.  With s = sigma(g): dg = dh u (s + g s (1 - s)), du = dh g s, h = g s u
+__device__ __forceinline__ void gate_back(float &g, float &u, float &dh)
+{
+    const float s = 1.0f / (1.0f + __expf(-g)), gs = g * s, du = dh * gs;
+    dh = dh * u * fmaf(gs, 1.0f - s, s);
+    g = gs * u;
+    u = du;
+}
+
 // How a warp's 32 rows of 32 16-bit values (row = lane) go to and come from memory: through 2 KB of shared memory, so that four
 // lanes take a row's 64 bytes and whole sectors are moved.  From the rows directly a 16-byte piece of every row went at a time,
 // half sectors: 150 us instead of 111 at 64 experts, 32768 rows, 1024 -> 2048.  Pieces of 16 bytes are swizzled over the banks.
@@ -144,37 +155,6 @@ struct WarpRows {
             if (r < live) *(uint4 *)(first + r * ld + (lane & 3) * 8) = *piece(r, lane & 3);
         }
     }
-    // in two steps, so that the loads are on their way while something else is waited for
-    template <typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[4], int n) const
-    {
-        if (!whole(first, ld, n)) return;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int r = i * 8 + (lane >> 2);
-            w[i] = r < live ? *(const uint4 *)(first + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
-        }
-    }
-    template <typename T> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[4], float (&v)[32], int n) const
-    {
-        if (!whole(first, ld, n)) {
-            load32(first + (lane < live ? lane : 0) * ld, v, lane < live ? n : 0);
-            return;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; i++) *piece(i * 8 + (lane >> 2), lane & 3) = w[i];
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint4 x = *piece(lane, i);
-            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 f = unpack2(y[j], T());
-                v[8 * i + 2 * j] = f.x, v[8 * i + 2 * j + 1] = f.y;
-            }
-        }
-    }
 };
 
 // What happens to the 32 columns col .. of 32 output rows, one for each lane of a warp, from `row0` on (in TN rows of out_e, and
@@ -190,7 +170,6 @@ template <typename T, int EPI> struct RowEpilogue {
     int64_t target = -1;            // LSE, DLOGIT: column of the row's target in this launch's columns, or outside of them
     bool kept = true;
     float lse = 0.0f;
-    uint4 g4[EPI == GATED_BACK ? 4 : 1], u4[EPI == GATED_BACK ? 4 : 1];
     __device__ __forceinline__ RowEpilogue(const Args &args, const WarpRows &w, int64_t row0, int e) : p(args), w(w), row0(row0), e(e), live(w.lane < w.live)
     {
         if constexpr (EPI == LSE || EPI == DLOGIT) {
@@ -200,15 +179,6 @@ template <typename T, int EPI> struct RowEpilogue {
                 target = t - p.col0;
                 if constexpr (EPI == DLOGIT) lse = p.lse[row0 + w.lane];
             }
-        }
-    }
-    // what the columns need from memory, ahead of them
-    __device__ __forceinline__ void ahead(int col)
-    {
-        if constexpr (EPI == GATED_BACK) {
-            const T *gu = (const T *)p.gu + row0 * p.ldgu + col;
-            w.fetch(gu, p.ldgu, g4, p.ncols - col);
-            w.fetch(gu + p.ncols, p.ldgu, u4, p.ncols - col);
         }
     }
     __device__ __forceinline__ void columns(int col, float (&v)[32], float (&v2)[32])
@@ -252,22 +222,16 @@ template <typename T, int EPI> struct RowEpilogue {
                 w.store(o + p.ncols, p.ldo, v2, n);
             }
 #pragma unroll
-            for (int i = 0; i < 32; i++) v[i] = v[i] / (1.0f + __expf(-v[i])) * v2[i];
+            for (int i = 0; i < 32; i++) v[i] = gate(v[i], v2[i]);
             w.store((T *)p.h + row0 * p.ldh + col, p.ldh, v, n);
         }
         if constexpr (EPI == GATED_BACK) {
             float g[32];
-            const T *gu = (const T *)p.gu + row0 * p.ldgu + col;
-            w.take(gu, p.ldgu, g4, g, n);
-            w.take(gu + p.ncols, p.ldgu, u4, v2, n);
+            const T *gu = (const T *)p.gu + (row0 + w.lane) * p.ldgu + col;
+            load32(gu, g, live ? n : 0);
+            load32(gu + p.ncols, v2, live ? n : 0);
 #pragma unroll
-            for (int i = 0; i < 32; i++) {      // s = sigma(g): dg = dh u (s + g s (1 - s)), du = dh g s, h = g s u
-                const float s = 1.0f / (1.0f + __expf(-g[i]));
-                const float gs = g[i] * s, dh = v[i], u = v2[i];
-                v[i] = dh * u * fmaf(gs, 1.0f - s, s);
-                v2[i] = dh * gs;
-                g[i] = gs * u;
-            }
+            for (int i = 0; i < 32; i++) gate_back(g[i], v2[i], v[i]);
             T *o = (T *)p.out + row0 * p.ldo + col;
             w.store(o, p.ldo, v, n);
             w.store(o + p.ncols, p.ldo, v2, n);

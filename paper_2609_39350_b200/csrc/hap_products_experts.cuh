@@ -1,0 +1,272 @@
+// Products of the experts' rows on the tensor cores, turned around: the weight's columns are the 256 rows of a product (128 for
+// each block of a pair) and the expert's rows its columns, 32 to 256 of them in steps of 32.  So an expert with 40 rows costs 64
+// columns, not 128 or 256 rows, and experts have few rows each: of 32 experts with 8190 rows by Zipf's law, tiles of 256 rows
+// would be 63 % filled, of 128 rows 82 %, these are 94 %.  Sums come out of tensor memory with a weight's column in each lane;
+// they are turned back in shared memory.
+//   NT  out[i][n] = sum_k a[i][k] w_e[n][k]          NN  out[i][k] = sum_n a[i][n] w_e[n][k]
+// GATED makes two products of 256 x 128 in a tile, g and u of the same columns in the same lanes.
+// The rest is as in hap_products_tc.cuh, whose pieces this uses.
+#pragma once
+#include "hap_products_tc.cuh"
+
+namespace hapop {
+
+template <int EPI> struct Turned {
+    static constexpr int ROWS = EPI == GATED ? 128 : 256;           // most rows of a tile
+    static constexpr int A_BYTES = (EPI == GATED ? 2 : 1) * 128 * BK * 2, B_BYTES = ROWS / 2 * BK * 2, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = EPI == GATED ? 5 : 6;
+};
+
+template <int EPI> struct TurnedShared {
+    Schedule<Turned<EPI>::ROWS> sched;
+    uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int stop;
+};
+
+// A warp's 32 columns (one for each lane) of 32 rows of 16-bit values, to and from memory through 2 KB of shared memory: words of
+// two rows of a column, 16 rows of 32 words.  Four lanes take two rows' 64 bytes; of pairs side by side one reads the words the
+// other way around, so that the banks differ.
+struct WarpColumns {
+    uint32_t *staged;
+    int lane;
+    template <typename T> __device__ __forceinline__ bool whole(const T *first, int64_t ld, int cols) const { return cols >= 32 && ((uintptr_t)first & 15) == 0 && ld % 8 == 0; }
+    __device__ __forceinline__ uint4 *words(int pair, int c, int h) const { return (uint4 *)(staged + pair * 32 + c * 8 + h * 4); }
+    // first: row 0 of the first lane's column; rows, cols: how many there are
+    template <typename T> __device__ __forceinline__ void store(T *first, int64_t ld, const float (&v)[32], int rows, int cols) const
+    {
+        if (!whole(first, ld, cols)) {
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (i < rows && lane < cols) first[i * ld + lane] = from_float<T>(v[i]);
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; i++) staged[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int pair = i * 8 + (lane >> 2), c = lane & 3, odd = pair & 1;
+            const uint4 x = *words(pair, c, odd), y = *words(pair, c, odd ^ 1);
+            const uint4 lo = odd ? y : x, hi = odd ? x : y;
+            T *o = first + 2 * pair * ld + c * 8;
+            if (2 * pair < rows) *(uint4 *)o = make_uint4(__byte_perm(lo.x, lo.y, 0x5410), __byte_perm(lo.z, lo.w, 0x5410), __byte_perm(hi.x, hi.y, 0x5410), __byte_perm(hi.z, hi.w, 0x5410));
+            if (2 * pair + 1 < rows)
+                *(uint4 *)(o + ld) = make_uint4(__byte_perm(lo.x, lo.y, 0x7632), __byte_perm(lo.z, lo.w, 0x7632), __byte_perm(hi.x, hi.y, 0x7632), __byte_perm(hi.z, hi.w, 0x7632));
+        }
+    }
+    // in two steps, so that the loads are on their way while something else is waited for
+    template <typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[4], int rows, int cols) const
+    {
+        if (!whole(first, ld, cols)) return;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int r = 2 * (i / 2 * 8 + (lane >> 2)) + i % 2;
+            w[i] = r < rows ? *(const uint4 *)(first + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    template <typename T> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[4], float (&v)[32], int rows, int cols) const
+    {
+        if (!whole(first, ld, cols)) {
+#pragma unroll
+            for (int i = 0; i < 32; i++) v[i] = i < rows && lane < cols ? to_float(first[i * ld + lane]) : 0.0f;
+            return;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int pair = i * 8 + (lane >> 2), c = lane & 3, odd = pair & 1;
+            const uint4 a = w[2 * i], b = w[2 * i + 1];
+            const uint4 lo = make_uint4(__byte_perm(a.x, b.x, 0x5410), __byte_perm(a.x, b.x, 0x7632), __byte_perm(a.y, b.y, 0x5410), __byte_perm(a.y, b.y, 0x7632));
+            const uint4 hi = make_uint4(__byte_perm(a.z, b.z, 0x5410), __byte_perm(a.z, b.z, 0x7632), __byte_perm(a.w, b.w, 0x5410), __byte_perm(a.w, b.w, 0x7632));
+            *words(pair, c, odd) = odd ? hi : lo;
+            *words(pair, c, odd ^ 1) = odd ? lo : hi;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            const float2 f = unpack2(staged[i * 32 + lane], T());
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+    }
+};
+
+template <typename T, int FORM, int EPI>
+__global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ Args p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_rows,
+                                                        const __grid_constant__ CUtensorMap map_few)
+{
+    using S = Turned<EPI>;
+    extern __shared__ char raw[];
+    char *stages = (char *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    char *outs = stages + S::STAGES * S::STAGE;
+    TurnedShared<EPI> &sh = *(TurnedShared<EPI> *)(outs + 8 * 2048);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    constexpr int BN = 256;                                 // columns of out that a tile covers
+    const int col_tiles = (p.ncols + BN - 1) / BN;
+
+    if (warp == 0) sh.sched.build(p, FORM, col_tiles, lane);
+    if (warp == 1) {
+        if (lane == 0) {
+            for (int i = 0; i < S::STAGES; i++) bar_init(&sh.full[i], 2), bar_init(&sh.empty[i], 1);
+            for (int i = 0; i < 2; i++) bar_init(&sh.acc_full[i], 1), bar_init(&sh.acc_empty[i], 16);
+            sh.stop = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async;" ::: "memory");
+        }
+        __syncwarp();
+        tmem_alloc<2>(&sh.tmem);
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    const uint32_t tmem = *(volatile uint32_t *)&sh.tmem;
+    volatile int *stop = &sh.stop;
+    const int total = sh.sched.total(p, FORM, col_tiles);
+    const int step = gridDim.x / 2, begin = blockIdx.x / 2;
+    // rows of a tile, as the products count them
+    auto rows_of = [](const auto &tile) { return min(S::ROWS, (tile.hi - tile.lo - tile.m * S::ROWS + 31) & ~31); };
+
+    if (warp == 0) {
+        uint32_t at = 0;
+        bool good = true;
+        for (int t = begin; t < total && good; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+            const int n0 = tile.n * BN + (int)rank * 128, half = rows_of(tile) / 2, row = tile.lo + tile.m * S::ROWS + (int)rank * half;
+            for (int k = 0; k < p.kdim; k += BK, at++) {
+                const int s = at % S::STAGES;
+                if (!(good = bar_wait(&sh.empty[s], (at / S::STAGES + 1) & 1, stop))) break;
+                const uint32_t a = smem_u32(stages + s * S::STAGE), b = a + S::A_BYTES, full = of_leader(smem_u32(&sh.full[s]));
+                if (elected()) {
+                    bar_expect_at<2>(full, S::A_BYTES + half * 128);
+                    if (FORM == NT) {
+                        tma_load<2>(&map_w, a, full, k, n0, tile.e);
+                        if (EPI == GATED) tma_load<2>(&map_w, a + 128 * 128, full, k, p.ncols + n0, tile.e);
+                    } else {
+                        tma_load<2>(&map_w, a, full, n0, k, tile.e);
+                        tma_load<2>(&map_w, a + BK * 128, full, n0 + 64, k, tile.e);
+                    }
+                    if (half == S::ROWS / 2) tma_load<2>(&map_rows, b, full, k, row, 0);
+                    else
+                        for (int i = 0; i < half; i += 16) tma_load<2>(&map_few, b + i * 128, full, k, row + i, 0);
+                }
+                __syncwarp();
+            }
+        }
+        if (*stop && rank == 0) drain(sh.full, at, S::STAGES);
+    } else if (warp == 1) {
+        if (rank == 0) {
+            constexpr uint32_t idesc = 1u << 4 | TypeBits<T>::value << 7 | TypeBits<T>::value << 10 | (FORM == NN ? 1u << 15 : 0) | (256u / 16) << 24;
+            uint32_t at = 0, sums = 0;
+            bool good = true;
+            for (int t = begin; t < total && good; t += step) {
+                const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+                const uint32_t of = idesc | (uint32_t)(rows_of(tile) / 8) << 17;
+                const int set = sums & 1;
+                if (!(good = bar_wait(&sh.acc_empty[set], (sums / 2 + 1) & 1, stop))) break;
+                sums++;
+                fence_after();
+                for (int k = 0; k < p.kdim; k += BK, at++) {
+                    const int s = at % S::STAGES;
+                    if (!(good = bar_wait(&sh.full[s], (at / S::STAGES) & 1, stop))) break;
+                    fence_after();
+                    if (elected()) {
+                        const uint32_t a = smem_u32(stages + s * S::STAGE), b = a + S::A_BYTES;
+                        const uint64_t da = FORM == NN ? smem_desc(a, BK * 128, 1024) : smem_desc(a, 16, 1024), db = smem_desc(b, 16, 1024);
+#pragma unroll
+                        for (int i = 0; i < BK / 16; i++) {
+                            mma<2>(tmem + set * 256, da + i * (FORM == NN ? 128 : 2), db + i * 2, of, k > 0 || i > 0);
+                            if (EPI == GATED) mma<2>(tmem + set * 256 + 128, da + 1024 + i * 2, db + i * 2, of, k > 0 || i > 0);
+                        }
+                        mma_commit<2>(&sh.empty[s]);
+                        if (k + BK >= p.kdim) mma_commit<2>(&sh.acc_full[set]);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+    } else {
+        uint32_t sums = 0;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const WarpColumns w{(uint32_t *)(outs + (warp - 2) * 2048), lane};
+        const uint32_t from = tmem + ((uint32_t)quarter << 21);
+        for (int t = begin; t < total; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+            const int set = sums & 1, col = tile.n * BN + (int)rank * 128 + quarter * 32, cols = p.ncols - col;
+            const int chunks = rows_of(tile) / 32, live = tile.hi - tile.lo - tile.m * S::ROWS;
+            const int64_t row0 = (int64_t)tile.lo + tile.m * S::ROWS;
+            uint4 g4[EPI == GATED_BACK ? 4 : 1], u4[EPI == GATED_BACK ? 4 : 1];
+            auto ahead = [&](int q) {
+                if constexpr (EPI == GATED_BACK) {
+                    const T *gu = (const T *)p.gu + (row0 + q * 32) * p.ldgu + col;
+                    w.fetch(gu, p.ldgu, g4, live - q * 32, cols);
+                    w.fetch(gu + p.ncols, p.ldgu, u4, live - q * 32, cols);
+                }
+            };
+            if (cols > 0 && half < chunks) ahead(half);
+            if (!bar_wait(&sh.acc_full[set], (sums / 2) & 1, stop)) break;
+            sums++;
+            fence_after();
+            auto taken = [&] {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_at<2>(of_leader(smem_u32(&sh.acc_empty[set])));
+            };
+            if (cols <= 0 || half >= chunks) {
+                taken();
+                continue;
+            }
+            for (int q = half; q < chunks; q += 2) {
+                const int n = live - q * 32;                // rows of this piece
+                const int64_t row = row0 + q * 32;
+                float v[32], v2[32];
+                __syncwarp();
+                tmem_load32(from + set * 256 + q * 32, v);
+                if (EPI == GATED) tmem_load32(from + set * 256 + 128 + q * 32, v2);
+                tmem_load_wait();
+                if (q + 2 >= chunks) taken();
+                if constexpr (EPI == STORE) {
+                    T *o = (T *)p.out + row * p.ldo + col;
+                    if (p.accumulate) {
+#pragma unroll
+                        for (int i = 0; i < 32; i++)
+                            if (i < n && lane < cols) v[i] += to_float(o[i * p.ldo + lane]);
+                    }
+                    w.store(o, p.ldo, v, n, cols);
+                }
+                if constexpr (EPI == GATED) {
+                    if (p.out) {
+                        T *o = (T *)p.out + row * p.ldo + col;
+                        w.store(o, p.ldo, v, n, cols);
+                        w.store(o + p.ncols, p.ldo, v2, n, cols);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i++) v[i] = gate(v[i], v2[i]);
+                    w.store((T *)p.h + row * p.ldh + col, p.ldh, v, n, cols);
+                }
+                if constexpr (EPI == GATED_BACK) {
+                    float g[32];
+                    const T *gu = (const T *)p.gu + row * p.ldgu + col;
+                    w.take(gu, p.ldgu, g4, g, n, cols);
+                    w.take(gu + p.ncols, p.ldgu, u4, v2, n, cols);
+                    if (q + 2 < chunks) ahead(q + 2);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) gate_back(g[i], v2[i], v[i]);
+                    T *o = (T *)p.out + row * p.ldo + col;
+                    w.store(o, p.ldo, v, n, cols);
+                    w.store(o + p.ncols, p.ldo, v2, n, cols);
+                    if (p.h) w.store((T *)p.h + row * p.ldh + col, p.ldh, g, n, cols);
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    if (warp == 1) tmem_free<2>(tmem);
+}
+
+} // namespace hapop
