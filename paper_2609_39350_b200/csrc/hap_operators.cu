@@ -114,7 +114,7 @@ template <typename T, int FORM, int EPI> static hap_status launch_experts(const 
     if (!make_map(&mw, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK) ||
         !make_map(&mr, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, S::ROWS / 2) || !make_map(&mf, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 16))
         return HAP_E_CUDA;
-    return launch_pairs<expert_kernel<T, FORM, EPI>>(1024 + S::STAGES * S::STAGE + 8 * 2048 + sizeof(TurnedShared<EPI>), most, d, stream, p, mw, mr, mf);
+    return launch_pairs<expert_kernel<T, FORM, EPI>>(1024 + S::STAGES * S::STAGE + 8 * S::OUT + sizeof(TurnedShared<EPI>), most, d, stream, p, mw, mr, mf);
 }
 
 template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
@@ -251,7 +251,7 @@ extern "C" hap_status hap_linear_cross_entropy(int32_t dtype, int64_t rows, int3
     cudaStream_t s = (cudaStream_t)stream;
     const hap_status st = HAP_BY_TYPE(NT, LSE);
     if (st != HAP_OK) return st;
-    loss_rows_kernel<<<(unsigned)ceil_div(rows, 32), 256, 0, s>>>(p.part, pieces, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
+    loss_rows_kernel<<<(unsigned)ceil_div(rows, 8), 256, 0, s>>>(p.part, pieces, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
     return launched();
 }
 

@@ -118,12 +118,14 @@ template <typename T> __device__ __forceinline__ void load32(const T *p, float (
     for (int i = 0; i < 32; i++) v[i] = i < n ? to_float(p[i]) : 0.0f;
 }
 
+// 1 / (1 + exp(-g)), off by a few units in the last place; at exp(88), above 2^126, the quotient is 0
+__device__ __forceinline__ float sigma(float g) { return __fdividef(1.0f, 1.0f + __expf(fminf(-g, 88.0f))); }
 // h = silu(g) u
-__device__ __forceinline__ float gate(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+__device__ __forceinline__ float gate(float g, float u) { return g * sigma(g) * u; }
 // from g, u and dh: g becomes h, u becomes du, dh becomes dg.  With s = sigma(g): dg = dh u (s + g s (1 - s)), du = dh g s, h = g s u
 __device__ __forceinline__ void gate_back(float &g, float &u, float &dh)
 {
-    const float s = 1.0f / (1.0f + __expf(-g)), gs = g * s, du = dh * gs;
+    const float s = sigma(g), gs = g * s, du = dh * gs;
     dh = dh * u * fmaf(gs, 1.0f - s, s);
     g = gs * u;
     u = du;
@@ -290,73 +292,92 @@ template <typename T, int EPI> struct RowEpilogue {
     }
 };
 
-// Tiles of all groups in one order.  Offsets come from device memory: they are clamped to the rows and made ascending here,
-// so that no offset can lead outside of the operands.
+// The tiles that a worker (a block or a pair of blocks) takes, in order.  Groups come in two classes: of those with few rows the
+// weights (or the output) are the cost, of the others the products.  Each class is dealt out over the workers tile by tile, so
+// that those at work at one time share operands in L2, and a worker takes turns between its tiles of the two, in the proportion
+// in which it has them: memory and tensor cores are then busy at the same time (one class after the other took
+// 124 -> 103 us at 64 experts, 32768 rows by Zipf's law, 1024 -> 2048).  The second class is dealt from the other end, so that
+// the workers with one tile more in both are few.
+// Offsets come from device memory: they are clamped to the rows and made ascending here, so that no offset can lead outside of
+// the operands.
 template <int BM> struct Schedule {
     int bound[MAX_GROUPS + 1];
-    int first[MAX_GROUPS + 1];      // first tile of each group (NT, NN)
+    int first[MAX_GROUPS + 1];      // first tile of each group, in the order of `group`; behind all of them their number
+    uint16_t group[MAX_GROUPS];     // the groups with many rows, then the others
+    int many;                       // tiles of the first class
     struct Tile { int e, m, n, lo, hi; };
 
     __device__ static int row_tiles(int n) { return (n + BM - 1) / BM; }
-    // by all threads of the first warp
-    __device__ void build(const Args &p, int form, int col_tiles, int lane)
+    // the offsets, by all threads of the block; a barrier of the block follows
+    __device__ void fetch(const Args &p)
     {
-        if (!p.offsets) {
-            if (lane < 2) bound[lane] = lane ? p.rows : 0, first[lane] = lane ? row_tiles(p.rows) * col_tiles : 0;
-            __syncwarp();
-            return;
+        for (int i = threadIdx.x; i <= p.groups; i += blockDim.x) {
+            const int64_t o = p.offsets ? p.offsets[i] : i ? p.rows : 0;
+            bound[i] = o < 0 ? 0 : o > p.rows ? p.rows : (int)o;
         }
-        int below = 0, tiles = 0;   // carried over the blocks of 32
+    }
+    // by all threads of a warp; groups of at most `few` rows are of the second class
+    __device__ void build(const Args &p, int form, int col_tiles, int few, int lane)
+    {
+        const int per = row_tiles(p.mdim) * col_tiles;      // TN: tiles of every group
+        int below = 0;
         for (int i0 = 0; i0 <= p.groups; i0 += 32) {
             const int i = i0 + lane;
-            int64_t o = i <= p.groups ? p.offsets[i] : 0;
-            int b = o < 0 ? 0 : o > p.rows ? p.rows : (int)o;
-            b = max(b, below);
+            int b = max(i <= p.groups ? bound[i] : 0, below);
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const int x = __shfl_up_sync(~0u, b, d);
                 if (lane >= d) b = max(b, x);
             }
-            int prev = __shfl_up_sync(~0u, b, 1);
-            if (lane == 0) prev = below;
-            int t = i > 0 && i <= p.groups ? row_tiles(b - prev) * col_tiles : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const int x = __shfl_up_sync(~0u, t, d);
-                if (lane >= d) t += x;
-            }
-            t += tiles;
-            if (i <= p.groups) bound[i] = b, first[i] = t;
+            if (i <= p.groups) bound[i] = b;
             below = __shfl_sync(~0u, b, 31);
-            tiles = __shfl_sync(~0u, t, 31);
         }
         __syncwarp();
-    }
-    __device__ int total(const Args &p, int form, int col_tiles) const
-    {
-        return form == TN ? p.groups * row_tiles(p.mdim) * col_tiles : first[p.groups];
-    }
-    __device__ Tile tile(const Args &p, int form, int col_tiles, int t) const
-    {
-        Tile r;
-        int rows;
-        if (form == TN) {
-            rows = p.mdim;
-            const int per = row_tiles(rows) * col_tiles;
-            r.e = t / per;
-            t -= r.e * per;
-        } else {
-            int lo = 0, hi = p.groups - 1;                  // last group whose first tile is not behind t
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (first[mid] <= t) lo = mid; else hi = mid - 1;
+        int at = 0, tiles = 0;
+        for (int second = 0; second < 2; second++) {
+            if (second && lane == 0) many = tiles;
+            for (int i0 = 0; i0 < p.groups; i0 += 32) {
+                const int i = i0 + lane, rows = i < p.groups ? bound[i + 1] - bound[i] : 0;
+                const bool mine = i < p.groups && (rows <= few) == (second == 1);
+                const unsigned all = __ballot_sync(~0u, mine);
+                int t = !mine ? 0 : form == TN ? per : row_tiles(rows) * col_tiles;
+                const int own = t;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const int x = __shfl_up_sync(~0u, t, d);
+                    if (lane >= d) t += x;
+                }
+                if (mine) {
+                    const int k = at + __popc(all & ((1u << lane) - 1));
+                    group[k] = (uint16_t)i, first[k] = tiles + t - own;
+                }
+                at += __popc(all);
+                tiles += __shfl_sync(~0u, t, 31);
             }
-            r.e = lo;
-            t -= first[lo];
-            rows = bound[lo + 1] - bound[lo];
         }
+        if (lane == 0) first[p.groups] = tiles;
+        __syncwarp();
+    }
+    // tiles of worker w of n
+    struct Share { int a, b; };
+    __device__ Share share(int groups, int w, int n) const { return {max(0, (many - w + n - 1) / n), max(0, (first[groups] - many - (n - 1 - w) + n - 1) / n)}; }
+    // its i-th
+    __device__ Tile tile(const Args &p, int form, int col_tiles, Share s, int i, int w, int n) const
+    {
+        const int all = s.a + s.b;
+        const int64_t phase = (int64_t)w * all / n;         // workers are at different places of the same pattern
+        const int a0 = (int)((i * (int64_t)s.a + phase) / all), a1 = (int)(((i + 1) * (int64_t)s.a + phase) / all);
+        int t = a1 > a0 ? w + a0 * n : many + (n - 1 - w) + (i - a0) * n;
+        int lo = 0, hi = p.groups - 1;                      // last place whose first tile is not behind t
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= t) lo = mid; else hi = mid - 1;
+        }
+        Tile r;
+        r.e = group[lo];
+        t -= first[lo];
         r.lo = bound[r.e], r.hi = bound[r.e + 1];
-        const int mt = row_tiles(rows), band = min(mt, BAND);
+        const int mt = row_tiles(form == TN ? p.mdim : r.hi - r.lo), band = min(mt, BAND);
         const int which = t / (band * col_tiles);
         t -= which * band * col_tiles;
         const int high = min(band, mt - which * band);
@@ -380,11 +401,13 @@ template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) 
     const int tid = threadIdx.x;
     constexpr int BN = EPI == GATED ? TILE_N / 2 : TILE_N;
     const int col_tiles = (p.ncols + BN - 1) / BN;
-    if (tid < 32) sched.build(p, FORM, col_tiles, tid);
+    sched.fetch(p);
     __syncthreads();
-    const int total = sched.total(p, FORM, col_tiles);
-    for (int t = blockIdx.x; t < total; t += gridDim.x) {
-        const auto tile = sched.tile(p, FORM, col_tiles, t);
+    if (tid < 32) sched.build(p, FORM, col_tiles, 0, tid);
+    __syncthreads();
+    const auto share = sched.share(p.groups, blockIdx.x, gridDim.x);
+    for (int t = 0; t < share.a + share.b; t++) {
+        const auto tile = sched.tile(p, FORM, col_tiles, share, t, blockIdx.x, gridDim.x);
         const int m0 = tile.m * PM, n0 = tile.n * BN;
         const int mrows = FORM == TN ? p.mdim - m0 : tile.hi - tile.lo - m0;        // rows of out from m0 on
         const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
@@ -441,30 +464,34 @@ template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) 
     }
 }
 
-// ---- the loss from the pieces' statistics ------------------------------------------------------------------------------
-// lse = M + log(sum_t s_t exp(m_t - M)).  A block takes 32 rows, its warps every eighth piece; a piece's rows lie side by side.
+// ---- the loss from the pieces' statistics -----------------------------------------------------------------------------
+// lse = M + log(sum_t s_t exp(m_t - M)).  A block takes 8 rows, whose statistics lie side by side, and 32 slices of the pieces.
 __global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int pieces, int rows, const float *at_target, const int64_t *target,
                                                         int64_t ignore, int V, float *loss, float *lse)
 {
-    __shared__ float2 sh[8][32];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    __shared__ float2 sh[32][8];
+    const int r = threadIdx.x & 7, slice = threadIdx.x >> 3, row = blockIdx.x * 8 + r;
     float m = -INFINITY, s = 0.0f;
-    if (row < rows)
-        for (int t = w; t < pieces; t += 8) {
+    if (row < rows) {
+#pragma unroll 4
+        for (int t = slice; t < pieces; t += 32) {
             const float2 x = part[(int64_t)t * rows + row];
             const float top = fmaxf(m, x.x);
             const float from = top == -INFINITY ? 0.0f : top;
-            s = s * expf(m - from) + x.y * expf(x.x - from);
+            s = s * __expf(m - from) + x.y * __expf(x.x - from);
             m = top;
         }
-    sh[w][lane] = make_float2(m, s);
+    }
+    sh[slice][r] = make_float2(m, s);
     __syncthreads();
-    if (w || row >= rows) return;
+    if (slice || row >= rows) return;
     float top = -INFINITY;
-    for (int i = 0; i < 8; i++) top = fmaxf(top, sh[i][lane].x);
+#pragma unroll
+    for (int i = 0; i < 32; i++) top = fmaxf(top, sh[i][r].x);
     const float from = top == -INFINITY ? 0.0f : top;
     s = 0.0f;
-    for (int i = 0; i < 8; i++) s += sh[i][lane].y * expf(sh[i][lane].x - from);
+#pragma unroll
+    for (int i = 0; i < 32; i++) s += sh[i][r].y * __expf(sh[i][r].x - from);
     const float l = top + logf(s);
     lse[row] = l;
     const int64_t t = target[row];

@@ -15,6 +15,9 @@ template <int EPI> struct Turned {
     static constexpr int ROWS = EPI == GATED ? 128 : 256;           // most rows of a tile
     static constexpr int A_BYTES = (EPI == GATED ? 2 : 1) * 128 * BK * 2, B_BYTES = ROWS / 2 * BK * 2, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = EPI == GATED ? 5 : 6;
+    static constexpr int FEW = 256;                                 // rows of a group whose weight costs more to read than to multiply
+    static constexpr int PIECE = EPI == STORE ? 32 : 16;            // rows that a warp takes at a time: what fits its registers
+    static constexpr int OUT = PIECE * 64;                          // shared memory of a warp for them
 };
 
 template <int EPI> struct TurnedShared {
@@ -24,8 +27,8 @@ template <int EPI> struct TurnedShared {
     int stop;
 };
 
-// A warp's 32 columns (one for each lane) of 32 rows of 16-bit values, to and from memory through 2 KB of shared memory: words of
-// two rows of a column, 16 rows of 32 words.  Four lanes take two rows' 64 bytes; of pairs side by side one reads the words the
+// A warp's 32 columns (one for each lane) of R rows of 16-bit values, to and from memory through shared memory: words of two
+// rows of a column, R / 2 rows of 32 words.  Four lanes take two rows' 64 bytes; of pairs side by side one reads the words the
 // other way around, so that the banks differ.
 struct WarpColumns {
     uint32_t *staged;
@@ -33,20 +36,20 @@ struct WarpColumns {
     template <typename T> __device__ __forceinline__ bool whole(const T *first, int64_t ld, int cols) const { return cols >= 32 && ((uintptr_t)first & 15) == 0 && ld % 8 == 0; }
     __device__ __forceinline__ uint4 *words(int pair, int c, int h) const { return (uint4 *)(staged + pair * 32 + c * 8 + h * 4); }
     // first: row 0 of the first lane's column; rows, cols: how many there are
-    template <typename T> __device__ __forceinline__ void store(T *first, int64_t ld, const float (&v)[32], int rows, int cols) const
+    template <typename T, int R> __device__ __forceinline__ void store(T *first, int64_t ld, const float (&v)[R], int rows, int cols) const
     {
         if (!whole(first, ld, cols)) {
 #pragma unroll
-            for (int i = 0; i < 32; i++)
+            for (int i = 0; i < R; i++)
                 if (i < rows && lane < cols) first[i * ld + lane] = from_float<T>(v[i]);
             return;
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 16; i++) staged[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
+        for (int i = 0; i < R / 2; i++) staged[i * 32 + lane] = pack2(v[2 * i], v[2 * i + 1], T());
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < R / 16; i++) {
             const int pair = i * 8 + (lane >> 2), c = lane & 3, odd = pair & 1;
             const uint4 x = *words(pair, c, odd), y = *words(pair, c, odd ^ 1);
             const uint4 lo = odd ? y : x, hi = odd ? x : y;
@@ -57,25 +60,25 @@ struct WarpColumns {
         }
     }
     // in two steps, so that the loads are on their way while something else is waited for
-    template <typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[4], int rows, int cols) const
+    template <int R, typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[R / 8], int rows, int cols) const
     {
         if (!whole(first, ld, cols)) return;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < R / 8; i++) {
             const int r = 2 * (i / 2 * 8 + (lane >> 2)) + i % 2;
             w[i] = r < rows ? *(const uint4 *)(first + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
         }
     }
-    template <typename T> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[4], float (&v)[32], int rows, int cols) const
+    template <typename T, int R> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[R / 8], float (&v)[R], int rows, int cols) const
     {
         if (!whole(first, ld, cols)) {
 #pragma unroll
-            for (int i = 0; i < 32; i++) v[i] = i < rows && lane < cols ? to_float(first[i * ld + lane]) : 0.0f;
+            for (int i = 0; i < R; i++) v[i] = i < rows && lane < cols ? to_float(first[i * ld + lane]) : 0.0f;
             return;
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < R / 16; i++) {
             const int pair = i * 8 + (lane >> 2), c = lane & 3, odd = pair & 1;
             const uint4 a = w[2 * i], b = w[2 * i + 1];
             const uint4 lo = make_uint4(__byte_perm(a.x, b.x, 0x5410), __byte_perm(a.x, b.x, 0x7632), __byte_perm(a.y, b.y, 0x5410), __byte_perm(a.y, b.y, 0x7632));
@@ -85,7 +88,7 @@ struct WarpColumns {
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
+        for (int i = 0; i < R / 2; i++) {
             const float2 f = unpack2(staged[i * 32 + lane], T());
             v[2 * i] = f.x, v[2 * i + 1] = f.y;
         }
@@ -100,13 +103,14 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
     extern __shared__ char raw[];
     char *stages = (char *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     char *outs = stages + S::STAGES * S::STAGE;
-    TurnedShared<EPI> &sh = *(TurnedShared<EPI> *)(outs + 8 * 2048);
+    TurnedShared<EPI> &sh = *(TurnedShared<EPI> *)(outs + 8 * S::OUT);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     constexpr int BN = 256;                                 // columns of out that a tile covers
     const int col_tiles = (p.ncols + BN - 1) / BN;
 
-    if (warp == 0) sh.sched.build(p, FORM, col_tiles, lane);
+    sh.sched.fetch(p);
+    if (threadIdx.x == 0) prefetch_map(&map_w), prefetch_map(&map_rows);
     if (warp == 1) {
         if (lane == 0) {
             for (int i = 0; i < S::STAGES; i++) bar_init(&sh.full[i], 2), bar_init(&sh.empty[i], 1);
@@ -118,22 +122,25 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
         __syncwarp();
         tmem_alloc<2>(&sh.tmem);
     }
+    __syncthreads();
+    if (warp == 0) sh.sched.build(p, FORM, col_tiles, S::FEW, lane);
     fence_before();
     __syncthreads();
     cluster_sync();
     fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sh.tmem;
     volatile int *stop = &sh.stop;
-    const int total = sh.sched.total(p, FORM, col_tiles);
-    const int step = gridDim.x / 2, begin = blockIdx.x / 2;
+    const int workers = gridDim.x / 2, worker = blockIdx.x / 2;
+    const auto share = sh.sched.share(p.groups, worker, workers);
+    const int total = share.a + share.b;
     // rows of a tile, as the products count them
     auto rows_of = [](const auto &tile) { return min(S::ROWS, (tile.hi - tile.lo - tile.m * S::ROWS + 31) & ~31); };
 
     if (warp == 0) {
         uint32_t at = 0;
         bool good = true;
-        for (int t = begin; t < total && good; t += step) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+        for (int t = 0; t < total && good; t++) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int n0 = tile.n * BN + (int)rank * 128, half = rows_of(tile) / 2, row = tile.lo + tile.m * S::ROWS + (int)rank * half;
             for (int k = 0; k < p.kdim; k += BK, at++) {
                 const int s = at % S::STAGES;
@@ -161,8 +168,8 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
             constexpr uint32_t idesc = 1u << 4 | TypeBits<T>::value << 7 | TypeBits<T>::value << 10 | (FORM == NN ? 1u << 15 : 0) | (256u / 16) << 24;
             uint32_t at = 0, sums = 0;
             bool good = true;
-            for (int t = begin; t < total && good; t += step) {
-                const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+            for (int t = 0; t < total && good; t++) {
+                const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
                 const uint32_t of = idesc | (uint32_t)(rows_of(tile) / 8) << 17;
                 const int set = sums & 1;
                 if (!(good = bar_wait(&sh.acc_empty[set], (sums / 2 + 1) & 1, stop))) break;
@@ -190,22 +197,23 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
     } else {
         uint32_t sums = 0;
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const WarpColumns w{(uint32_t *)(outs + (warp - 2) * 2048), lane};
+        const WarpColumns w{(uint32_t *)(outs + (warp - 2) * S::OUT), lane};
         const uint32_t from = tmem + ((uint32_t)quarter << 21);
-        for (int t = begin; t < total; t += step) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+        for (int t = 0; t < total; t++) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int set = sums & 1, col = tile.n * BN + (int)rank * 128 + quarter * 32, cols = p.ncols - col;
-            const int chunks = rows_of(tile) / 32, live = tile.hi - tile.lo - tile.m * S::ROWS;
+            constexpr int R = S::PIECE;
+            const int pieces = rows_of(tile) / R, live = tile.hi - tile.lo - tile.m * S::ROWS;
             const int64_t row0 = (int64_t)tile.lo + tile.m * S::ROWS;
-            uint4 g4[EPI == GATED_BACK ? 4 : 1], u4[EPI == GATED_BACK ? 4 : 1];
+            uint4 g4[R / 8], u4[R / 8];
             auto ahead = [&](int q) {
                 if constexpr (EPI == GATED_BACK) {
-                    const T *gu = (const T *)p.gu + (row0 + q * 32) * p.ldgu + col;
-                    w.fetch(gu, p.ldgu, g4, live - q * 32, cols);
-                    w.fetch(gu + p.ncols, p.ldgu, u4, live - q * 32, cols);
+                    const T *gu = (const T *)p.gu + (row0 + q * R) * p.ldgu + col;
+                    w.fetch<R>(gu, p.ldgu, g4, live - q * R, cols);
+                    w.fetch<R>(gu + p.ncols, p.ldgu, u4, live - q * R, cols);
                 }
             };
-            if (cols > 0 && half < chunks) ahead(half);
+            if (cols > 0 && half < pieces) ahead(half);
             if (!bar_wait(&sh.acc_full[set], (sums / 2) & 1, stop)) break;
             sums++;
             fence_after();
@@ -214,49 +222,54 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
                 __syncwarp();
                 if (lane == 0) bar_arrive_at<2>(of_leader(smem_u32(&sh.acc_empty[set])));
             };
-            if (cols <= 0 || half >= chunks) {
+            if (cols <= 0 || half >= pieces) {
                 taken();
                 continue;
             }
-            for (int q = half; q < chunks; q += 2) {
-                const int n = live - q * 32;                // rows of this piece
-                const int64_t row = row0 + q * 32;
-                float v[32], v2[32];
+            for (int q = half; q < pieces; q += 2) {
+                const int n = live - q * R;                 // rows of this piece
+                const int64_t row = row0 + q * R;
+                float v[R];
                 __syncwarp();
-                tmem_load32(from + set * 256 + q * 32, v);
-                if (EPI == GATED) tmem_load32(from + set * 256 + 128 + q * 32, v2);
-                tmem_load_wait();
-                if (q + 2 >= chunks) taken();
+                tmem_load(from + set * 256 + q * R, v);
                 if constexpr (EPI == STORE) {
+                    tmem_load_wait();
+                    if (q + 2 >= pieces) taken();
                     T *o = (T *)p.out + row * p.ldo + col;
                     if (p.accumulate) {
 #pragma unroll
-                        for (int i = 0; i < 32; i++)
+                        for (int i = 0; i < R; i++)
                             if (i < n && lane < cols) v[i] += to_float(o[i * p.ldo + lane]);
                     }
                     w.store(o, p.ldo, v, n, cols);
                 }
                 if constexpr (EPI == GATED) {
+                    float v2[R];
+                    tmem_load(from + set * 256 + 128 + q * R, v2);
+                    tmem_load_wait();
+                    if (q + 2 >= pieces) taken();
                     if (p.out) {
                         T *o = (T *)p.out + row * p.ldo + col;
                         w.store(o, p.ldo, v, n, cols);
                         w.store(o + p.ncols, p.ldo, v2, n, cols);
                     }
 #pragma unroll
-                    for (int i = 0; i < 32; i++) v[i] = gate(v[i], v2[i]);
+                    for (int i = 0; i < R; i++) v[i] = gate(v[i], v2[i]);
                     w.store((T *)p.h + row * p.ldh + col, p.ldh, v, n, cols);
                 }
                 if constexpr (EPI == GATED_BACK) {
-                    float g[32];
+                    float g[R], u[R];
+                    tmem_load_wait();
+                    if (q + 2 >= pieces) taken();
                     const T *gu = (const T *)p.gu + row * p.ldgu + col;
                     w.take(gu, p.ldgu, g4, g, n, cols);
-                    w.take(gu + p.ncols, p.ldgu, u4, v2, n, cols);
-                    if (q + 2 < chunks) ahead(q + 2);
+                    w.take(gu + p.ncols, p.ldgu, u4, u, n, cols);
+                    if (q + 2 < pieces) ahead(q + 2);
 #pragma unroll
-                    for (int i = 0; i < 32; i++) gate_back(g[i], v2[i], v[i]);
+                    for (int i = 0; i < R; i++) gate_back(g[i], u[i], v[i]);
                     T *o = (T *)p.out + row * p.ldo + col;
                     w.store(o, p.ldo, v, n, cols);
-                    w.store(o + p.ncols, p.ldo, v2, n, cols);
+                    w.store(o + p.ncols, p.ldo, u, n, cols);
                     if (p.h) w.store((T *)p.h + row * p.ldh + col, p.ldh, g, n, cols);
                 }
             }

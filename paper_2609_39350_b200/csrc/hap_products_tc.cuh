@@ -30,6 +30,7 @@ template <int EPI, int CG> struct Shape {
     // 1024 steps there, and these sums in registers; reading them costs some 400 cycles in 8192, under the next products.
     static constexpr bool SUMS = EPI == STORE32 || EPI == LSE;
     static constexpr int SUM_STEPS = 1024;
+    static constexpr int FEW = 1024;                    // TN: rows of a group whose output costs more than its products
 };
 
 template <int EPI, int CG> struct Shared {
@@ -108,6 +109,7 @@ template <int CG> __device__ __forceinline__ void tma_load(const CUtensorMap *ma
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
                      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 template <int CG> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
     if constexpr (CG == 1)
@@ -141,6 +143,19 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16])
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
                    "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load8(uint32_t addr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    tmem_load16(addr, r);
+#pragma unroll
+    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -205,7 +220,8 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
     constexpr int BN = TILE_N;
     const int col_tiles = (p.ncols + BN - 1) / BN;
 
-    if (warp == 0) sh.sched.build(p, FORM, col_tiles, lane);
+    sh.sched.fetch(p);
+    if (threadIdx.x == 0) prefetch_map(&map_a), prefetch_map(&map_b);
     if (warp == 1) {
         if (lane == 0) {
             for (int i = 0; i < S::STAGES; i++) bar_init(&sh.full[i], CG), bar_init(&sh.empty[i], 1);
@@ -218,14 +234,17 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
         __syncwarp();
         tmem_alloc<CG>(&sh.tmem);
     }
+    __syncthreads();
+    if (warp == 0) sh.sched.build(p, FORM, col_tiles, FORM == TN ? S::FEW : 0, lane);
     fence_before();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();
     fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sh.tmem;
     volatile int *stop = &sh.stop;
-    const int total = sh.sched.total(p, FORM, col_tiles);
-    const int step = gridDim.x / CG, begin = blockIdx.x / CG;
+    const int workers = gridDim.x / CG, worker = blockIdx.x / CG;
+    const auto share = sh.sched.share(p.groups, worker, workers);
+    const int total = share.a + share.b;
 
     if (warp == 0) {
         uint32_t at = 0;                                    // stages brought so far
@@ -242,8 +261,8 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
             if (lane == 0) bar_arrive_with_data_at(CG == 1 ? full : of_leader(full));
             end_rows = 0;
         };
-        for (int t = begin; t < total && good; t += step) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+        for (int t = 0; t < total && good; t++) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int m0 = tile.m * S::BM + rank * 128, n0 = tile.n * BN;
             const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
             for (int k = 0; k < K && good; k += BK, at++) {
@@ -282,10 +301,10 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
             constexpr uint32_t idesc = Instruction<T, FORM, CG>::bits;
             uint32_t at = 0, sums = 0;
             bool good = true;
-            for (int t = begin; t < total && good; t += step) {
+            for (int t = 0; t < total && good; t++) {
                 int K = p.kdim;
                 if (FORM == TN) {
-                    const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+                    const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
                     K = tile.hi - tile.lo;
                     if (!K) continue;                       // nothing to sum: the epilogue writes zeros by itself
                 }
@@ -321,8 +340,8 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
         constexpr int CHUNKS = BN / 64;                     // pieces of 32 columns that a warp has
         char *staged = outs + (warp - 2) * S::OUT;
         const uint32_t from = tmem + ((uint32_t)quarter << 21) + half * CHUNKS * 32;
-        for (int t = begin; t < total; t += step) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
+        for (int t = 0; t < total; t++) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int m = tile.m * S::BM + rank * 128 + quarter * 32, n0 = tile.n * BN + half * CHUNKS * 32;
             const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
             if (FORM == TN && !K && p.accumulate) continue;
@@ -347,13 +366,13 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
                     sums++;
                     fence_after();
 #pragma unroll
-                    for (int q = 0; q < 2 * CHUNKS; q++) {
-                        uint32_t v[16];
+                    for (int q = 0; q < 4 * CHUNKS; q++) {  // eight at a time: the sums fill the registers
+                        uint32_t v[8];
                         __syncwarp();
-                        tmem_load16(from + set * TILE_N + q * 16, v);
+                        tmem_load8(from + set * TILE_N + q * 8, v);
                         tmem_load_wait();
 #pragma unroll
-                        for (int i = 0; i < 16; i++) acc[q / 2][q % 2 * 16 + i] += __uint_as_float(v[i]);
+                        for (int i = 0; i < 8; i++) acc[q / 4][q % 4 * 8 + i] += __uint_as_float(v[i]);
                     }
                     taken(set);
                 }
