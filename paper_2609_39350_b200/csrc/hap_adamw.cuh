@@ -30,18 +30,20 @@ template <int N> __device__ __forceinline__ int adamw_tensor(const AdamwList<N> 
     return lo;
 }
 
+__device__ __forceinline__ float root_of(float x) { float y; asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// (a root and a quotient that are off by a unit or two in the last place: the parameter's own rounding is larger or as large)
 __device__ __forceinline__ float adamw_value(float p, float m, float v, const AdamwFactors &f)
 {
-    return p * f.decay - f.step * m / (sqrtf(v) * f.root + f.eps);
+    return p * f.decay - __fdividef(f.step * m, root_of(v) * f.root + f.eps);
 }
-__device__ __forceinline__ float adamw_read_m(int c, float s)
+__device__ __forceinline__ float adamw_read_m(float c, float s)
 {
-    const float t = __fmul_rn((float)c, 1.0f / 127.0f);
+    const float t = __fmul_rn(c, 1.0f / 127.0f);
     return __fmul_rn(__fmul_rn(t, fabsf(t)), s);
 }
-__device__ __forceinline__ float adamw_read_v(int c, float s)
+__device__ __forceinline__ float adamw_read_v(float c, float s)
 {
-    const float t = __fmul_rn((float)c, 1.0f / 255.0f), q = __fmul_rn(t, t);
+    const float t = __fmul_rn(c, 1.0f / 255.0f), q = __fmul_rn(t, t);
     return __fmul_rn(__fmul_rn(q, q), s);
 }
 __device__ __forceinline__ float adamw_first(float m, float g, const AdamwFactors &f) { return __fadd_rn(__fmul_rn(m, f.b1), __fmul_rn(g, f.a1)); }
@@ -55,6 +57,41 @@ __device__ __forceinline__ void adamw_copy(void *copy, int fp16, uint64_t i, flo
     else ((__nv_bfloat16 *)copy)[i] = __float2bfloat16_rn(x);
 }
 
+// eight values side by side, at an address that is a multiple of 16 bytes
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    } else {
+        const uint4 a = *(const uint4 *)p;
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float2 f = unpack2(w[i], T());
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        ((float4 *)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        ((float4 *)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        *(uint4 *)p = make_uint4(pack2(x[0], x[1], T()), pack2(x[2], x[3], T()), pack2(x[4], x[5], T()), pack2(x[6], x[7], T()));
+    }
+}
+__device__ __forceinline__ void copy8(void *copy, int fp16, uint64_t i, const float (&x)[8])
+{
+    if (fp16) store8((__half *)copy + i, x);
+    else store8((__nv_bfloat16 *)copy + i, x);
+}
+// values in front of the first one whose address, and those of the following eights, is a multiple of 16 bytes
+template <typename T> __device__ __forceinline__ int in_front(const T *p) { return (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)); }
+
+// States in 32 bits: 12 to 30 bytes a value and nothing else to do; bound by memory.  Tensors that begin at the same odd place in
+// all of their buffers (views of flat buffers) move in eights from the first aligned value on; others value by value.
 template <typename P, typename G, int N> __global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ AdamwList<N> list, AdamwFactors f, const float *grad_scale)
 {
     const int k = adamw_tensor(list, blockIdx.x);
@@ -64,14 +101,132 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
     P *p = (P *)t.p + from;
     const G *g = (const G *)t.g + from;
     float *m = (float *)t.m + from, *v = (float *)t.v + from;
+    char *copy = t.copy ? (char *)t.copy + 2 * from : nullptr;
     const float scale = grad_scale ? *grad_scale : 1.0f;
-    for (int i = threadIdx.x; i < n; i += 256) {
+    auto one = [&](int i) {
         const float x = to_float(g[i]) * scale;
         const float mi = adamw_first(m[i], x, f), vi = adamw_second(v[i], x, f);
         m[i] = mi, v[i] = vi;
         const float y = adamw_value(to_float(p[i]), mi, vi, f);
         p[i] = from_float<P>(y);
-        if (t.copy) adamw_copy(t.copy, f.copy16, from + i, y);
+        if (copy) adamw_copy(copy, f.copy16, i, y);
+    };
+    const int h = max(in_front(p), max(in_front(g), copy ? in_front((const __half *)copy) : 0));
+    const bool eights = !(((uintptr_t)(p + h) | (uintptr_t)(g + h) | (uintptr_t)(m + h) | (uintptr_t)(v + h) | (copy ? (uintptr_t)(copy + 2 * h) : 0)) & 15);
+    if (!eights) {
+        for (int i = threadIdx.x; i < n; i += 256) one(i);
+        return;
+    }
+    const int groups = n > h ? (n - h) / 8 : 0, rest = h + groups * 8;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < groups; i += 256) {
+        const int at = h + i * 8;
+        float x[8], a[8], b[8], y[8];
+        load8(g + at, x), load8(m + at, a), load8(v + at, b), load8(p + at, y);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            x[j] *= scale;
+            a[j] = adamw_first(a[j], x[j], f), b[j] = adamw_second(b[j], x[j], f);
+            y[j] = adamw_value(y[j], a[j], b[j], f);
+        }
+        store8(m + at, a), store8(v + at, b), store8(p + at, y);
+        if (copy) copy8(copy, f.copy16, at, y);
+    }
+    if (threadIdx.x < min(h, n)) one(threadIdx.x);
+    if (rest + (int)threadIdx.x < n) one(rest + threadIdx.x);          // (fewer than eight)
+}
+
+// c of a magnitude x under the scale s, as the definition's operations round it.  The quick way's result q is off by less than 1e-4
+// (some units in the last place of at most 255), so only where it lies that near to a border are the operations themselves made;
+// made everywhere they took most of the kernel's time.
+template <bool FOURTH> __device__ __forceinline__ float adamw_code(float x, float s, float inverse)
+{
+    const float most = FOURTH ? 255.0f : 127.0f;
+    float q = root_of(x * inverse);
+    if (FOURTH) q = root_of(q);
+    q *= most;
+    float c = rintf(q);
+    if (!(fabsf(q - c) < 0.4998f)) {
+        q = __fsqrt_rn(__fdiv_rn(x, s));
+        if (FOURTH) q = __fsqrt_rn(q);
+        c = rintf(__fmul_rn(q, most));
+    }
+    return c;
+}
+
+// States in 8 bits: a warp takes the 256 values of a block, eight for each lane, side by side where every address allows it.
+template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void adamw8_block(const AdamwTensor &t, uint64_t from, const AdamwFactors &f, float scale, int lane)
+{
+    const uint64_t block = from / ADAMW_BLOCK;
+    const int n = (int)min((uint64_t)ADAMW_BLOCK, t.n - from);
+    P *p = (P *)t.p + from;
+    const G *g = (const G *)t.g + from;
+    int8_t *m = (int8_t *)t.m + from;
+    uint8_t *v = (uint8_t *)t.v + from;
+    char *copy = t.copy ? (char *)t.copy + 2 * from : nullptr;
+    const float ms = t.ms[block], vs = t.vs[block];
+    float x[8], y[8], a[8], b[8];
+    auto at = [&](int j) { return EIGHTS ? lane * 8 + j : lane + 32 * j; };
+    if (EIGHTS) {
+        const uint2 cm = *(const uint2 *)(m + lane * 8), cv = *(const uint2 *)(v + lane * 8);
+        load8(g + lane * 8, x), load8(p + lane * 8, y);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            a[j] = (float)(int8_t)((j < 4 ? cm.x : cm.y) >> 8 * (j & 3));
+            b[j] = (float)(uint8_t)((j < 4 ? cv.x : cv.y) >> 8 * (j & 3));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int i = at(j);
+            const bool in = i < n;
+            a[j] = in ? (float)m[i] : 0.0f, b[j] = in ? (float)v[i] : 0.0f, x[j] = in ? to_float(g[i]) : 0.0f, y[j] = in ? to_float(p[i]) : 0.0f;
+        }
+    }
+    float mt = 0.0f, vt = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        x[j] = __fmul_rn(x[j], scale);
+        a[j] = adamw_first(adamw_read_m(a[j], ms), x[j], f);
+        b[j] = adamw_second(adamw_read_v(b[j], vs), x[j], f);
+        y[j] = adamw_value(y[j], a[j], b[j], f);
+        if (EIGHTS || at(j) < n) mt = larger(mt, fabsf(a[j])), vt = larger(vt, b[j]);
+    }
+    if (EIGHTS) {
+        store8(p + lane * 8, y);
+        if (copy) copy8(copy, f.copy16, lane * 8, y);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int i = at(j);
+            if (i < n) p[i] = from_float<P>(y[j]);
+            if (i < n && copy) adamw_copy(copy, f.copy16, i, y[j]);
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
+        mt = larger(mt, __shfl_xor_sync(~0u, mt, d));
+        vt = larger(vt, __shfl_xor_sync(~0u, vt, d));
+    }
+    if (lane == 0) t.ms[block] = mt, t.vs[block] = vt;
+    // (codes of a block whose scale is not finite are read as values that are not finite, whatever they are; where a scale is
+    // so small that its inverse overflows, or 0, the quick way gives no number and the operations are made)
+    const float md = mt > 0.0f ? mt : 1.0f, vd = vt > 0.0f ? vt : 1.0f, mr = __fdividef(1.0f, md), vr = __fdividef(1.0f, vd);
+    uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        const float q = adamw_code<false>(fabsf(a[j]), md, mr), u = adamw_code<true>(b[j], vd, vr);
+        const int8_t c = (int8_t)(int)copysignf(fminf(q, 127.0f), a[j]);
+        const uint8_t w = (uint8_t)(b[j] > 0.0f ? min(255, max(1, (int)u)) : 0);
+        if (EIGHTS) {
+            cm[j / 4] |= (uint32_t)(uint8_t)c << 8 * (j & 3), cv[j / 4] |= (uint32_t)w << 8 * (j & 3);
+        } else if (at(j) < n) {
+            m[at(j)] = c, v[at(j)] = w;
+        }
+    }
+    if (EIGHTS) {
+        *(uint2 *)(m + lane * 8) = make_uint2(cm[0], cm[1]);
+        *(uint2 *)(v + lane * 8) = make_uint2(cv[0], cv[1]);
     }
 }
 
@@ -80,48 +235,13 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
     const int k = adamw_tensor(list, blockIdx.x);
     const AdamwTensor &t = list.t[k];
     const float scale = grad_scale ? *grad_scale : 1.0f;
-    const int lane = threadIdx.x & 31;
     const uint64_t first = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
+    const bool eights = !(((uintptr_t)t.p | (uintptr_t)t.g | (uintptr_t)t.copy) & 15) && !(((uintptr_t)t.m | (uintptr_t)t.v) & 7);
     for (int w = threadIdx.x >> 5; w < ADAMW_CHUNK / ADAMW_BLOCK; w += 8) {
-        const uint64_t from = first + w * ADAMW_BLOCK, block = from / ADAMW_BLOCK;
+        const uint64_t from = first + w * ADAMW_BLOCK;
         if (from >= t.n) break;
-        const int n = (int)min((uint64_t)ADAMW_BLOCK, t.n - from);
-        P *p = (P *)t.p + from;
-        const G *g = (const G *)t.g + from;
-        int8_t *m = (int8_t *)t.m + from;
-        uint8_t *v = (uint8_t *)t.v + from;
-        const float ms = t.ms[block], vs = t.vs[block];
-        float mi[8], vi[8], mt = 0.0f, vt = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int i = lane + 32 * j;
-            mi[j] = vi[j] = 0.0f;
-            if (i >= n) continue;
-            const float x = __fmul_rn(to_float(g[i]), scale);
-            mi[j] = adamw_first(adamw_read_m(m[i], ms), x, f);
-            vi[j] = adamw_second(adamw_read_v(v[i], vs), x, f);
-            const float y = adamw_value(to_float(p[i]), mi[j], vi[j], f);
-            p[i] = from_float<P>(y);
-            if (t.copy) adamw_copy(t.copy, f.copy16, from + i, y);
-            mt = larger(mt, fabsf(mi[j])), vt = larger(vt, vi[j]);
-        }
-#pragma unroll
-        for (int d = 16; d; d /= 2) {
-            mt = larger(mt, __shfl_xor_sync(~0u, mt, d));
-            vt = larger(vt, __shfl_xor_sync(~0u, vt, d));
-        }
-        if (lane == 0) t.ms[block] = mt, t.vs[block] = vt;
-        // (codes of a block whose scale is not finite are read as values that are not finite, whatever they are)
-        const float md = mt > 0.0f ? mt : 1.0f, vd = vt > 0.0f ? vt : 1.0f;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int i = lane + 32 * j;
-            if (i >= n) continue;
-            const float q = rintf(__fmul_rn(__fsqrt_rn(__fdiv_rn(fabsf(mi[j]), md)), 127.0f));
-            const float u = rintf(__fmul_rn(__fsqrt_rn(__fsqrt_rn(__fdiv_rn(vi[j], vd))), 255.0f));
-            m[i] = (int8_t)(int)copysignf(fminf(q, 127.0f), mi[j]);
-            v[i] = (uint8_t)(vi[j] > 0.0f ? min(255, max(1, (int)u)) : 0);
-        }
+        if (eights && from + ADAMW_BLOCK <= t.n) adamw8_block<P, G, true>(t, from, f, scale, threadIdx.x & 31);
+        else adamw8_block<P, G, false>(t, from, f, scale, threadIdx.x & 31);
     }
 }
 
@@ -132,6 +252,7 @@ template <int N> __global__ void __launch_bounds__(256) adamw_values_kernel(cons
     const AdamwTensor &t = list.t[k];                           // (p: m's values, copy: v's values)
     const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
     const int n = (int)min((uint64_t)ADAMW_CHUNK, t.n - from);
+#pragma unroll 8
     for (int i = threadIdx.x; i < n; i += 256) {
         const uint64_t at = from + i, block = at / ADAMW_BLOCK;
         if (t.p) ((float *)t.p)[at] = adamw_read_m(((const int8_t *)t.m)[at], t.ms[block]);
