@@ -48,8 +48,12 @@ __device__ __forceinline__ float adamw_read_v(float c, float s)
 }
 __device__ __forceinline__ float adamw_first(float m, float g, const AdamwFactors &f) { return __fadd_rn(__fmul_rn(m, f.b1), __fmul_rn(g, f.a1)); }
 __device__ __forceinline__ float adamw_second(float v, float g, const AdamwFactors &f) { return __fadd_rn(__fmul_rn(v, f.b2), __fmul_rn(__fmul_rn(g, g), f.a2)); }
-// largest of two magnitudes; a NaN stays
-__device__ __forceinline__ float larger(float a, float b) { return a != a ? a : b > a || b != b ? b : a; }
+// A magnitude's bits, which order as the values do, infinity and then NaN above all.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// 0 .. 255 as a float: in the low bits of 2^23
+__device__ __forceinline__ float byte_value(uint32_t c) { return __uint_as_float(0x4b000000u | c) - 8388608.0f; }
+__device__ __forceinline__ float signed_byte_value(uint32_t c) { return __uint_as_float(0x4b000000u | (c ^ 0x80u)) - 8388736.0f; }
+
 // the copy in 16 bits of a parameter that is held in 32
 __device__ __forceinline__ void adamw_copy(void *copy, int fp16, uint64_t i, float x)
 {
@@ -138,20 +142,21 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
 
 // c of a magnitude x under the scale s, as the definition's operations round it.  The quick way's result q is off by less than 1e-4
 // (some units in the last place of at most 255), so only where it lies that near to a border are the operations themselves made;
-// made everywhere they took most of the kernel's time.
-template <bool FOURTH> __device__ __forceinline__ float adamw_code(float x, float s, float inverse)
+// made everywhere they took most of the kernel's time.  (A quotient below 2^-126 counts as 0: its code is 0 either way.)
+__device__ __forceinline__ float quick_root(float x) { float y; asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+template <bool FOURTH> __device__ __forceinline__ uint32_t adamw_code(float x, float s, float inverse)
 {
     const float most = FOURTH ? 255.0f : 127.0f;
-    float q = root_of(x * inverse);
-    if (FOURTH) q = root_of(q);
+    float q = quick_root(x * inverse);
+    if (FOURTH) q = quick_root(q);
     q *= most;
-    float c = rintf(q);
-    if (!(fabsf(q - c) < 0.4998f)) {
+    float c = q + 12582912.0f;                              // 1.5 * 2^23: rounds to a whole number, which is in the low bits
+    if (!(fabsf(q - (c - 12582912.0f)) < 0.4998f)) {
         q = __fsqrt_rn(__fdiv_rn(x, s));
         if (FOURTH) q = __fsqrt_rn(q);
-        c = rintf(__fmul_rn(q, most));
+        c = fminf(__fmul_rn(q, most), most) + 12582912.0f;  // (fminf: a number also from NaN)
     }
-    return c;
+    return __float_as_uint(c) & 0xffu;
 }
 
 // States in 8 bits: a warp takes the 256 values of a block, eight for each lane, side by side where every address allows it.
@@ -172,25 +177,29 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
         load8(g + lane * 8, x), load8(p + lane * 8, y);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            a[j] = (float)(int8_t)((j < 4 ? cm.x : cm.y) >> 8 * (j & 3));
-            b[j] = (float)(uint8_t)((j < 4 ? cv.x : cv.y) >> 8 * (j & 3));
+            a[j] = signed_byte_value(__byte_perm(j < 4 ? cm.x : cm.y, 0, 0x4440 + (j & 3)));
+            b[j] = byte_value(__byte_perm(j < 4 ? cv.x : cv.y, 0, 0x4440 + (j & 3)));
         }
     } else {
+        uint32_t cm[8], cv[8];
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const int i = at(j);
             const bool in = i < n;
-            a[j] = in ? (float)m[i] : 0.0f, b[j] = in ? (float)v[i] : 0.0f, x[j] = in ? to_float(g[i]) : 0.0f, y[j] = in ? to_float(p[i]) : 0.0f;
+            cm[j] = in ? ((const uint8_t *)m)[i] : 0, cv[j] = in ? v[i] : 0, x[j] = in ? to_float(g[i]) : 0.0f, y[j] = in ? to_float(p[i]) : 0.0f;
         }
+#pragma unroll
+        for (int j = 0; j < 8; j++) a[j] = signed_byte_value(cm[j]), b[j] = byte_value(cv[j]);
     }
-    float mt = 0.0f, vt = 0.0f;
+    uint32_t mt = 0, vt = 0;                                // (behind the tensor's end everything is 0)
 #pragma unroll
     for (int j = 0; j < 8; j++) {
         x[j] = __fmul_rn(x[j], scale);
+        if (!EIGHTS && at(j) >= n) x[j] = 0.0f;
         a[j] = adamw_first(adamw_read_m(a[j], ms), x[j], f);
         b[j] = adamw_second(adamw_read_v(b[j], vs), x[j], f);
         y[j] = adamw_value(y[j], a[j], b[j], f);
-        if (EIGHTS || at(j) < n) mt = larger(mt, fabsf(a[j])), vt = larger(vt, b[j]);
+        if (EIGHTS || at(j) < n) mt = max(mt, magnitude(a[j])), vt = max(vt, magnitude(b[j]));
     }
     if (EIGHTS) {
         store8(p + lane * 8, y);
@@ -203,25 +212,21 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
             if (i < n && copy) adamw_copy(copy, f.copy16, i, y[j]);
         }
     }
-#pragma unroll
-    for (int d = 16; d; d /= 2) {
-        mt = larger(mt, __shfl_xor_sync(~0u, mt, d));
-        vt = larger(vt, __shfl_xor_sync(~0u, vt, d));
-    }
-    if (lane == 0) t.ms[block] = mt, t.vs[block] = vt;
+    const float mtop = __uint_as_float(__reduce_max_sync(~0u, mt)), vtop = __uint_as_float(__reduce_max_sync(~0u, vt));
+    if (lane == 0) t.ms[block] = mtop, t.vs[block] = vtop;
     // (codes of a block whose scale is not finite are read as values that are not finite, whatever they are; where a scale is
-    // so small that its inverse overflows, or 0, the quick way gives no number and the operations are made)
-    const float md = mt > 0.0f ? mt : 1.0f, vd = vt > 0.0f ? vt : 1.0f, mr = __fdividef(1.0f, md), vr = __fdividef(1.0f, vd);
+    // so small that its inverse overflows the quick way gives no number and the operations are made)
+    const float md = mtop > 0.0f ? mtop : 1.0f, vd = vtop > 0.0f ? vtop : 1.0f, mr = __fdividef(1.0f, md), vr = __fdividef(1.0f, vd);
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-        const float q = adamw_code<false>(fabsf(a[j]), md, mr), u = adamw_code<true>(b[j], vd, vr);
-        const int8_t c = (int8_t)(int)copysignf(fminf(q, 127.0f), a[j]);
-        const uint8_t w = (uint8_t)(b[j] > 0.0f ? min(255, max(1, (int)u)) : 0);
+        uint32_t c = adamw_code<false>(fabsf(a[j]), md, mr), w = adamw_code<true>(b[j], vd, vr);
+        c = a[j] < 0.0f ? (0u - c) & 0xffu : c;
+        w = b[j] > 0.0f ? max(w, 1u) : 0;
         if (EIGHTS) {
-            cm[j / 4] |= (uint32_t)(uint8_t)c << 8 * (j & 3), cv[j / 4] |= (uint32_t)w << 8 * (j & 3);
+            cm[j / 4] |= c << 8 * (j & 3), cv[j / 4] |= w << 8 * (j & 3);
         } else if (at(j) < n) {
-            m[at(j)] = c, v[at(j)] = w;
+            ((uint8_t *)m)[at(j)] = (uint8_t)c, v[at(j)] = (uint8_t)w;
         }
     }
     if (EIGHTS) {
@@ -230,7 +235,7 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
     }
 }
 
-template <typename P, typename G, int N> __global__ void __launch_bounds__(256) adamw8_kernel(const __grid_constant__ AdamwList<N> list, AdamwFactors f, const float *grad_scale)
+template <typename P, typename G, int N> __global__ void __launch_bounds__(256, 4) adamw8_kernel(const __grid_constant__ AdamwList<N> list, AdamwFactors f, const float *grad_scale)
 {
     const int k = adamw_tensor(list, blockIdx.x);
     const AdamwTensor &t = list.t[k];
@@ -252,12 +257,21 @@ template <int N> __global__ void __launch_bounds__(256) adamw_values_kernel(cons
     const AdamwTensor &t = list.t[k];                           // (p: m's values, copy: v's values)
     const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
     const int n = (int)min((uint64_t)ADAMW_CHUNK, t.n - from);
-#pragma unroll 8
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const uint64_t at = from + i, block = at / ADAMW_BLOCK;
-        if (t.p) ((float *)t.p)[at] = adamw_read_m(((const int8_t *)t.m)[at], t.ms[block]);
-        if (t.copy) ((float *)t.copy)[at] = adamw_read_v(((const uint8_t *)t.v)[at], t.vs[block]);
-    }
+    // a warp's 32 values are of one block
+    auto read = [&](const uint8_t *codes, const float *scales, float *to, auto value) {
+        for (int i0 = threadIdx.x; i0 < n; i0 += 8 * 256) {
+            uint32_t c[8];
+            float s[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (i0 + 256 * j < n) c[j] = codes[from + i0 + 256 * j], s[j] = scales[(from + i0 + 256 * j) / ADAMW_BLOCK];
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (i0 + 256 * j < n) to[from + i0 + 256 * j] = value(c[j], s[j]);
+        }
+    };
+    if (t.p) read((const uint8_t *)t.m, t.ms, (float *)t.p, [](uint32_t c, float s) { return adamw_read_m(signed_byte_value(c), s); });
+    if (t.copy) read((const uint8_t *)t.v, t.vs, (float *)t.copy, [](uint32_t c, float s) { return adamw_read_v(byte_value(c), s); });
 }
 
 } // namespace hapop
