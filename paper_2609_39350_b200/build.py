@@ -12,7 +12,7 @@ HEADERS = [os.path.join(_DIR, "csrc", "hap_device.cuh"), os.path.join(_DIR, "csr
            os.path.join(_DIR, "csrc", "hap_tree_host.h"), os.path.join(_DIR, "csrc", "hap_joint.cuh"),
            os.path.join(os.path.dirname(_DIR), "include", "hap.h")]
 OPERATOR_HEADERS = [os.path.join(_DIR, "csrc", "hap_products.cuh"), os.path.join(_DIR, "csrc", "hap_products_tc.cuh"),
-                    os.path.join(_DIR, "csrc", "hap_products_experts.cuh"), os.path.join(_DIR, "csrc", "hap_adamw.cuh"),
+                    os.path.join(_DIR, "csrc", "hap_products_experts.cuh"), os.path.join(_DIR, "csrc", "hap_products_few.cuh"), os.path.join(_DIR, "csrc", "hap_adamw.cuh"),
                     os.path.join(os.path.dirname(_DIR), "include", "hap.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "--fmad=false", "-std=c++17",

@@ -1,6 +1,7 @@
 // Host side of the training operators: checks of arguments, choice of variant, launches.
 #include "hap_adamw.cuh"
 #include "hap_products_experts.cuh"
+#include "hap_products_few.cuh"
 #include "hap_products_tc.cuh"
 
 #include <atomic>
@@ -132,6 +133,13 @@ template <typename T, int FORM, int EPI> static hap_status launch_product(const 
     if (!d.sms) return HAP_E_CUDA;
     if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, d.sms, stream);
     if constexpr (FORM != TN && (EPI == STORE || EPI == GATED || EPI == GATED_BACK)) {
+        if constexpr (FORM == NT) {
+            if (p.rows <= FEW_ROWS) {
+                const int64_t warps = p.groups * (EPI == GATED ? (int64_t)p.ncols : ceil_div(p.ncols, 2)), blocks = ceil_div(warps, 8);
+                few_rows_kernel<T, EPI><<<(unsigned)(blocks < 4 * d.sms ? blocks : 4 * d.sms), 256, 0, stream>>>(p);
+                return launched();
+            }
+        }
         return launch_experts<T, FORM, EPI>(p, d, stream);
     } else {
         const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output

@@ -40,11 +40,33 @@ def _refuse(what: str):
     raise HapError(1, what)
 
 
-def _here(name, t, dtypes, dims):
+def _lib():
+    """The library with the operators' argument types set: plain numbers and addresses are passed."""
+    global _typed
+    if _typed is None:
+        L = load_library()
+        i, l, u, p = C.c_int32, C.c_int64, C.c_uint64, C.c_void_p
+        L.hap_expert_matmul.argtypes = [i] * 5 + [l, i, i, p, p, l, p, l, p, l, p]
+        L.hap_expert_gated.argtypes = [i, i, l, i, i, p, p, l, p, l, p, l, p, l, p]
+        L.hap_expert_gated_backward.argtypes = [i, i, l, i, i, p, p, l, p, l, p, l, p, l, p, l, p]
+        L.hap_linear_cross_entropy_workspace.argtypes = [l, i, l, p]
+        L.hap_linear_cross_entropy.argtypes = [i, l, i, l, p, l, p, l, p, l, p, p, p, u, p]
+        L.hap_linear_cross_entropy_backward.argtypes = [i, l, i, l, p, l, p, l, p, l, p, p, p, l, p, l, p, u, p]
+        L.hap_adamw_step.argtypes = [p, i, i, i, i, i, p, p, p]
+        L.hap_adamw_state.argtypes = [p, i, p, p, p]
+        L.hap_operator_status.argtypes = [p]
+        _typed = L
+    return _typed
+
+
+_typed = None
+
+
+def _here(name, t, here, dtypes, dims):
     """Checks what every tensor argument has to be."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name}: must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != here:
         _refuse(f"{name}: must live on the current CUDA device")
     if t.dtype not in dtypes:
         _refuse(f"{name}: {t.dtype} where one of {[str(d) for d in dtypes]} is needed")
@@ -52,33 +74,43 @@ def _here(name, t, dtypes, dims):
         _refuse(f"{name}: {t.dim()} dimensions where {dims} are needed")
 
 
-def _matrix(name, t, dtypes, rows=None, cols=None, batch=None):
-    """(address, distance of two rows) of a matrix, or of matrices that follow one another."""
-    _here(name, t, dtypes, 2 if batch is None else 3)
-    shape = tuple(t.shape)
-    want = ((batch,) if batch is not None else ()) + (rows, cols)
-    if any(w is not None and w != s for w, s in zip(want, shape)):
-        _refuse(f"{name}: shape {shape} where {want} is needed")
-    r, c = shape[-2:]
-    if c > 1 and t.stride(-1) != 1:
+def _matrix(name, t, here, dtypes, rows=None, cols=None):
+    """(address, distance of two rows) of a matrix."""
+    _here(name, t, here, dtypes, 2)
+    (r, c), (ld, one) = t.shape, t.stride()
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        _refuse(f"{name}: shape {tuple(t.shape)} where {(rows, cols)} is needed")
+    if one != 1 and c > 1:
         _refuse(f"{name}: elements of a row must lie side by side")
-    ld = t.stride(-2) if r > 1 else -(-c // 8) * 8 if batch is None or shape[0] < 2 else t.stride(0)
-    if ld < c or (batch is not None and shape[0] > 1 and t.stride(0) != r * ld):
+    if r < 2:
+        ld = (c + 7) & ~7
+    if ld < c:
+        _refuse(f"{name}: rows overlap")
+    return t.data_ptr(), ld
+
+
+def _matrices(name, t, here, dtypes, batch, rows=None, cols=None):
+    """The same of matrices that follow one another."""
+    _here(name, t, here, dtypes, 3)
+    (n, r, c), (far, ld, one) = t.shape, t.stride()
+    if n != batch or (rows is not None and r != rows) or (cols is not None and c != cols):
+        _refuse(f"{name}: shape {tuple(t.shape)} where {(batch, rows, cols)} is needed")
+    if one != 1 and c > 1:
+        _refuse(f"{name}: elements of a row must lie side by side")
+    if r < 2:
+        ld = (c + 7) & ~7 if n < 2 else far
+    if ld < c or (n > 1 and far != r * ld):
         _refuse(f"{name}: rows overlap, or matrices do not follow one another")
-    return C.c_void_p(t.data_ptr()), C.c_int64(ld)
+    return t.data_ptr(), ld
 
 
-def _vector(name, t, dtype, n=None):
-    _here(name, t, (dtype,), 1)
+def _vector(name, t, here, dtype, n=None):
+    _here(name, t, here, (dtype,), 1)
     if n is not None and t.numel() != n:
         _refuse(f"{name}: {t.numel()} elements where {n} are needed")
-    if t.numel() > 1 and t.stride(0) != 1:
+    if t.stride(0) != 1 and t.numel() > 1:
         _refuse(f"{name}: elements must lie side by side")
-    return C.c_void_p(t.data_ptr())
-
-
-def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return t.data_ptr()
 
 
 def _check(status, what):
@@ -86,8 +118,14 @@ def _check(status, what):
         raise HapError(status, what)
 
 
-def _offsets(offsets):
-    at = _vector("offsets", offsets, torch.int64)
+def _now():
+    """(current device, address of its current stream)"""
+    s = torch.cuda.current_stream()
+    return s.device_index, s.cuda_stream
+
+
+def _offsets(offsets, here):
+    at = _vector("offsets", offsets, here, torch.int64)
     if offsets.numel() < 2:
         _refuse("offsets: one more than there are experts are needed")
     return at, offsets.numel() - 1
@@ -102,7 +140,8 @@ def hap_expert_matmul(a, b, offsets, form=EXPERT_FORWARD, out=None, out_dtype=No
     EXPERT_GRAD_WEIGHT  a [rows][N], b [rows][K] -> out [E][N][K] = sum over the expert's rows of a^T b
 
     Rows of `out` outside of every expert's are left as they are (unset in an output made here)."""
-    at, E = _offsets(offsets)
+    here, stream = _now()
+    at, E = _offsets(offsets, here)
     if form not in (EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT):
         _refuse("form")
     if not isinstance(a, torch.Tensor) or not isinstance(b, torch.Tensor) or a.dim() != 2:
@@ -110,14 +149,14 @@ def hap_expert_matmul(a, b, offsets, form=EXPERT_FORWARD, out=None, out_dtype=No
     halves = (a.dtype,) if a.dtype in _HALVES else _HALVES
     rows = a.shape[0]
     if form == EXPERT_GRAD_WEIGHT:
-        pa, lda = _matrix("a", a, halves)
-        pb, ldb = _matrix("b", b, halves, rows=rows)
+        pa, lda = _matrix("a", a, here, halves)
+        pb, ldb = _matrix("b", b, here, halves, rows)
         N, K = a.shape[1], b.shape[1]
         shape = (E, N, K)
     else:
-        pb, ldb = _matrix("b", b, halves, batch=E)
+        pb, ldb = _matrices("b", b, here, halves, E)
         N, K = b.shape[1:]
-        pa, lda = _matrix("a", a, halves, cols=K if form == EXPERT_FORWARD else N)
+        pa, lda = _matrix("a", a, here, halves, None, K if form == EXPERT_FORWARD else N)
         shape = (rows, N if form == EXPERT_FORWARD else K)
     if out is None:
         if accumulate:
@@ -125,100 +164,104 @@ def hap_expert_matmul(a, b, offsets, form=EXPERT_FORWARD, out=None, out_dtype=No
         out = torch.empty(shape, dtype=out_dtype or a.dtype, device=a.device)
     elif out_dtype is not None and out.dtype != out_dtype:
         _refuse("out: is not of out_dtype")
-    po, ldo = _matrix("out", out, (a.dtype, torch.float32), *shape[-2:], batch=E if form == EXPERT_GRAD_WEIGHT else None)
-    _check(load_library().hap_expert_matmul(C.c_int32(form), C.c_int32(_TYPES[a.dtype]), C.c_int32(_TYPES[out.dtype]), C.c_int32(bool(accumulate)), C.c_int32(E),
-                                            C.c_int64(rows), C.c_int32(N), C.c_int32(K), at, pa, lda, pb, ldb, po, ldo, _stream()), "hap_expert_matmul")
+    kinds = (a.dtype, torch.float32)
+    po, ldo = _matrices("out", out, here, kinds, *shape) if form == EXPERT_GRAD_WEIGHT else _matrix("out", out, here, kinds, *shape)
+    _check(_lib().hap_expert_matmul(form, _TYPES[a.dtype], _TYPES[out.dtype], bool(accumulate), E, rows, N, K, at, pa, lda, pb, ldb, po, ldo, stream), "hap_expert_matmul")
     return out
 
 
 @_on_stream
 def hap_expert_gated(x, w, offsets, gu=None, h=None, keep=True):
     """(h, gu): [g | u] = x w_e^T with w [E][2F][H] and h = silu(g) u.  gu is None where keep is false."""
-    at, E = _offsets(offsets)
-    pw, ldw = _matrix("w", w, _HALVES, batch=E)
+    here, stream = _now()
+    at, E = _offsets(offsets, here)
+    pw, ldw = _matrices("w", w, here, _HALVES, E)
     F2, H = w.shape[1:]
     if F2 % 2:
         _refuse("w: the gate's rows and as many others are needed")
-    px, ldx = _matrix("x", x, (w.dtype,), cols=H)
+    kind = (w.dtype,)
+    px, ldx = _matrix("x", x, here, kind, None, H)
     rows, F = x.shape[0], F2 // 2
     if gu is None and keep:
         gu = torch.empty((rows, F2), dtype=x.dtype, device=x.device)
     if h is None:
         h = torch.empty((rows, F), dtype=x.dtype, device=x.device)
-    pg, ldg = _matrix("gu", gu, (w.dtype,), rows, F2) if gu is not None else (C.c_void_p(0), C.c_int64(0))
-    ph, ldh = _matrix("h", h, (w.dtype,), rows, F)
-    _check(load_library().hap_expert_gated(C.c_int32(_TYPES[w.dtype]), C.c_int32(E), C.c_int64(rows), C.c_int32(H), C.c_int32(F), at, px, ldx, pw, ldw, pg, ldg,
-                                           ph, ldh, _stream()), "hap_expert_gated")
+    pg, ldg = _matrix("gu", gu, here, kind, rows, F2) if gu is not None else (None, 0)
+    ph, ldh = _matrix("h", h, here, kind, rows, F)
+    _check(_lib().hap_expert_gated(_TYPES[w.dtype], E, rows, H, F, at, px, ldx, pw, ldw, pg, ldg, ph, ldh, stream), "hap_expert_gated")
     return h, gu
 
 
 @_on_stream
 def hap_expert_gated_backward(dy, w2, offsets, gu, dgu=None, h=None, want_h=True):
     """(dgu, h): dh = dy w2_e with w2 [E][H][F], the gradients of g and u from it and the kept gu, and h again.  dgu may be gu."""
-    at, E = _offsets(offsets)
-    pw, ldw = _matrix("w2", w2, _HALVES, batch=E)
+    here, stream = _now()
+    at, E = _offsets(offsets, here)
+    pw, ldw = _matrices("w2", w2, here, _HALVES, E)
     H, F = w2.shape[1:]
-    py, ldy = _matrix("dy", dy, (w2.dtype,), cols=H)
+    kind = (w2.dtype,)
+    py, ldy = _matrix("dy", dy, here, kind, None, H)
     rows = dy.shape[0]
-    pg, ldg = _matrix("gu", gu, (w2.dtype,), rows, 2 * F)
+    pg, ldg = _matrix("gu", gu, here, kind, rows, 2 * F)
     if dgu is None:
         dgu = torch.empty((rows, 2 * F), dtype=dy.dtype, device=dy.device)
     if h is None and want_h:
         h = torch.empty((rows, F), dtype=dy.dtype, device=dy.device)
-    pd, ldd = _matrix("dgu", dgu, (w2.dtype,), rows, 2 * F)
-    ph, ldh = _matrix("h", h, (w2.dtype,), rows, F) if h is not None else (C.c_void_p(0), C.c_int64(0))
-    _check(load_library().hap_expert_gated_backward(C.c_int32(_TYPES[w2.dtype]), C.c_int32(E), C.c_int64(rows), C.c_int32(H), C.c_int32(F), at, py, ldy, pw, ldw,
-                                                    pg, ldg, pd, ldd, ph, ldh, _stream()), "hap_expert_gated_backward")
+    pd, ldd = _matrix("dgu", dgu, here, kind, rows, 2 * F)
+    ph, ldh = _matrix("h", h, here, kind, rows, F) if h is not None else (None, 0)
+    _check(_lib().hap_expert_gated_backward(_TYPES[w2.dtype], E, rows, H, F, at, py, ldy, pw, ldw, pg, ldg, pd, ldd, ph, ldh, stream), "hap_expert_gated_backward")
     return dgu, h
 
 
 def hap_linear_cross_entropy_workspace(x, w):
     """A workspace for the forward and the backward pass of x [rows][H] and w [V][H]; needed during a call only."""
-    _matrix("x", x, _HALVES)
-    _matrix("w", w, (x.dtype,), cols=x.shape[1])
+    here = torch.cuda.current_device()
+    _matrix("x", x, here, _HALVES)
+    _matrix("w", w, here, (x.dtype,), None, x.shape[1])
     n = C.c_uint64()
-    _check(load_library().hap_linear_cross_entropy_workspace(C.c_int64(x.shape[0]), C.c_int32(x.shape[1]), C.c_int64(w.shape[0]), C.byref(n)), "hap_linear_cross_entropy_workspace")
+    _check(_lib().hap_linear_cross_entropy_workspace(x.shape[0], x.shape[1], w.shape[0], C.byref(n)), "hap_linear_cross_entropy_workspace")
     return torch.empty(max(256, n.value), dtype=torch.uint8, device=x.device)
 
 
-def _loss_args(x, w, target, workspace):
-    px, ldx = _matrix("x", x, _HALVES)
-    pw, ldw = _matrix("w", w, (x.dtype,), cols=x.shape[1])
-    pt = _vector("target", target, torch.int64, x.shape[0])
+def _loss_args(x, w, target, workspace, here):
+    px, ldx = _matrix("x", x, here, _HALVES)
+    pw, ldw = _matrix("w", w, here, (x.dtype,), None, x.shape[1])
+    pt = _vector("target", target, here, torch.int64, x.shape[0])
     if workspace is None:
         workspace = hap_linear_cross_entropy_workspace(x, w)
-    ps = _vector("workspace", workspace, torch.uint8)
-    head = (C.c_int32(_TYPES[x.dtype]), C.c_int64(x.shape[0]), C.c_int32(x.shape[1]), C.c_int64(w.shape[0]), px, ldx, pw, ldw, pt)
-    return head, ps, C.c_uint64(workspace.numel()), workspace
+    ps = _vector("workspace", workspace, here, torch.uint8)
+    return (_TYPES[x.dtype], x.shape[0], x.shape[1], w.shape[0], px, ldx, pw, ldw, pt), ps, workspace
 
 
 @_on_stream
 def hap_linear_cross_entropy(x, w, target, ignore_index=-100, loss=None, lse=None, workspace=None):
     """(loss, lse), fp32 [rows]: cross entropy of the logits x w^T against int64 targets, without keeping the logits."""
-    head, ps, n, workspace = _loss_args(x, w, target, workspace)
-    loss = torch.empty(x.shape[0], device=x.device) if loss is None else loss
-    lse = torch.empty(x.shape[0], device=x.device) if lse is None else lse
-    pl, pe = _vector("loss", loss, torch.float32, x.shape[0]), _vector("lse", lse, torch.float32, x.shape[0])
-    _check(load_library().hap_linear_cross_entropy(*head, C.c_int64(ignore_index), pl, pe, ps, n, _stream()), "hap_linear_cross_entropy")
+    here, stream = _now()
+    head, ps, workspace = _loss_args(x, w, target, workspace, here)
+    rows = x.shape[0]
+    loss = torch.empty(rows, device=x.device) if loss is None else loss
+    lse = torch.empty(rows, device=x.device) if lse is None else lse
+    pl, pe = _vector("loss", loss, here, torch.float32, rows), _vector("lse", lse, here, torch.float32, rows)
+    _check(_lib().hap_linear_cross_entropy(*head, ignore_index, pl, pe, ps, workspace.numel(), stream), "hap_linear_cross_entropy")
     return loss, lse
 
 
 @_on_stream
 def hap_linear_cross_entropy_backward(x, w, target, lse, grad, ignore_index=-100, dx=None, dw=None, want_dx=True, want_dw=True, workspace=None):
     """(dx, dw): gradients of grad * sum(loss); grad: fp32 scalar on the device."""
-    head, ps, n, workspace = _loss_args(x, w, target, workspace)
-    pe = _vector("lse", lse, torch.float32, x.shape[0])
+    here, stream = _now()
+    head, ps, workspace = _loss_args(x, w, target, workspace, here)
+    pe = _vector("lse", lse, here, torch.float32, x.shape[0])
     if not isinstance(grad, torch.Tensor) or grad.numel() != 1:
         _refuse("grad: one fp32 value on the device is needed")
-    pg = _vector("grad", grad.reshape(1), torch.float32)
-    none = C.c_void_p(0), C.c_int64(0)
+    pg = _vector("grad", grad.reshape(1), here, torch.float32)
     if dx is None and want_dx:
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if dw is None and want_dw:
         dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
-    pdx = _matrix("dx", dx, (x.dtype,), *x.shape) if dx is not None else none
-    pdw = _matrix("dw", dw, (x.dtype,), *w.shape) if dw is not None else none
-    _check(load_library().hap_linear_cross_entropy_backward(*head, C.c_int64(ignore_index), pe, pg, *pdx, *pdw, ps, n, _stream()), "hap_linear_cross_entropy_backward")
+    pdx = _matrix("dx", dx, here, (x.dtype,), *x.shape) if dx is not None else (None, 0)
+    pdw = _matrix("dw", dw, here, (x.dtype,), *w.shape) if dw is not None else (None, 0)
+    _check(_lib().hap_linear_cross_entropy_backward(*head, ignore_index, pe, pg, *pdx, *pdw, ps, workspace.numel(), stream), "hap_linear_cross_entropy_backward")
     return dx, dw
 
 
@@ -237,6 +280,7 @@ class HapAdamWTensors:
         self.bits = 32 if m_scale is None else 8
         self.kept = [params, *[x for _, x in lists if x is not None]]
         self.device = params[0].device
+        here = torch.cuda.current_device()
         types = dict(params=(torch.float32, *_HALVES), grads=(torch.float32, *_HALVES), copies=_HALVES,
                      m=(torch.float32,) if self.bits == 32 else (torch.int8,), v=(torch.float32,) if self.bits == 32 else (torch.uint8,),
                      m_scale=(torch.float32,), v_scale=(torch.float32,))
@@ -247,7 +291,7 @@ class HapAdamWTensors:
                 at[name] = [0] * n
                 continue
             for p, t in zip(params, tensors):
-                _here(name, t, types[name][:1] if len(types[name]) == 1 else (tensors[0].dtype,), t.dim() if isinstance(t, torch.Tensor) else 0)
+                _here(name, t, here, types[name][:1] if len(types[name]) == 1 else (tensors[0].dtype,), t.dim() if isinstance(t, torch.Tensor) else 0)
                 if t.dtype not in types[name]:
                     _refuse(f"{name}: {t.dtype}")
                 if not t.is_contiguous():
@@ -279,14 +323,14 @@ def hap_adamw_step(tensors: HapAdamWTensors, step, lr, beta1=0.9, beta2=0.999, e
     """One step over all tensors; step counts from 1.  grad_scale: fp32 scalar on the device (loss scaling, clipping)."""
     if tensors.device.index != torch.cuda.current_device():
         _refuse("tensors: must live on the current CUDA device")
-    pg = C.c_void_p(0)
+    here, stream = _now()
+    pg = None
     if grad_scale is not None:
         if not isinstance(grad_scale, torch.Tensor) or grad_scale.numel() != 1:
             _refuse("grad_scale: one fp32 value on the device is needed")
-        pg = _vector("grad_scale", grad_scale.reshape(1), torch.float32)
+        pg = _vector("grad_scale", grad_scale.reshape(1), here, torch.float32)
     options = _AdamWOptions(lr, beta1, beta2, eps, weight_decay, step)
-    _check(load_library().hap_adamw_step(tensors.array, C.c_int32(len(tensors.array)), *(C.c_int32(t) for t in tensors.types), C.c_int32(tensors.bits),
-                                         C.byref(options), pg, _stream()), "hap_adamw_step")
+    _check(_lib().hap_adamw_step(tensors.array, len(tensors.array), *tensors.types, tensors.bits, C.byref(options), pg, stream), "hap_adamw_step")
 
 
 @_on_stream
@@ -306,12 +350,12 @@ def hap_adamw_state(tensors: HapAdamWTensors, m=None, v=None):
             if t.numel() != d.count or t.dtype != torch.float32 or not t.is_contiguous() or t.device != tensors.device:
                 _refuse(f"{name}: contiguous fp32 tensors of the parameters' sizes are needed")
         got.append((values, (C.c_void_p * len(values))(*[t.data_ptr() for t in values])))
-    _check(load_library().hap_adamw_state(tensors.array, C.c_int32(len(tensors)), got[0][1], got[1][1], _stream()), "hap_adamw_state")
+    _check(_lib().hap_adamw_state(tensors.array, len(tensors), got[0][1], got[1][1], _now()[1]), "hap_adamw_state")
     return got[0][0], got[1][0]
 
 
 def hap_operator_status() -> int:
     """0, or the bits of waits that ran out in an operator's kernel since the last call (waits for the current device)."""
     bits = C.c_uint32()
-    _check(load_library().hap_operator_status(C.byref(bits)), "hap_operator_status")
+    _check(_lib().hap_operator_status(C.byref(bits)), "hap_operator_status")
     return int(bits.value)
