@@ -499,6 +499,24 @@ hap_status hap_adamw_step(const hap_adamw_tensor *tensors, int32_t n, int32_t pa
                           const float *dev_grad_scale, void *stream);
 hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *const *host_m, float *const *host_v, void *stream);
 
+/* Times of the operators on the current device, as profile entries of a device type (the paper's first step, profiling, for
+ * the device the library runs on).  Read from the model: S, H, E, k, F_dense, F_exp, V, beta (2: bf16); from the profile: the
+ * lists of TP, CP and micro-batch.  Measured, with CUDA events, the median of five runs after one that is not counted:
+ *   tff, tfb  [ntp][ncp][nmb][2] (HAP_DENSE, HAP_MOE): gated feed-forward block of width F_dense or F_exp / TP on b S / CP
+ *             tokens, forward and backward (0 where the width is 0)
+ *   tpost     [ntp][ncp][nmb]: the head's loss and its gradients on b S / CP tokens and V / TP columns
+ *   eta       Eq. 2's efficiency: the block's time scaled to the rows of a rank with 8 of the E experts (all, if fewer), each
+ *             with an equal share of k b S rows, over that rank's time; at most 1
+ *   gamma     what that rank's time grows by when its rows are doubled (rho = 2), 0 .. 1
+ *   copt      ns per parameter of an AdamW step, bf16 parameters and gradients with 32-bit states
+ * Attention, embedding, router and links are not measured.  Runs on `stream` and waits for it; refuses a stream that is being
+ * captured with HAP_E_STATE.  Workspace: hap_measure_workspace bytes of 256-byte aligned device memory (some GB for large
+ * models). */
+typedef struct { double *tff, *tfb, *tpost; double eta, gamma, copt; } hap_measured;
+hap_status hap_measure_workspace(const hap_model *, const hap_profile *, uint64_t *host_bytes);
+hap_status hap_measure_profile(const hap_model *, const hap_profile *, hap_measured *host_out, void *dev_workspace, uint64_t bytes,
+                               void *stream);
+
 /* Waits inside the operators' kernels are bounded; one that runs out ends its kernel early and sets a bit in a device word.
  * Waits for the current device, returns that word in *host_bits (0: none, results are whole) and clears it. */
 hap_status hap_operator_status(uint32_t *host_bits);

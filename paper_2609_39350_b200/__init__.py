@@ -13,4 +13,5 @@ from .binding import (HapError, HapProblem, hap_problem_create, hap_enumerate, h
                       OPT_HETERO_DISPATCH)
 from .operators import (EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, HapAdamWTensors, hap_expert_matmul,  # noqa: F401,E402
                         hap_expert_gated, hap_expert_gated_backward, hap_linear_cross_entropy_workspace, hap_linear_cross_entropy,
-                        hap_linear_cross_entropy_backward, hap_adamw_tensors, hap_adamw_step, hap_adamw_state, hap_operator_status)
+                        hap_linear_cross_entropy_backward, hap_adamw_tensors, hap_adamw_step, hap_adamw_state, hap_operator_status,
+                        hap_measure_workspace, hap_measure_profile)

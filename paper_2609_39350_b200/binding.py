@@ -22,7 +22,8 @@ EXPORTS = ["hap_problem_create", "hap_problem_destroy", "hap_enumerate", "hap_ge
            "hap_search_range", "hap_search_range_f64",
            "hap_search_best", "hap_argmin", "hap_argmin_static", "hap_joint_bottleneck", "hap_count_cells", "hap_get_timings", "hap_launches_per_pass", "hap_eval_appendix_b", "hap_simulate_1f1b", "hap_release_cached_memory", "hap_self_check", "hap_problem_save", "hap_problem_load", "hap_problem_dims", "hap_status_str", "hap_last_error",
            "hap_expert_matmul", "hap_expert_gated", "hap_expert_gated_backward", "hap_linear_cross_entropy_workspace",
-           "hap_linear_cross_entropy", "hap_linear_cross_entropy_backward", "hap_adamw_step", "hap_adamw_state", "hap_operator_status"]
+           "hap_linear_cross_entropy", "hap_linear_cross_entropy_backward", "hap_adamw_step", "hap_adamw_state", "hap_operator_status",
+           "hap_measure_workspace", "hap_measure_profile"]
 
 
 class HapError(RuntimeError):

@@ -7,7 +7,8 @@ import subprocess
 _DIR = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(_DIR, "libhap.so")
 LIB_CHECKED = os.path.join(_DIR, "libhap_checked.so")      # the same sources with -DHAP_CHECKED (self-checking kernels)
-SOURCES = [os.path.join(_DIR, "csrc", "hap_api.cu"), os.path.join(_DIR, "csrc", "hap_operators.cu")]
+SOURCES = [os.path.join(_DIR, "csrc", "hap_api.cu"), os.path.join(_DIR, "csrc", "hap_operators.cu"),
+           os.path.join(_DIR, "csrc", "hap_measure.cu")]
 HEADERS = [os.path.join(_DIR, "csrc", "hap_device.cuh"), os.path.join(_DIR, "csrc", "hap_tree.cuh"),
            os.path.join(_DIR, "csrc", "hap_tree_host.h"), os.path.join(_DIR, "csrc", "hap_joint.cuh"),
            os.path.join(os.path.dirname(_DIR), "include", "hap.h")]
@@ -38,7 +39,7 @@ def build_library(force: bool = False, verbose: bool = False, checked: bool = Fa
         nvcc = os.environ.get("NVCC", "nvcc")
         more = [*(["-DHAP_CHECKED"] if checked else []), *(["-Xptxas", "-v"] if verbose else [])]
         objects, running = [], []
-        for src, headers in zip(SOURCES, (HEADERS, OPERATOR_HEADERS)):
+        for src, headers in zip(SOURCES, (HEADERS, OPERATOR_HEADERS, OPERATOR_HEADERS[-1:])):
             obj = lib[:-len(".so")] + "_" + os.path.basename(src)[:-len(".cu")] + ".o"
             objects.append(obj)
             if force or _older(obj, [src, *headers]):

@@ -5,11 +5,14 @@ live on the current device; rows may be a distance apart (a slice of a wider mat
 """
 from __future__ import annotations
 
+import copy
 import ctypes as C
 import functools
 
+import numpy as np
 import torch
 
+from . import binding
 from .binding import HapError, load_library
 
 EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT = 0, 1, 2
@@ -359,3 +362,50 @@ def hap_operator_status() -> int:
     bits = C.c_uint32()
     _check(_lib().hap_operator_status(C.byref(bits)), "hap_operator_status")
     return int(bits.value)
+
+
+class _Measured(C.Structure):
+    _fields_ = [*[(n, C.c_void_p) for n in ("tff", "tfb", "tpost")], *[(n, C.c_double) for n in ("eta", "gamma", "copt")]]
+
+
+def _measured_parts(pb):
+    descriptors, keep = binding._descriptors(pb, 0, 0)
+    return C.byref(descriptors, binding._OFFSETS[0]), C.byref(descriptors, binding._OFFSETS[2]), (descriptors, keep)
+
+
+def hap_measure_workspace(pb) -> int:
+    """Bytes of device memory that hap_measure_profile needs for a problem."""
+    model, profile, keep = _measured_parts(pb)
+    n = C.c_uint64()
+    _check(_lib().hap_measure_workspace(model, profile, C.byref(n)), "hap_measure_workspace")
+    return int(n.value)
+
+
+@_on_stream
+def hap_measure_profile(pb, device_type, workspace=None):
+    """Times the training operators on the current device and returns (problem, measured): a copy of the problem whose entries of
+    one device type are these times, and what was measured as a dict.  Replaced: tff, tfb, tpost, eta and copt of the type; tdf
+    and tdb keep their difference to tff and tfb (attention and the rest of a layer, which are not measured).  gamma, which all
+    types share, is in the dict only."""
+    T = int(pb.P.shape[0])
+    if not 0 <= device_type < T:
+        _refuse(f"device_type: {device_type} of {T}")
+    if workspace is None:
+        workspace = torch.empty(hap_measure_workspace(pb), dtype=torch.uint8, device="cuda")
+    here, stream = _now()
+    ps = _vector("workspace", workspace, here, torch.uint8)
+    n = tuple(len(x) for x in (pb.tp_list, pb.cp_list, pb.mb_list))
+    tff, tfb, tpost = np.zeros((*n, 2)), np.zeros((*n, 2)), np.zeros(n)
+    out = _Measured(tff.ctypes.data, tfb.ctypes.data, tpost.ctypes.data)
+    model, profile, keep = _measured_parts(pb)
+    _check(_lib().hap_measure_profile(model, profile, C.byref(out), C.c_void_p(ps), C.c_uint64(workspace.numel()), C.c_void_p(stream)), "hap_measure_profile")
+    new = copy.copy(pb)
+    for name in ("tdf", "tdb", "tff", "tfb", "tpost", "eta", "copt"):
+        setattr(new, name, np.array(getattr(pb, name), dtype=np.float64))
+    kind = np.asarray(pb.kind)
+    for total, part, times in ((new.tdf, new.tff, tff), (new.tdb, new.tfb, tfb)):
+        measured = times[..., kind]                     # [ntp][ncp][nmb][N]
+        total[device_type] = np.maximum(total[device_type] - part[device_type], 0.0) + measured
+        part[device_type] = measured
+    new.tpost[device_type], new.eta[device_type], new.copt[device_type] = tpost, out.eta, out.copt
+    return new, dict(tff=tff, tfb=tfb, tpost=tpost, eta=out.eta, gamma=out.gamma, copt=out.copt)
