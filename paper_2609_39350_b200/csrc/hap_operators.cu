@@ -62,7 +62,7 @@ static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols
 static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
 
 // a persistent kernel of blocks or pairs of blocks, as many as fit and `most` tiles need
-template <auto KERNEL, int CG = 2, typename... A> static hap_status launch_pairs(int smem, int64_t most, Device d, cudaStream_t stream, const A &...args)
+template <auto KERNEL, int CG = 2, int THREADS = 320, typename... A> static hap_status launch_pairs(int smem, int64_t most, Device d, cudaStream_t stream, const A &...args)
 {
     static std::atomic<uint64_t> allowed;                   // devices on which the kernel may have this much shared memory
     const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
@@ -72,7 +72,7 @@ template <auto KERNEL, int CG = 2, typename... A> static hap_status launch_pairs
     }
     cudaLaunchConfig_t c{};
     const int64_t at_once = d.sms / CG;
-    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(320), c.dynamicSmemBytes = smem, c.stream = stream;
+    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(THREADS), c.dynamicSmemBytes = smem, c.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
     c.attrs = attr, c.numAttrs = CG > 1;
@@ -100,7 +100,7 @@ template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor
                                       CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     }
     constexpr int smem = 1024 + S::STAGES * S::STAGE + 8 * S::OUT + sizeof(Shared<EPI, CG>);
-    return launch_pairs<product_kernel<T, FORM, EPI, CG>, CG>(smem, most, d, stream, p, ma, mb, mo);
+    return launch_pairs<product_kernel<T, FORM, EPI, CG>, CG, FORM == TN ? 352 : 320>(smem, most, d, stream, p, ma, mb, mo);
 }
 
 // experts' rows as columns of the products (NT, NN; out in 16 bits)

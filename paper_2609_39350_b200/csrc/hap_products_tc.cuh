@@ -7,9 +7,10 @@
 // Operands along the contraction (K-major) lie as rows of 128 bytes, those across it (MN-major) as strips of 64 columns with
 // a row per step of the contraction; both under the 128-byte swizzle that the descriptors name.
 // Ragged ends: rows of other groups in a tile of NT, NN give rows of sums that are not stored; columns and steps outside of a
-// matrix arrive as zeros.  In TN the steps are rows, and those behind a group's last are another group's: the producer warp
-// overwrites them with zeros (in both operands: 0 times what lies there could be NaN) before it hands the stage on, after two
-// more stages are on their way: 2403 -> 1215 us for 8 weight gradients of 4096 x 14336 against loading such stages by threads.
+// matrix arrive as zeros.  In TN the steps are rows, and those behind a group's last are another group's: a warp of its own
+// overwrites them with zeros (in both operands: 0 times what lies there could be NaN) before the stage is handed on.  (8 weight
+// gradients of 4096 x 14336, 8192 rows: 2403 us with such stages loaded by the producer's threads, 1373 where the producer
+// cleared them, ENDUS with the warp.)
 #pragma once
 #include <cuda.h>
 #include "hap_products.cuh"
@@ -35,7 +36,7 @@ template <int EPI, int CG> struct Shape {
 
 template <int EPI, int CG> struct Shared {
     Schedule<Shape<EPI, CG>::BM> sched;
-    uint64_t full[8], empty[8], acc_full[2], acc_empty[2], end;
+    uint64_t full[8], empty[8], acc_full[2], acc_empty[2], end[8];
     uint32_t tmem;
     int stop;
 };
@@ -207,7 +208,7 @@ __device__ __forceinline__ void clear_rows(char *strips, int n, int valid, int l
 }
 
 template <typename T, int FORM, int EPI, int CG>
-__global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__ Args p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+__global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(const __grid_constant__ Args p, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                          const __grid_constant__ CUtensorMap map_out)
 {
     using S = Shape<EPI, CG>;
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
         if (lane == 0) {
             for (int i = 0; i < S::STAGES; i++) bar_init(&sh.full[i], CG), bar_init(&sh.empty[i], 1);
             for (int i = 0; i < 2; i++) bar_init(&sh.acc_full[i], 1), bar_init(&sh.acc_empty[i], 8 * CG);
-            bar_init(&sh.end, 1);
+            for (int i = 0; i < S::STAGES; i++) bar_init(&sh.end[i], 1);
             sh.stop = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async;" ::: "memory");
@@ -248,19 +249,7 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
 
     if (warp == 0) {
         uint32_t at = 0;                                    // stages brought so far
-        uint32_t ends = 0, end_at = 0;                      // TN: stages in which a group ended; where the last of them is
-        int end_rows = 0;                                   // and how many of its rows are the group's, until it is handed on
         bool good = true;
-        auto hand_on = [&] {
-            if (!(good = bar_wait(&sh.end, (ends - 1) & 1, stop))) return;
-            char *a = stages + end_at % S::STAGES * S::STAGE;
-            clear_rows(a, 2 + S::BROWS / 64, end_rows, lane);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            const uint32_t full = smem_u32(&sh.full[end_at % S::STAGES]);
-            if (lane == 0) bar_arrive_with_data_at(CG == 1 ? full : of_leader(full));
-            end_rows = 0;
-        };
         for (int t = 0; t < total && good; t++) {
             const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int m0 = tile.m * S::BM + rank * 128, n0 = tile.n * BN;
@@ -269,9 +258,8 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
                 const int s = at % S::STAGES;
                 if (!(good = bar_wait(&sh.empty[s], (at / S::STAGES + 1) & 1, stop))) break;
                 const bool ends_here = FORM == TN && K - k < BK;
-                if (FORM == TN && end_rows && (ends_here || at - end_at > 2)) hand_on();
                 char *a = stages + s * S::STAGE, *b = a + S::A_BYTES;
-                const uint32_t full = ends_here ? smem_u32(&sh.end) : CG == 1 ? smem_u32(&sh.full[s]) : of_leader(smem_u32(&sh.full[s]));
+                const uint32_t full = ends_here ? smem_u32(&sh.end[s]) : CG == 1 ? smem_u32(&sh.full[s]) : of_leader(smem_u32(&sh.full[s]));
                 if (elected()) {
                     bar_expect_at<CG>(full, S::STAGE);
                     const uint32_t da = smem_u32(a), db = smem_u32(b);
@@ -291,10 +279,8 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
                     }
                 }
                 __syncwarp();
-                if (ends_here) end_rows = K - k, end_at = at, ends++;
             }
         }
-        if (FORM == TN && good && end_rows) hand_on();
         if (*stop && rank == 0) drain(sh.full, at, S::STAGES);
     } else if (warp == 1) {
         if (rank == 0) {
@@ -332,6 +318,22 @@ __global__ void __launch_bounds__(320, 1) product_kernel(const __grid_constant__
                     }
                 }
             }
+        }
+    } else if (FORM == TN && warp == 10) {
+        uint32_t at = 0, phases = 0;
+        for (int t = 0; t < total; t++) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+            const int K = tile.hi - tile.lo, rest = K % BK;
+            at += (K + BK - 1) / BK;
+            if (!rest) continue;
+            const int s = (at - 1) % S::STAGES;
+            if (!bar_wait(&sh.end[s], phases >> s & 1, stop)) break;
+            phases ^= 1u << s;
+            clear_rows(stages + s * S::STAGE, 2 + S::BROWS / 64, rest, lane);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            const uint32_t full = smem_u32(&sh.full[s]);
+            if (lane == 0) bar_arrive_with_data_at(CG == 1 ? full : of_leader(full));
         }
     } else {
         uint32_t sums = 0;
