@@ -56,6 +56,10 @@ struct Args {
     float2 *part;                   // [pieces of PART_N columns][rows]
     float *at_target;               // [rows]
     const float *lse;
+    float *residual;                // DLOGIT, SUM32: [rows] what rounding took from the target's element
+    int64_t low;                    // DLOGIT: distance of what rounding took from all elements, or 0
+    const void *w;                  // SUM32: the whole weight
+    int64_t ldw;
     float *acc32;                   // SUM32: [rows][ncols]
     int first, last;
 };
@@ -266,7 +270,19 @@ template <typename T, int EPI> struct RowEpilogue {
                 d = col + i == target ? d - 1.0f : d;
                 v[i] = kept ? d * DLOGIT_SCALE : 0.0f;
             }
-            w.store((T *)p.out + row0 * p.ldo + col, p.ldo, v, n);
+            T *o = (T *)p.out + row0 * p.ldo + col;
+            w.store(o, p.ldo, v, n);
+            const bool here = live && kept && target >= col && target < col + 32 && target < p.ncols;
+            if (p.low || __any_sync(~0u, here)) {
+                float r = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 32; i++) {
+                    v[i] -= to_float(from_float<T>(v[i]));
+                    r = col + i == target ? v[i] : r;
+                }
+                if (here) p.residual[row0 + w.lane] = r;
+                if (p.low) w.store(o + p.low, p.ldo, v, n);
+            }
         }
         if constexpr (EPI == SUM32) {
             float *a = p.acc32 + (row0 + w.lane) * (int64_t)p.ncols + col;
@@ -276,7 +292,15 @@ template <typename T, int EPI> struct RowEpilogue {
                 for (int i = 0; i < 32; i++) v[i] += v2[i];
             }
             if (p.last) {
+                // the target's element is most of a row, and its rounding would be most of the error: what it took comes back
                 const float f = *p.scale * p.scale_by;
+                const int64_t t = live ? p.target[row0 + w.lane] : p.ignore;
+                if (t != p.ignore && t >= 0 && t < p.vocab) {
+                    const float r = p.residual[row0 + w.lane];
+                    load32((const T *)p.w + t * p.ldw + col, v2, n);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) v[i] = fmaf(r, v2[i], v[i]);
+                }
 #pragma unroll
                 for (int i = 0; i < 32; i++) v[i] *= f;
                 w.store((T *)p.out + row0 * p.ldo + col, p.ldo, v, n);
