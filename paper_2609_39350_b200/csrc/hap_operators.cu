@@ -82,7 +82,7 @@ template <auto KERNEL, int CG = 2, int THREADS = 320, typename... A> static hap_
 template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(Args p, Device d, cudaStream_t stream)
 {
     using S = Shape<EPI, CG>;
-    const int64_t cols = ceil_div(p.ncols, TILE_N);
+    const int64_t cols = ceil_div(p.ncols, TILE_N) * (EPI == SUM32 ? p.splits : 1);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, S::BM) : ceil_div(p.rows, S::BM) + (p.offsets ? p.groups : 0));
     if (most > INT32_MAX) return HAP_E_RANGE;
     constexpr bool fp16 = TypeBits<T>::value == 0;
@@ -226,6 +226,14 @@ static uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
 // is 1.0 to 1.4 times that of rounding the result alone.)
 constexpr int64_t TWICE_ROWS = 128;
 
+// dx of few rows is few tiles with the longest contraction there is, the vocabulary: it is split so that each of the device's 74
+// pairs of blocks has a tile, into parts of at least 1024 (8 rows, 1024 x 100000: SPLITUS us, SPLITWAS without)
+static int parts_of_dx(int64_t rows, int64_t H, int64_t piece)
+{
+    const int64_t tiles = ceil_div(rows < 1 ? 1 : rows, 2 * 128) * ceil_div(H, TILE_N), fit = 74 / tiles, most = ceil_div(piece, 1024);
+    return (int)(fit < 2 ? 1 : fit < most ? fit : most);
+}
+
 // where the parts of the backward pass's workspace begin
 struct LossSpace { uint64_t residual, acc, x2, bytes; };
 static LossSpace loss_space(int64_t rows, int64_t H, int64_t V)
@@ -234,7 +242,8 @@ static LossSpace loss_space(int64_t rows, int64_t H, int64_t V)
     LossSpace s;
     s.residual = up256(halves * n * piece * 2);
     s.acc = s.residual + up256(n * 4);
-    s.x2 = s.acc + ((int64_t)piece < V ? up256(n * H * 4) : 0);
+    const uint64_t parts = (uint64_t)parts_of_dx(rows, H, (int64_t)piece);
+    s.x2 = s.acc + ((int64_t)piece < V || parts > 1 ? up256(parts * n * H * 4) : 0);
     s.bytes = s.x2 + (halves > 1 ? up256(2 * n * ((H + 7) / 8 * 8) * 2) : 0);
     return s;
 }
@@ -294,6 +303,10 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
     char *d = (char *)workspace, *x2 = d + at.x2;
     float *acc = (float *)(d + at.acc), *residual = (float *)(d + at.residual);
     const bool twice = rows <= TWICE_ROWS && rows > 0 && dw;
+    // parts of dx's contraction, of the same length in every piece, so that none is empty and those of a later, shorter piece are
+    // among the first one's (the plain kernel makes one sum)
+    const int64_t whole = V < piece ? V : piece, split_k = ceil_div(ceil_div(whole, mappable(w, ldw) ? parts_of_dx(rows, H, piece) : 1), BK) * BK;
+    const int parts = (int)ceil_div(whole, split_k);
     if (twice)
         for (int i = 0; i < 2; i++)
             if (cudaMemcpy2DAsync(x2 + i * rows * H8 * 2, H8 * 2, x, ldx * 2, (size_t)H * 2, (size_t)rows, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
@@ -313,10 +326,20 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
             Args p{};
             p.groups = 1, p.rows = (int)rows, p.ncols = H, p.kdim = (int)cols;
             p.a = d, p.b = wc, p.lda = piece, p.ldb = ldw;
-            p.out = dx, p.ldo = lddx, p.acc32 = acc, p.first = c0 == 0, p.last = c0 + cols == V;
+            const bool last = c0 + cols == V;
+            p.splits = (int)ceil_div(cols, split_k), p.split_k = (int)split_k;
+            p.out = dx, p.ldo = lddx, p.acc32 = acc, p.first = c0 == 0, p.last = last && parts == 1;
             p.scale = grad, p.scale_by = 1.0f / DLOGIT_SCALE;
             p.target = target, p.ignore = ignore, p.vocab = V, p.residual = residual, p.w = w, p.ldw = ldw;
             st = HAP_BY_TYPE(NN, SUM32);
+            if (st == HAP_OK && last && parts > 1) {
+                p.splits = parts;
+                const int64_t blocks = ceil_div(rows * H, 256);
+                const unsigned grid = (unsigned)(blocks < 8 * 148 ? blocks : 8 * 148);
+                if (dtype == HAP_BF16) join_parts_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(p);
+                else join_parts_kernel<__half><<<grid, 256, 0, s>>>(p);
+                st = launched();
+            }
         }
         if (st == HAP_OK && dw) {
             Args p{};

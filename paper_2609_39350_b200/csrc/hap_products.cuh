@@ -62,6 +62,7 @@ struct Args {
     int64_t ldw;
     float *acc32;                   // SUM32: [rows][ncols]
     int first, last;
+    int splits, split_k;            // SUM32: the contraction in this many parts of split_k, each with sums of its own in acc32
 };
 
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -164,7 +165,7 @@ struct WarpRows {
 };
 
 // What happens to the 32 columns col .. of 32 output rows, one for each lane of a warp, from `row0` on (in TN rows of out_e, and
-// then e is its group).  v: the sums; v2: those of u in GATED.  The softmax statistics of a row over a tile are held in m
+// then e is its group; in SUM32 the part of the contraction).  v: the sums; v2: those of u in GATED.  The softmax statistics of a row over a tile are held in m
 // (maximum) and s.  All lanes call, those of rows that do not exist too.
 template <typename T, int EPI> struct RowEpilogue {
     const Args &p;
@@ -285,7 +286,7 @@ template <typename T, int EPI> struct RowEpilogue {
             }
         }
         if constexpr (EPI == SUM32) {
-            float *a = p.acc32 + (row0 + w.lane) * (int64_t)p.ncols + col;
+            float *a = p.acc32 + (e * (int64_t)p.rows + row0 + w.lane) * p.ncols + col;         // e: the part
             if (!p.first) {
                 load32(a, v2, live ? n : 0);
 #pragma unroll
@@ -520,6 +521,21 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int 
     lse[row] = l;
     const int64_t t = target[row];
     loss[row] = t == ignore ? 0.0f : t < 0 || t >= V ? NAN : l - at_target[row];
+}
+
+// dx of few rows from the parts of the contraction: their sum in order, what rounding took from the target's element, the scale.
+template <typename T> __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ Args p)
+{
+    const int64_t n = (int64_t)p.rows * p.ncols;
+    const float f = *p.scale * p.scale_by;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        const int64_t row = i / p.ncols, col = i - row * p.ncols, t = p.target[row];
+        float x = 0.0f;
+#pragma unroll 8
+        for (int s = 0; s < p.splits; s++) x += p.acc32[s * n + i];
+        if (t != p.ignore && t >= 0 && t < p.vocab) x = fmaf(p.residual[row], to_float(((const T *)p.w)[t * p.ldw + col]), x);
+        ((T *)p.out)[row * p.ldo + col] = from_float<T>(x * f);
+    }
 }
 
 } // namespace hapop

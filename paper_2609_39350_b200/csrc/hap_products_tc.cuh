@@ -219,7 +219,8 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
     constexpr int BN = TILE_N;
-    const int col_tiles = (p.ncols + BN - 1) / BN;
+    // the parts of a split contraction are so many more columns of tiles
+    const int part_tiles = (p.ncols + BN - 1) / BN, col_tiles = EPI == SUM32 ? part_tiles * p.splits : part_tiles;
 
     sh.sched.fetch(p);
     if (threadIdx.x == 0) prefetch_map(&map_a), prefetch_map(&map_b);
@@ -252,9 +253,10 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
         bool good = true;
         for (int t = 0; t < total && good; t++) {
             const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
-            const int m0 = tile.m * S::BM + rank * 128, n0 = tile.n * BN;
-            const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
-            for (int k = 0; k < K && good; k += BK, at++) {
+            const int part = EPI == SUM32 ? tile.n / part_tiles : 0;
+            const int m0 = tile.m * S::BM + rank * 128, n0 = (tile.n - part * part_tiles) * BN;
+            const int K = FORM == TN ? tile.hi - tile.lo : EPI == SUM32 ? min(p.kdim, (part + 1) * p.split_k) : p.kdim;
+            for (int k = EPI == SUM32 ? part * p.split_k : 0; k < K && good; k += BK, at++) {
                 const int s = at % S::STAGES;
                 if (!(good = bar_wait(&sh.empty[s], (at / S::STAGES + 1) & 1, stop))) break;
                 const bool ends_here = FORM == TN && K - k < BK;
@@ -289,6 +291,10 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
             bool good = true;
             for (int t = 0; t < total && good; t++) {
                 int K = p.kdim;
+                if (EPI == SUM32) {
+                    const int part = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers).n / part_tiles;
+                    K = min(p.kdim - part * p.split_k, p.split_k);
+                }
                 if (FORM == TN) {
                     const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
                     K = tile.hi - tile.lo;
@@ -344,11 +350,12 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
         const uint32_t from = tmem + ((uint32_t)quarter << 21) + half * CHUNKS * 32;
         for (int t = 0; t < total; t++) {
             const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
-            const int m = tile.m * S::BM + rank * 128 + quarter * 32, n0 = tile.n * BN + half * CHUNKS * 32;
+            const int part = EPI == SUM32 ? tile.n / part_tiles : 0;
+            const int m = tile.m * S::BM + rank * 128 + quarter * 32, n0 = (tile.n - part * part_tiles) * BN + half * CHUNKS * 32;
             const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
             if (FORM == TN && !K && p.accumulate) continue;
             const int live = (FORM == TN ? p.mdim : tile.hi - tile.lo) - m;
-            RowEpilogue<T, EPI> row(p, WarpRows{staged, lane, min(max(live, 0), 32)}, (FORM == TN ? 0 : (int64_t)tile.lo) + m, FORM == TN ? tile.e : 0);
+            RowEpilogue<T, EPI> row(p, WarpRows{staged, lane, min(max(live, 0), 32)}, (FORM == TN ? 0 : (int64_t)tile.lo) + m, FORM == TN ? tile.e : part);
             // the set's sums are out of tensor memory: the next may be summed there
             auto taken = [&](int set) {
                 fence_before();

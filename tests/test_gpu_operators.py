@@ -209,7 +209,7 @@ def loss_reference(x, w, target, grad, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
-@pytest.mark.parametrize("rows,H,V", [(1, 8, 1), (1, 64, 1000), (3, 128, 257), (129, 72, 511), (128, 64, 256), (200, 264, 3001), (5, 33, 77), (300, 64, 8200)])
+@pytest.mark.parametrize("rows,H,V", [(1, 8, 1), (1, 64, 1000), (3, 128, 257), (129, 72, 511), (128, 64, 256), (200, 264, 3001), (5, 33, 77), (300, 64, 8200), (4, 264, 76033), (260, 320, 9001)])
 def test_linear_cross_entropy(rows, H, V, dtype):
     x, w = normal(rows, H, dtype=dtype), normal(V, H, seed=1, dtype=dtype, scale=2.0 * H ** -0.5)
     target = torch.randint(0, V, (rows,), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")
