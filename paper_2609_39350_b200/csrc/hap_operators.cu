@@ -61,6 +61,19 @@ static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols
 // whether TMA can address an operand
 static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
 
+// Launches a kernel that may start while its predecessor in the stream still ends: its setup (barriers, tensor memory, maps) and the
+// launch itself then cost nothing (loss of 129 rows: PDLWAS -> PDLUS us).  The kernel waits for the predecessor before it reads.
+template <typename... P, typename... A> static hap_status launch_next(void (*kernel)(P...), int64_t grid, int threads, int smem, int cluster, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)grid), c.blockDim = dim3((unsigned)threads), c.dynamicSmemBytes = (size_t)smem, c.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization, attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension, attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    c.attrs = attr, c.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&c, kernel, (P)args...) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+}
+
 // a persistent kernel of blocks or pairs of blocks, as many as fit and `most` tiles need
 template <auto KERNEL, int CG = 2, int THREADS = 320, typename... A> static hap_status launch_pairs(int smem, int64_t most, Device d, cudaStream_t stream, const A &...args)
 {
@@ -70,13 +83,8 @@ template <auto KERNEL, int CG = 2, int THREADS = 320, typename... A> static hap_
         if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    cudaLaunchConfig_t c{};
     const int64_t at_once = d.sms / CG;
-    c.gridDim = dim3((unsigned)((most < at_once ? most : at_once) * CG)), c.blockDim = dim3(THREADS), c.dynamicSmemBytes = smem, c.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension, attr[0].val.clusterDim = {CG, 1, 1};
-    c.attrs = attr, c.numAttrs = CG > 1;
-    return cudaLaunchKernelEx(&c, KERNEL, args...) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+    return launch_next(KERNEL, (most < at_once ? most : at_once) * CG, THREADS, smem, CG, stream, args...);
 }
 
 template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor(Args p, Device d, cudaStream_t stream)
@@ -136,8 +144,7 @@ template <typename T, int FORM, int EPI> static hap_status launch_product(const 
         if constexpr (FORM == NT) {
             if (p.rows <= FEW_ROWS) {
                 const int64_t warps = p.groups * (EPI == GATED ? (int64_t)p.ncols : ceil_div(p.ncols, 2)), blocks = ceil_div(warps, 8);
-                few_rows_kernel<T, EPI><<<(unsigned)(blocks < 4 * d.sms ? blocks : 4 * d.sms), 256, 0, stream>>>(p);
-                return launched();
+                return launch_next(few_rows_kernel<T, EPI>, blocks < 4 * d.sms ? blocks : 4 * d.sms, 256, 0, 1, stream, p);
             }
         }
         return launch_experts<T, FORM, EPI>(p, d, stream);
@@ -285,8 +292,7 @@ extern "C" hap_status hap_linear_cross_entropy(int32_t dtype, int64_t rows, int3
     cudaStream_t s = (cudaStream_t)stream;
     const hap_status st = HAP_BY_TYPE(NT, LSE);
     if (st != HAP_OK) return st;
-    loss_rows_kernel<<<(unsigned)ceil_div(rows, 8), 256, 0, s>>>(p.part, pieces, (int)rows, p.at_target, target, ignore, (int)V, loss, lse);
-    return launched();
+    return launch_next(loss_rows_kernel, ceil_div(rows, 8), 256, 0, 1, s, (const float2 *)p.part, pieces, (int)rows, (const float *)p.at_target, target, ignore, (int)V, loss, lse);
 }
 
 extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t rows, int32_t H, int64_t V, const void *x, int64_t ldx, const void *w,
@@ -335,10 +341,8 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
             if (st == HAP_OK && last && parts > 1) {
                 p.splits = parts;
                 const int64_t blocks = ceil_div(rows * H, 256);
-                const unsigned grid = (unsigned)(blocks < 8 * 148 ? blocks : 8 * 148);
-                if (dtype == HAP_BF16) join_parts_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(p);
-                else join_parts_kernel<__half><<<grid, 256, 0, s>>>(p);
-                st = launched();
+                const int64_t grid = blocks < 8 * 148 ? blocks : 8 * 148;
+                st = dtype == HAP_BF16 ? launch_next(join_parts_kernel<__nv_bfloat16>, grid, 256, 0, 1, s, p) : launch_next(join_parts_kernel<__half>, grid, 256, 0, 1, s, p);
             }
         }
         if (st == HAP_OK && dw) {

@@ -68,6 +68,11 @@ struct Args {
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
+// A kernel that was launched with its predecessor's end still ahead (see launch_next) starts by letting its successor do the same,
+// and touches no memory that others write before the predecessor's work is whole.
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
@@ -494,6 +499,8 @@ template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) 
 __global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int pieces, int rows, const float *at_target, const int64_t *target,
                                                         int64_t ignore, int V, float *loss, float *lse)
 {
+    launch_next();
+    wait_for_last();
     __shared__ float2 sh[32][8];
     const int r = threadIdx.x & 7, slice = threadIdx.x >> 3, row = blockIdx.x * 8 + r;
     float m = -INFINITY, s = 0.0f;
@@ -526,6 +533,8 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const float2 *part, int 
 // dx of few rows from the parts of the contraction: their sum in order, what rounding took from the target's element, the scale.
 template <typename T> __global__ void __launch_bounds__(256) join_parts_kernel(const __grid_constant__ Args p)
 {
+    launch_next();
+    wait_for_last();
     const int64_t n = (int64_t)p.rows * p.ncols;
     const float f = *p.scale * p.scale_by;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
     constexpr int BN = 256;                                 // columns of out that a tile covers
     const int col_tiles = (p.ncols + BN - 1) / BN;
 
-    sh.sched.fetch(p);
+    launch_next();
     if (threadIdx.x == 0) prefetch_map(&map_w), prefetch_map(&map_rows);
     if (warp == 1) {
         if (lane == 0) {
@@ -122,6 +122,8 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
         __syncwarp();
         tmem_alloc<2>(&sh.tmem);
     }
+    wait_for_last();
+    sh.sched.fetch(p);
     __syncthreads();
     if (warp == 0) sh.sched.build(p, FORM, col_tiles, S::FEW, lane);
     fence_before();

@@ -25,6 +25,8 @@ template <typename T, int EPI> __global__ void __launch_bounds__(256) few_rows_k
 {
     __shared__ int expert[FEW_ROWS], low[FEW_ROWS], high[FEW_ROWS], experts;
     __shared__ int bound[MAX_GROUPS + 1];
+    launch_next();
+    wait_for_last();
     for (int i = threadIdx.x; i <= p.groups; i += 256) {
         const int64_t o = p.offsets[i];
         bound[i] = o < 0 ? 0 : o > p.rows ? p.rows : (int)o;

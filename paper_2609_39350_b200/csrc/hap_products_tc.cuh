@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
     // the parts of a split contraction are so many more columns of tiles
     const int part_tiles = (p.ncols + BN - 1) / BN, col_tiles = EPI == SUM32 ? part_tiles * p.splits : part_tiles;
 
-    sh.sched.fetch(p);
+    launch_next();
     if (threadIdx.x == 0) prefetch_map(&map_a), prefetch_map(&map_b);
     if (warp == 1) {
         if (lane == 0) {
@@ -236,6 +236,8 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
         __syncwarp();
         tmem_alloc<CG>(&sh.tmem);
     }
+    wait_for_last();
+    sh.sched.fetch(p);
     __syncthreads();
     if (warp == 0) sh.sched.build(p, FORM, col_tiles, FORM == TN ? S::FEW : 0, lane);
     fence_before();
