@@ -181,9 +181,11 @@ template <typename T, int EPI> struct RowEpilogue {
     float m = -INFINITY, s = 0.0f;
     int64_t target = -1;            // LSE, DLOGIT: column of the row's target in this launch's columns, or outside of them
     bool kept = true;
-    float lse = 0.0f;
+    float lse = 0.0f, scale = 1.0f;
     __device__ __forceinline__ RowEpilogue(const Args &args, const WarpRows &w, int64_t row0, int e) : p(args), w(w), row0(row0), e(e), live(w.lane < w.live)
     {
+        if constexpr (EPI == STORE || EPI == SUM32)
+            if (p.scale) scale = *p.scale * p.scale_by;
         if constexpr (EPI == LSE || EPI == DLOGIT) {
             if (live) {
                 const int64_t t = p.target[row0 + w.lane];
@@ -198,11 +200,8 @@ template <typename T, int EPI> struct RowEpilogue {
         const int n = p.ncols - col;
         if (n <= 0) return;
         if constexpr (EPI == STORE) {
-            if (p.scale) {
-                const float f = *p.scale * p.scale_by;
 #pragma unroll
-                for (int i = 0; i < 32; i++) v[i] *= f;
-            }
+            for (int i = 0; i < 32; i++) v[i] *= scale;
             T *o = (T *)p.out + e * p.ogroup + row0 * p.ldo + col;
             if (p.accumulate) {
                 load32(o + w.lane * p.ldo, v2, live ? n : 0);
@@ -299,7 +298,6 @@ template <typename T, int EPI> struct RowEpilogue {
             }
             if (p.last) {
                 // the target's element is most of a row, and its rounding would be most of the error: what it took comes back
-                const float f = *p.scale * p.scale_by;
                 const int64_t t = live ? p.target[row0 + w.lane] : p.ignore;
                 if (t != p.ignore && t >= 0 && t < p.vocab) {
                     const float r = p.residual[row0 + w.lane];
@@ -308,7 +306,7 @@ template <typename T, int EPI> struct RowEpilogue {
                     for (int i = 0; i < 32; i++) v[i] = fmaf(r, v2[i], v[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < 32; i++) v[i] *= f;
+                for (int i = 0; i < 32; i++) v[i] *= scale;
                 w.store((T *)p.out + row0 * p.ldo + col, p.ldo, v, n);
             } else if (live) {
                 store32(a, v, n);

@@ -201,10 +201,8 @@ template <typename T, int FORM, int CG> struct Instruction {
 // Rows valid .. 63 of a stage's strips become zeros, by a warp.
 __device__ __forceinline__ void clear_rows(char *strips, int n, int valid, int lane)
 {
-    for (int i = lane; i < n * (BK - valid) * 8; i += 32) {
-        const int s = i / ((BK - valid) * 8), at = i - s * (BK - valid) * 8;
-        *(uint4 *)(strips + s * BK * 128 + valid * 128 + at * 16) = make_uint4(0, 0, 0, 0);
-    }
+    for (int s = 0; s < n; s++)
+        for (int r = valid + (lane >> 3); r < BK; r += 4) *(uint4 *)(strips + s * BK * 128 + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
 }
 
 template <typename T, int FORM, int EPI, int CG>
@@ -261,7 +259,7 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
             for (int k = EPI == SUM32 ? part * p.split_k : 0; k < K && good; k += BK, at++) {
                 const int s = at % S::STAGES;
                 if (!(good = bar_wait(&sh.empty[s], (at / S::STAGES + 1) & 1, stop))) break;
-                const bool ends_here = FORM == TN && K - k < BK;
+                const bool ends_here = FORM == TN && K - k < BK && tile.hi < p.rows;     // (behind the last row of all zeros arrive)
                 char *a = stages + s * S::STAGE, *b = a + S::A_BYTES;
                 const uint32_t full = ends_here ? smem_u32(&sh.end[s]) : CG == 1 ? smem_u32(&sh.full[s]) : of_leader(smem_u32(&sh.full[s]));
                 if (elected()) {
@@ -310,7 +308,7 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
                     for (int k = k0; k < end; k += BK, at++) {
                         const int s = at % S::STAGES;
                         if (!(good = bar_wait(&sh.full[s], (at / S::STAGES) & 1, stop))) break;
-                        if (CG == 2 && FORM == TN && K - k < BK) acquire_cluster();
+                        if (CG == 2 && FORM == TN && K - k < BK) acquire_cluster();      // (rows cleared by threads)
                         fence_after();
                         if (elected()) {
                             const uint32_t a = smem_u32(stages + s * S::STAGE), b = a + S::A_BYTES;
@@ -333,7 +331,7 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
             const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
             const int K = tile.hi - tile.lo, rest = K % BK;
             at += (K + BK - 1) / BK;
-            if (!rest) continue;
+            if (!rest || tile.hi >= p.rows) continue;
             const int s = (at - 1) % S::STAGES;
             if (!bar_wait(&sh.end[s], phases >> s & 1, stop)) break;
             phases ^= 1u << s;
