@@ -159,8 +159,9 @@ template <bool FOURTH> __device__ __forceinline__ uint32_t adamw_code(float x, f
     return __float_as_uint(c) & 0xffu;
 }
 
-// States in 8 bits: a warp takes the 256 values of a block, eight for each lane, side by side where every address allows it.
-template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void adamw8_block(const AdamwTensor &t, uint64_t from, const AdamwFactors &f, float scale, int lane)
+// States in 8 bits: a warp takes the 256 values of a block (WHOLE: it has so many), eight for each lane, side by side where every
+// address allows it (EIGHTS).
+template <typename P, typename G, bool EIGHTS, bool WHOLE> __device__ __forceinline__ void adamw8_block(const AdamwTensor &t, uint64_t from, const AdamwFactors &f, float scale, int lane)
 {
     const uint64_t block = from / ADAMW_BLOCK;
     const int n = (int)min((uint64_t)ADAMW_BLOCK, t.n - from);
@@ -185,7 +186,7 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const int i = at(j);
-            const bool in = i < n;
+            const bool in = WHOLE || i < n;
             cm[j] = in ? ((const uint8_t *)m)[i] : 0, cv[j] = in ? v[i] : 0, x[j] = in ? to_float(g[i]) : 0.0f, y[j] = in ? to_float(p[i]) : 0.0f;
         }
 #pragma unroll
@@ -195,11 +196,11 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
 #pragma unroll
     for (int j = 0; j < 8; j++) {
         x[j] = __fmul_rn(x[j], scale);
-        if (!EIGHTS && at(j) >= n) x[j] = 0.0f;
+        if (!WHOLE && at(j) >= n) x[j] = 0.0f;
         a[j] = adamw_first(adamw_read_m(a[j], ms), x[j], f);
         b[j] = adamw_second(adamw_read_v(b[j], vs), x[j], f);
         y[j] = adamw_value(y[j], a[j], b[j], f);
-        if (EIGHTS || at(j) < n) mt = max(mt, magnitude(a[j])), vt = max(vt, magnitude(b[j]));
+        if (WHOLE || at(j) < n) mt = max(mt, magnitude(a[j])), vt = max(vt, magnitude(b[j]));
     }
     if (EIGHTS) {
         store8(p + lane * 8, y);
@@ -208,8 +209,8 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const int i = at(j);
-            if (i < n) p[i] = from_float<P>(y[j]);
-            if (i < n && copy) adamw_copy(copy, f.copy16, i, y[j]);
+            if (WHOLE || i < n) p[i] = from_float<P>(y[j]);
+            if ((WHOLE || i < n) && copy) adamw_copy(copy, f.copy16, i, y[j]);
         }
     }
     const float mtop = __uint_as_float(__reduce_max_sync(~0u, mt)), vtop = __uint_as_float(__reduce_max_sync(~0u, vt));
@@ -225,7 +226,7 @@ template <typename P, typename G, bool EIGHTS> __device__ __forceinline__ void a
         w = b[j] > 0.0f ? max(w, 1u) : 0;
         if (EIGHTS) {
             cm[j / 4] |= c << 8 * (j & 3), cv[j / 4] |= w << 8 * (j & 3);
-        } else if (at(j) < n) {
+        } else if (WHOLE || at(j) < n) {
             ((uint8_t *)m)[at(j)] = (uint8_t)c, v[at(j)] = (uint8_t)w;
         }
     }
@@ -245,8 +246,9 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256, 
     for (int w = threadIdx.x >> 5; w < ADAMW_CHUNK / ADAMW_BLOCK; w += 8) {
         const uint64_t from = first + w * ADAMW_BLOCK;
         if (from >= t.n) break;
-        if (eights && from + ADAMW_BLOCK <= t.n) adamw8_block<P, G, true>(t, from, f, scale, threadIdx.x & 31);
-        else adamw8_block<P, G, false>(t, from, f, scale, threadIdx.x & 31);
+        if (from + ADAMW_BLOCK > t.n) adamw8_block<P, G, false, false>(t, from, f, scale, threadIdx.x & 31);
+        else if (eights) adamw8_block<P, G, true, true>(t, from, f, scale, threadIdx.x & 31);
+        else adamw8_block<P, G, false, true>(t, from, f, scale, threadIdx.x & 31);
     }
 }
 
@@ -257,18 +259,22 @@ template <int N> __global__ void __launch_bounds__(256) adamw_values_kernel(cons
     const AdamwTensor &t = list.t[k];                           // (p: m's values, copy: v's values)
     const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
     const int n = (int)min((uint64_t)ADAMW_CHUNK, t.n - from);
-    // a warp's 32 values are of one block
+    // four at a time from the first place on where codes and values are aligned, if there is one (views of flat buffers)
     auto read = [&](const uint8_t *codes, const float *scales, float *to, auto value) {
-        for (int i0 = threadIdx.x; i0 < n; i0 += 8 * 256) {
-            uint32_t c[8];
-            float s[8];
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (i0 + 256 * j < n) c[j] = codes[from + i0 + 256 * j], s[j] = scales[(from + i0 + 256 * j) / ADAMW_BLOCK];
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (i0 + 256 * j < n) to[from + i0 + 256 * j] = value(c[j], s[j]);
+        codes += from, to += from, scales += from / ADAMW_BLOCK;
+        const int h = (int)((16 - ((uintptr_t)to & 15)) & 15) / 4;
+        const bool fours = ((uintptr_t)(codes + h) & 3) == 0;
+        const int groups = fours && n > h ? (n - h) / 4 : 0, head = fours ? min(h, n) : n, rest = head + groups * 4;
+#pragma unroll 4
+        for (int g = threadIdx.x; g < groups; g += 256) {
+            const int i = h + g * 4;
+            const uint32_t c = *(const uint32_t *)(codes + i);
+            const float a = scales[i / ADAMW_BLOCK], b = scales[(i + 3) / ADAMW_BLOCK];     // (four values can be of two blocks)
+            const int turn = ADAMW_BLOCK - i % ADAMW_BLOCK;                                 // values of the first
+            *(float4 *)(to + i) = make_float4(value(c & 255, a), value(c >> 8 & 255, turn > 1 ? a : b), value(c >> 16 & 255, turn > 2 ? a : b), value(c >> 24, turn > 3 ? a : b));
         }
+        for (int i = threadIdx.x; i < head; i += 256) to[i] = value(codes[i], scales[i / ADAMW_BLOCK]);
+        for (int i = rest + threadIdx.x; i < n; i += 256) to[i] = value(codes[i], scales[i / ADAMW_BLOCK]);
     };
     if (t.p) read((const uint8_t *)t.m, t.ms, (float *)t.p, [](uint32_t c, float s) { return adamw_read_m(signed_byte_value(c), s); });
     if (t.copy) read((const uint8_t *)t.v, t.vs, (float *)t.copy, [](uint32_t c, float s) { return adamw_read_v(byte_value(c), s); });
