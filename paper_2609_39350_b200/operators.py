@@ -281,7 +281,7 @@ class HapAdamWTensors:
         if (m_scale is None) != (v_scale is None):
             _refuse("m_scale, v_scale: both or neither")
         self.bits = 32 if m_scale is None else 8
-        self.kept = [params, *[x for _, x in lists if x is not None]]
+        self.kept = [list(params), *[list(x) for _, x in lists if x is not None]]
         self.device = params[0].device
         here = torch.cuda.current_device()
         types = dict(params=(torch.float32, *_HALVES), grads=(torch.float32, *_HALVES), copies=_HALVES,

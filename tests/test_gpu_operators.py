@@ -130,6 +130,36 @@ def test_many_experts_and_long_groups():
     assert torch.equal(dw[1], a[40000:].float().T @ b[40000:].float())
 
 
+def test_more_row_tiles_than_a_band():
+    """A group of many tiles beside short ones, in all three forms."""
+    loads, N, K = [5000, 3, 0, 700, 260], 520, 264
+    off, o = offsets_of(loads, first=5)
+    rows, E = o[-1] + 9, len(loads)
+    x, dy, w = normal(rows, K), normal(rows, N, seed=1), normal(E, N, K, seed=2, scale=0.25)
+    y, dx, dw = hap.hap_expert_matmul(x, w, off), hap.hap_expert_matmul(dy, w, off, hap.EXPERT_GRAD_INPUT), hap.hap_expert_matmul(dy, x, off, hap.EXPERT_GRAD_WEIGHT, out_dtype=F32)
+    for e in range(E):
+        i, j = o[e], o[e + 1]
+        a, g, m = x[i:j].to(D), dy[i:j].to(D), w[e].to(D)
+        close(y[i:j], a @ m.T, (K + 8) * U * (a.abs() @ m.abs().T), BF)
+        close(dx[i:j], g @ m, (N + 8) * U * (g.abs() @ m.abs()), BF)
+        close(dw[e], g.T @ a, (j - i + 8) * U * (g.abs().T @ a.abs()), F32)
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("loads", [[1, 1], [90, 0, 300]], ids=str)
+def test_products_added_to_what_is_there(loads, out_dtype):
+    off, o = offsets_of(loads)
+    E, N, K, rows = len(loads), 264, 328, o[-1]
+    x, dy, w = normal(rows, K), normal(rows, N, seed=1), normal(E, N, K, seed=2, scale=0.1)
+    of = torch.repeat_interleave(torch.arange(E, device="cuda"), torch.tensor(loads, device="cuda"))
+    for form, a, cols, terms in ((hap.EXPERT_FORWARD, x, N, "rk,rnk->rn"), (hap.EXPERT_GRAD_INPUT, dy, K, "rn,rnk->rk")):
+        out = normal(rows, cols, seed=3, dtype=out_dtype)
+        before = out.to(D)
+        hap.hap_expert_matmul(a, w, off, form, out=out, accumulate=True)
+        ref, s = torch.einsum(terms, a.to(D), w[of].to(D)), torch.einsum(terms, a.to(D).abs(), w[of].to(D).abs())
+        close(out, before + ref, (a.shape[1] + 8) * U * s + U * (before.abs() + s), out_dtype)
+
+
 def gated_reference(x, w, F):
     z, s = x.to(D) @ w.to(D).T, x.to(D).abs() @ w.to(D).abs().T
     g, u = z[:, :F], z[:, F:]
@@ -249,6 +279,13 @@ def test_loss_in_pieces_against_differences():
     slope = (total(h) - total(-h)) / (2 * h)        # off by h^2 / 6 of a third derivative, below 1e-6 of the slope's terms
     along = (dx.to(D) * step).sum()
     assert (slope - along).abs() <= 2.0 ** -11 * 4 * (dx.to(D) * step).square().sum().sqrt() + 1e-5 * (dx.to(D) * step).abs().sum()
+
+
+def test_loss_without_rows():
+    x, w, t = torch.zeros(0, 64, dtype=BF, device="cuda"), normal(300, 64), torch.zeros(0, dtype=torch.int64, device="cuda")
+    loss, lse = hap.hap_linear_cross_entropy(x, w, t)
+    dx, dw = hap.hap_linear_cross_entropy_backward(x, w, t, lse, torch.ones((), device="cuda"), dw=torch.full((300, 64), 3.0, dtype=BF, device="cuda"))
+    assert loss.shape == (0,) and dx.shape == (0, 64) and not dw.any()
 
 
 def test_loss_of_bad_targets_and_infinite_logits():
@@ -429,6 +466,7 @@ def calls():
     grad = torch.full((), 0.01, device="cuda")
     lse = hap.hap_linear_cross_entropy(x, head, target)[1]
     space = hap.hap_linear_cross_entropy_workspace(x, head)
+    one = torch.tensor([0, 1, 1, 2, 2], device="cuda")
     return {
         "forward": lambda: hap.hap_expert_matmul(x, w, off),
         "grad_input": lambda: hap.hap_expert_matmul(dy, w, off, hap.EXPERT_GRAD_INPUT),
@@ -437,10 +475,12 @@ def calls():
         "gated_backward": lambda: hap.hap_expert_gated_backward(dy, w2, off, gu),
         "loss": lambda: hap.hap_linear_cross_entropy(x, head, target, workspace=space),
         "loss_backward": lambda: hap.hap_linear_cross_entropy_backward(x, head, target, lse, grad, workspace=space),
+        "loss_backward_few": lambda: hap.hap_linear_cross_entropy_backward(x[:5], head, target[:5], lse[:5], grad, workspace=space),
+        "one_row": lambda: hap.hap_expert_matmul(x[:2], w, one),
     }
 
 
-@pytest.mark.parametrize("name", ["forward", "grad_input", "grad_weight", "gated", "gated_backward", "loss", "loss_backward"])
+@pytest.mark.parametrize("name", ["forward", "grad_input", "grad_weight", "gated", "gated_backward", "loss", "loss_backward", "loss_backward_few", "one_row"])
 def test_repeated_captured_and_on_another_stream(name):
     """The same bits from a second call, from a call on another stream, and from a graph that is replayed twice."""
     call = calls()[name]
