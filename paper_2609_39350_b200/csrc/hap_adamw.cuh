@@ -13,12 +13,13 @@
 namespace hapop {
 
 constexpr int ADAMW_BLOCK = 256;        // values that share a scale
-constexpr int ADAMW_CHUNK = 4096;       // values that a block of threads takes
+// Values that a block of threads takes: the larger number where there are blocks enough for every multiprocessor to have several
+constexpr int ADAMW_CHUNK = 4096, ADAMW_SHORT = 1024;
 
 struct AdamwTensor { void *p; const void *g; void *m, *v; float *ms, *vs; void *copy; uint64_t n; };
 struct AdamwFactors { float b1, b2, a1, a2, decay, step, root, eps; int copy16; };      // a = 1 - b; step = lr / c1; root = 1 / sqrt(c2)
 // descriptors of one launch; the larger form fills most of a launch's 32 KB of arguments
-template <int N> struct AdamwList { AdamwTensor t[N]; unsigned first[N + 1]; int n; };      // first: first chunk of each tensor
+template <int N> struct AdamwList { AdamwTensor t[N]; unsigned first[N + 1]; int n, chunk; };      // first: first chunk of each tensor
 
 template <int N> __device__ __forceinline__ int adamw_tensor(const AdamwList<N> &list, unsigned chunk)
 {
@@ -100,8 +101,8 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
 {
     const int k = adamw_tensor(list, blockIdx.x);
     const AdamwTensor &t = list.t[k];
-    const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
-    const int n = (int)min((uint64_t)ADAMW_CHUNK, t.n - from);
+    const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * list.chunk;
+    const int n = (int)min((uint64_t)list.chunk, t.n - from);
     P *p = (P *)t.p + from;
     const G *g = (const G *)t.g + from;
     float *m = (float *)t.m + from, *v = (float *)t.v + from;
@@ -241,9 +242,9 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256, 
     const int k = adamw_tensor(list, blockIdx.x);
     const AdamwTensor &t = list.t[k];
     const float scale = grad_scale ? *grad_scale : 1.0f;
-    const uint64_t first = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
+    const uint64_t first = (uint64_t)(blockIdx.x - list.first[k]) * list.chunk;
     const bool eights = !(((uintptr_t)t.p | (uintptr_t)t.g | (uintptr_t)t.copy) & 15) && !(((uintptr_t)t.m | (uintptr_t)t.v) & 7);
-    for (int w = threadIdx.x >> 5; w < ADAMW_CHUNK / ADAMW_BLOCK; w += 8) {
+    for (int w = threadIdx.x >> 5; w < list.chunk / ADAMW_BLOCK; w += 8) {
         const uint64_t from = first + w * ADAMW_BLOCK;
         if (from >= t.n) break;
         if (from + ADAMW_BLOCK > t.n) adamw8_block<P, G, false, false>(t, from, f, scale, threadIdx.x & 31);
@@ -257,8 +258,8 @@ template <int N> __global__ void __launch_bounds__(256) adamw_values_kernel(cons
 {
     const int k = adamw_tensor(list, blockIdx.x);
     const AdamwTensor &t = list.t[k];                           // (p: m's values, copy: v's values)
-    const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * ADAMW_CHUNK;
-    const int n = (int)min((uint64_t)ADAMW_CHUNK, t.n - from);
+    const uint64_t from = (uint64_t)(blockIdx.x - list.first[k]) * list.chunk;
+    const int n = (int)min((uint64_t)list.chunk, t.n - from);
     // four at a time from the first place on where codes and values are aligned, if there is one (views of flat buffers)
     auto read = [&](const uint8_t *codes, const float *scales, float *to, auto value) {
         codes += from, to += from, scales += from / ADAMW_BLOCK;

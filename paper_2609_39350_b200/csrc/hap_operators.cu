@@ -361,18 +361,21 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
 // ---- AdamW ------------------------------------------------------------------------------------------------------------
 // Descriptors of one launch: a short list for the usual call on few tensors, whose arguments are copied faster, and one that
 // fills most of the 32 KB that a launch may carry.
-constexpr int FEW = 32, MANY = 440;
+constexpr int FEW = 56, MANY = 440;
 
 template <int N, typename F> static hap_status adamw_launches(const hap_adamw_tensor *tensors, int32_t n, float *const *m_out, float *const *v_out, F &&launch)
 {
     AdamwList<N> list;
+    uint64_t all = 0;
+    for (int i = 0; i < n; i++) all += tensors[i].count;
+    list.chunk = all < 4ull * 148 * ADAMW_CHUNK ? ADAMW_SHORT : ADAMW_CHUNK;
     for (int i = 0; i < n;) {
         list.n = 0;
         uint64_t chunks = 0;
         for (; i < n && list.n < N; i++) {
             const hap_adamw_tensor &t = tensors[i];
             if (!t.count) continue;
-            const uint64_t c = (t.count + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+            const uint64_t c = (t.count + list.chunk - 1) / list.chunk;
             if (chunks + c > INT32_MAX) {
                 if (!list.n) return HAP_E_RANGE;
                 break;
