@@ -320,19 +320,14 @@ template <typename T, int EPI> struct RowEpilogue {
     }
 };
 
-// The tiles that a worker (a block or a pair of blocks) takes, in order.  Groups come in two classes: of those with few rows the
-// weights (or the output) are the cost, of the others the products.  Each class is dealt out over the workers tile by tile, so
-// that those at work at one time share operands in L2, and a worker takes turns between its tiles of the two, in the proportion
-// in which it has them: memory and tensor cores are then busy at the same time (one class after the other took
-// 124 -> 103 us at 64 experts, 32768 rows by Zipf's law, 1024 -> 2048).  The second class is dealt from the other end, so that
-// the workers with one tile more in both are few.
+// Tiles of all groups in one order, in which workers (blocks or pairs of blocks) take every n-th: those at work at one time share
+// operands in L2.  (Groups with few rows, whose weights cost more to read than to multiply, in turns with the others instead of
+// where they come: no difference, 129 us either way at 64 experts with 32768 rows by Zipf's law, 1024 -> 2048.)
 // Offsets come from device memory: they are clamped to the rows and made ascending here, so that no offset can lead outside of
 // the operands.
 template <int BM> struct Schedule {
     int bound[MAX_GROUPS + 1];
-    int first[MAX_GROUPS + 1];      // first tile of each group, in the order of `group`; behind all of them their number
-    uint16_t group[MAX_GROUPS];     // the groups with many rows, then the others
-    int many;                       // tiles of the first class
+    int first[MAX_GROUPS + 1];      // first tile of each group (NT, NN)
     struct Tile { int e, m, n, lo, hi; };
 
     __device__ static int row_tiles(int n) { return (n + BM - 1) / BM; }
@@ -344,11 +339,10 @@ template <int BM> struct Schedule {
             bound[i] = o < 0 ? 0 : o > p.rows ? p.rows : (int)o;
         }
     }
-    // by all threads of a warp; groups of at most `few` rows are of the second class
-    __device__ void build(const Args &p, int form, int col_tiles, int few, int lane)
+    // by all threads of a warp
+    __device__ void build(const Args &p, int col_tiles, int lane)
     {
-        const int per = row_tiles(p.mdim) * col_tiles;      // TN: tiles of every group
-        int below = 0;
+        int below = 0, tiles = 0;   // carried over the blocks of 32
         for (int i0 = 0; i0 <= p.groups; i0 += 32) {
             const int i = i0 + lane;
             int b = max(i <= p.groups ? bound[i] : 0, below);
@@ -357,55 +351,42 @@ template <int BM> struct Schedule {
                 const int x = __shfl_up_sync(~0u, b, d);
                 if (lane >= d) b = max(b, x);
             }
-            if (i <= p.groups) bound[i] = b;
-            below = __shfl_sync(~0u, b, 31);
-        }
-        __syncwarp();
-        int at = 0, tiles = 0;
-        for (int second = 0; second < 2; second++) {
-            if (second && lane == 0) many = tiles;
-            for (int i0 = 0; i0 < p.groups; i0 += 32) {
-                const int i = i0 + lane, rows = i < p.groups ? bound[i + 1] - bound[i] : 0;
-                const bool mine = i < p.groups && (rows <= few) == (second == 1);
-                const unsigned all = __ballot_sync(~0u, mine);
-                int t = !mine ? 0 : form == TN ? per : row_tiles(rows) * col_tiles;
-                const int own = t;
+            int last = __shfl_up_sync(~0u, b, 1);
+            if (lane == 0) last = below;
+            int t = i > 0 && i <= p.groups ? row_tiles(b - last) * col_tiles : 0;
 #pragma unroll
-                for (int d = 1; d < 32; d *= 2) {
-                    const int x = __shfl_up_sync(~0u, t, d);
-                    if (lane >= d) t += x;
-                }
-                if (mine) {
-                    const int k = at + __popc(all & ((1u << lane) - 1));
-                    group[k] = (uint16_t)i, first[k] = tiles + t - own;
-                }
-                at += __popc(all);
-                tiles += __shfl_sync(~0u, t, 31);
+            for (int d = 1; d < 32; d *= 2) {
+                const int x = __shfl_up_sync(~0u, t, d);
+                if (lane >= d) t += x;
             }
+            if (i <= p.groups) bound[i] = b, first[i] = tiles + t;
+            below = __shfl_sync(~0u, b, 31);
+            tiles += __shfl_sync(~0u, t, 31);
         }
-        if (lane == 0) first[p.groups] = tiles;
         __syncwarp();
     }
-    // tiles of worker w of n
-    struct Share { int a, b; };
-    __device__ Share share(int groups, int w, int n) const { return {max(0, (many - w + n - 1) / n), max(0, (first[groups] - many - (n - 1 - w) + n - 1) / n)}; }
-    // its i-th
-    __device__ Tile tile(const Args &p, int form, int col_tiles, Share s, int i, int w, int n) const
+    __device__ int total(const Args &p, int form, int col_tiles) const { return form == TN ? p.groups * row_tiles(p.mdim) * col_tiles : first[p.groups]; }
+    __device__ Tile tile(const Args &p, int form, int col_tiles, int t) const
     {
-        const int all = s.a + s.b;
-        const int64_t phase = (int64_t)w * all / n;         // workers are at different places of the same pattern
-        const int a0 = (int)((i * (int64_t)s.a + phase) / all), a1 = (int)(((i + 1) * (int64_t)s.a + phase) / all);
-        int t = a1 > a0 ? w + a0 * n : many + (n - 1 - w) + (i - a0) * n;
-        int lo = 0, hi = p.groups - 1;                      // last place whose first tile is not behind t
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (first[mid] <= t) lo = mid; else hi = mid - 1;
-        }
         Tile r;
-        r.e = group[lo];
-        t -= first[lo];
+        int rows;
+        if (form == TN) {
+            rows = p.mdim;
+            const int per = row_tiles(rows) * col_tiles;
+            r.e = t / per;
+            t -= r.e * per;
+        } else {
+            int lo = 0, hi = p.groups - 1;                  // last group whose first tile is not behind t
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= t) lo = mid; else hi = mid - 1;
+            }
+            r.e = lo;
+            t -= first[lo];
+            rows = bound[lo + 1] - bound[lo];
+        }
         r.lo = bound[r.e], r.hi = bound[r.e + 1];
-        const int mt = row_tiles(form == TN ? p.mdim : r.hi - r.lo), band = min(mt, BAND);
+        const int mt = row_tiles(rows), band = min(mt, BAND);
         const int which = t / (band * col_tiles);
         t -= which * band * col_tiles;
         const int high = min(band, mt - which * band);
@@ -431,11 +412,11 @@ template <typename T, int FORM, int EPI> __global__ void __launch_bounds__(256) 
     const int col_tiles = (p.ncols + BN - 1) / BN;
     sched.fetch(p);
     __syncthreads();
-    if (tid < 32) sched.build(p, FORM, col_tiles, 0, tid);
+    if (tid < 32) sched.build(p, col_tiles, tid);
     __syncthreads();
-    const auto share = sched.share(p.groups, blockIdx.x, gridDim.x);
-    for (int t = 0; t < share.a + share.b; t++) {
-        const auto tile = sched.tile(p, FORM, col_tiles, share, t, blockIdx.x, gridDim.x);
+    const int total = sched.total(p, FORM, col_tiles);
+    for (int t = blockIdx.x; t < total; t += gridDim.x) {
+        const auto tile = sched.tile(p, FORM, col_tiles, t);
         const int m0 = tile.m * PM, n0 = tile.n * BN;
         const int mrows = FORM == TN ? p.mdim - m0 : tile.hi - tile.lo - m0;        // rows of out from m0 on
         const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;

@@ -15,7 +15,6 @@ template <int EPI> struct Turned {
     static constexpr int ROWS = EPI == GATED ? 128 : 256;           // most rows of a tile
     static constexpr int A_BYTES = (EPI == GATED ? 2 : 1) * 128 * BK * 2, B_BYTES = ROWS / 2 * BK * 2, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = EPI == GATED ? 5 : 6;
-    static constexpr int FEW = 256;                                 // rows of a group whose weight costs more to read than to multiply
     static constexpr int PIECE = EPI == STORE ? 32 : 16;            // rows that a warp takes at a time: what fits its registers
     static constexpr int OUT = PIECE * 64;                          // shared memory of a warp for them
 };
@@ -125,24 +124,22 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
     wait_for_last();
     sh.sched.fetch(p);
     __syncthreads();
-    if (warp == 0) sh.sched.build(p, FORM, col_tiles, S::FEW, lane);
+    if (warp == 0) sh.sched.build(p, col_tiles, lane);
     fence_before();
     __syncthreads();
     cluster_sync();
     fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sh.tmem;
     volatile int *stop = &sh.stop;
-    const int workers = gridDim.x / 2, worker = blockIdx.x / 2;
-    const auto share = sh.sched.share(p.groups, worker, workers);
-    const int total = share.a + share.b;
+    const int total = sh.sched.total(p, FORM, col_tiles), step = gridDim.x / 2, begin = blockIdx.x / 2;
     // rows of a tile, as the products count them
     auto rows_of = [](const auto &tile) { return min(S::ROWS, (tile.hi - tile.lo - tile.m * S::ROWS + 31) & ~31); };
 
     if (warp == 0) {
         uint32_t at = 0;
         bool good = true;
-        for (int t = 0; t < total && good; t++) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+        for (int t = begin; t < total && good; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
             const int n0 = tile.n * BN + (int)rank * 128, half = rows_of(tile) / 2, row = tile.lo + tile.m * S::ROWS + (int)rank * half;
             for (int k = 0; k < p.kdim; k += BK, at++) {
                 const int s = at % S::STAGES;
@@ -170,8 +167,8 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
             constexpr uint32_t idesc = 1u << 4 | TypeBits<T>::value << 7 | TypeBits<T>::value << 10 | (FORM == NN ? 1u << 15 : 0) | (256u / 16) << 24;
             uint32_t at = 0, sums = 0;
             bool good = true;
-            for (int t = 0; t < total && good; t++) {
-                const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+            for (int t = begin; t < total && good; t += step) {
+                const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
                 const uint32_t of = idesc | (uint32_t)(rows_of(tile) / 8) << 17;
                 const int set = sums & 1;
                 if (!(good = bar_wait(&sh.acc_empty[set], (sums / 2 + 1) & 1, stop))) break;
@@ -201,8 +198,8 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const WarpColumns w{(uint32_t *)(outs + (warp - 2) * S::OUT), lane};
         const uint32_t from = tmem + ((uint32_t)quarter << 21);
-        for (int t = 0; t < total; t++) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+        for (int t = begin; t < total; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
             const int set = sums & 1, col = tile.n * BN + (int)rank * 128 + quarter * 32, cols = p.ncols - col;
             constexpr int R = S::PIECE;
             const int pieces = rows_of(tile) / R, live = tile.hi - tile.lo - tile.m * S::ROWS;

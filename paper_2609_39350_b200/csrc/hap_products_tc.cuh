@@ -31,7 +31,6 @@ template <int EPI, int CG> struct Shape {
     // 1024 steps there, and these sums in registers; reading them costs some 400 cycles in 8192, under the next products.
     static constexpr bool SUMS = EPI == STORE32 || EPI == LSE;
     static constexpr int SUM_STEPS = 1024;
-    static constexpr int FEW = 1024;                    // TN: rows of a group whose output costs more than its products
 };
 
 template <int EPI, int CG> struct Shared {
@@ -237,22 +236,20 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
     wait_for_last();
     sh.sched.fetch(p);
     __syncthreads();
-    if (warp == 0) sh.sched.build(p, FORM, col_tiles, FORM == TN ? S::FEW : 0, lane);
+    if (warp == 0) sh.sched.build(p, col_tiles, lane);
     fence_before();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();
     fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sh.tmem;
     volatile int *stop = &sh.stop;
-    const int workers = gridDim.x / CG, worker = blockIdx.x / CG;
-    const auto share = sh.sched.share(p.groups, worker, workers);
-    const int total = share.a + share.b;
+    const int total = sh.sched.total(p, FORM, col_tiles), step = gridDim.x / CG, begin = blockIdx.x / CG;
 
     if (warp == 0) {
         uint32_t at = 0;                                    // stages brought so far
         bool good = true;
-        for (int t = 0; t < total && good; t++) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+        for (int t = begin; t < total && good; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
             const int part = EPI == SUM32 ? tile.n / part_tiles : 0;
             const int m0 = tile.m * S::BM + rank * 128, n0 = (tile.n - part * part_tiles) * BN;
             const int K = FORM == TN ? tile.hi - tile.lo : EPI == SUM32 ? min(p.kdim, (part + 1) * p.split_k) : p.kdim;
@@ -289,14 +286,14 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
             constexpr uint32_t idesc = Instruction<T, FORM, CG>::bits;
             uint32_t at = 0, sums = 0;
             bool good = true;
-            for (int t = 0; t < total && good; t++) {
+            for (int t = begin; t < total && good; t += step) {
                 int K = p.kdim;
                 if (EPI == SUM32) {
-                    const int part = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers).n / part_tiles;
+                    const int part = sh.sched.tile(p, FORM, col_tiles, t).n / part_tiles;
                     K = min(p.kdim - part * p.split_k, p.split_k);
                 }
                 if (FORM == TN) {
-                    const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+                    const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
                     K = tile.hi - tile.lo;
                     if (!K) continue;                       // nothing to sum: the epilogue writes zeros by itself
                 }
@@ -327,8 +324,8 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
         }
     } else if (FORM == TN && warp == 10) {
         uint32_t at = 0, phases = 0;
-        for (int t = 0; t < total; t++) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+        for (int t = begin; t < total; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
             const int K = tile.hi - tile.lo, rest = K % BK;
             at += (K + BK - 1) / BK;
             if (!rest || tile.hi >= p.rows) continue;
@@ -348,8 +345,8 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
         constexpr int CHUNKS = BN / 64;                     // pieces of 32 columns that a warp has
         char *staged = outs + (warp - 2) * S::OUT;
         const uint32_t from = tmem + ((uint32_t)quarter << 21) + half * CHUNKS * 32;
-        for (int t = 0; t < total; t++) {
-            const auto tile = sh.sched.tile(p, FORM, col_tiles, share, t, worker, workers);
+        for (int t = begin; t < total; t += step) {
+            const auto tile = sh.sched.tile(p, FORM, col_tiles, t);
             const int part = EPI == SUM32 ? tile.n / part_tiles : 0;
             const int m = tile.m * S::BM + rank * 128 + quarter * 32, n0 = (tile.n - part * part_tiles) * BN + half * CHUNKS * 32;
             const int K = FORM == TN ? tile.hi - tile.lo : p.kdim;
