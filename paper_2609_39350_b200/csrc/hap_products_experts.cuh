@@ -61,11 +61,11 @@ struct WarpColumns {
     // in two steps, so that the loads are on their way while something else is waited for
     template <int R, typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[R / 8], int rows, int cols) const
     {
-        if (!whole(first, ld, cols)) return;
+        if (!whole(first, ld, cols) || rows <= 0) return;
 #pragma unroll
-        for (int i = 0; i < R / 8; i++) {
-            const int r = 2 * (i / 2 * 8 + (lane >> 2)) + i % 2;
-            w[i] = r < rows ? *(const uint4 *)(first + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < R / 8; i++) {                   // (rows behind the last are the last: a choice after the load would wait for it)
+            const int r = min(2 * (i / 2 * 8 + (lane >> 2)) + i % 2, rows - 1);
+            w[i] = *(const uint4 *)(first + r * ld + (lane & 3) * 8);
         }
     }
     template <typename T, int R> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[R / 8], float (&v)[R], int rows, int cols) const
