@@ -216,9 +216,10 @@ template <typename P, typename G, bool EIGHTS, bool WHOLE> __device__ __forceinl
     }
     const float mtop = __uint_as_float(__reduce_max_sync(~0u, mt)), vtop = __uint_as_float(__reduce_max_sync(~0u, vt));
     if (lane == 0) t.ms[block] = mtop, t.vs[block] = vtop;
-    // (codes of a block whose scale is not finite are read as values that are not finite, whatever they are; where a scale is
-    // so small that its inverse overflows the quick way gives no number and the operations are made)
-    const float md = mtop > 0.0f ? mtop : 1.0f, vd = vtop > 0.0f ? vtop : 1.0f, mr = __fdividef(1.0f, md), vr = __fdividef(1.0f, vd);
+    // (codes of a block whose scale is not finite are read as values that are not finite, whatever they are; where a scale's
+    // inverse would overflow or be 0 the quick way gets no number, and the operations are made)
+    const float md = mtop > 0.0f ? mtop : 1.0f, vd = vtop > 0.0f ? vtop : 1.0f;
+    const float mr = md < 1e37f ? __fdividef(1.0f, md) : NAN, vr = vd < 1e37f ? __fdividef(1.0f, vd) : NAN;
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; j++) {

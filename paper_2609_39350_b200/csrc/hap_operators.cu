@@ -9,9 +9,6 @@
 
 using namespace hapop;
 
-#ifndef HAP_PAIR_ROWS
-#define HAP_PAIR_ROWS 128
-#endif
 
 static hap_status launched() { return cudaGetLastError() == cudaSuccess ? HAP_OK : HAP_E_CUDA; }
 
@@ -62,7 +59,7 @@ static bool make_map(CUtensorMap *map, bool fp16, const void *base, int64_t cols
 static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 15) == 0 && ld % 8 == 0 && ld < (1ll << 36); }
 
 // Launches a kernel that may start while its predecessor in the stream still ends: its setup (barriers, tensor memory, maps) and the
-// launch itself then cost nothing (loss of 129 rows: PDLWAS -> PDLUS us).  The kernel waits for the predecessor before it reads.
+// launch itself then cost nothing (loss of 129 rows: 28.7 -> 25.3 us).  The kernel waits for the predecessor before it reads.
 template <typename... P, typename... A> static hap_status launch_next(void (*kernel)(P...), int64_t grid, int threads, int smem, int cluster, cudaStream_t stream, const A &...args)
 {
     cudaLaunchConfig_t c{};
@@ -112,18 +109,24 @@ template <typename T, int FORM, int EPI, int CG> static hap_status launch_tensor
 }
 
 // experts' rows as columns of the products (NT, NN; out in 16 bits)
-template <typename T, int FORM, int EPI> static hap_status launch_experts(const Args &p, Device d, cudaStream_t stream)
+template <typename T, int FORM, int EPI> static hap_status launch_experts(Args p, Device d, cudaStream_t stream)
 {
     using S = Turned<EPI>;
     const int64_t most = ceil_div(p.ncols, 256) * (ceil_div(p.rows, S::ROWS) + p.groups);
     if (most > INT32_MAX) return HAP_E_RANGE;
     constexpr bool fp16 = TypeBits<T>::value == 0;
-    CUtensorMap mw, mr, mf;
+    CUtensorMap mw, mr, mf, mk{};
     const int64_t wrows = FORM == NT ? (EPI == GATED ? 2ll * p.ncols : p.ncols) : p.kdim;
     if (!make_map(&mw, fp16, p.b, FORM == NT ? p.kdim : p.ncols, wrows, p.groups, p.ldb, p.bgroup, FORM == NT ? 128 : BK) ||
         !make_map(&mr, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, S::ROWS / 2) || !make_map(&mf, fp16, p.a, p.kdim, p.rows, 1, p.lda, 0, 16))
         return HAP_E_CUDA;
-    return launch_pairs<expert_kernel<T, FORM, EPI>>(1024 + S::STAGES * S::STAGE + 8 * S::OUT + sizeof(TurnedShared<EPI>), most, d, stream, p, mw, mr, mf);
+    if (EPI == GATED_BACK && mappable(p.gu, p.ldgu) && p.ncols % 8 == 0) {      // (u begins ncols values behind g, at a multiple of 16 bytes)
+        const cuuint64_t dims[3] = {2 * (cuuint64_t)p.ncols, (cuuint64_t)p.rows, 1}, strides[2] = {(cuuint64_t)p.ldgu * 2, (cuuint64_t)p.ldgu * 2 * (cuuint64_t)p.rows};
+        const cuuint32_t box[3] = {32, 16, 1}, each[3] = {1, 1, 1};
+        p.kept_mapped = encode_tiled()(&mk, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, (void *)p.gu, dims, strides, box, each,
+                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
+    return launch_pairs<expert_kernel<T, FORM, EPI>>(1024 + S::STAGES * S::STAGE + 8 * (S::OUT + S::KEPT) + sizeof(TurnedShared<EPI>), most, d, stream, p, mw, mr, mf, mk);
 }
 
 template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
@@ -149,8 +152,11 @@ template <typename T, int FORM, int EPI> static hap_status launch_product(const 
         }
         return launch_experts<T, FORM, EPI>(p, d, stream);
     } else {
-        const int64_t high = FORM == TN ? p.mdim : p.rows / p.groups;       // rows of a group's output
-        return high > HAP_PAIR_ROWS ? launch_tensor<T, FORM, EPI, 2>(p, d, stream) : launch_tensor<T, FORM, EPI, 1>(p, d, stream);
+        // rows of the output: up to 128 fill one block's tile, and pairs cost more to start (loss of 128 rows, 1024 x 32003: 17.5 us
+        // alone, 23.4 in pairs; 8192 x 16000: 67 and 58); above, a pair reads each operand half as often (8192 x 8192 x 8192: 1483
+        // and 1662 TFLOP/s)
+        const int64_t high = FORM == TN ? p.mdim : p.rows;
+        return high > 128 ? launch_tensor<T, FORM, EPI, 2>(p, d, stream) : launch_tensor<T, FORM, EPI, 1>(p, d, stream);
     }
 }
 
@@ -234,7 +240,7 @@ static uint64_t up256(uint64_t n) { return (n + 255) / 256 * 256; }
 constexpr int64_t TWICE_ROWS = 128;
 
 // dx of few rows is few tiles with the longest contraction there is, the vocabulary: it is split so that each of the device's 74
-// pairs of blocks has a tile, into parts of at least 1024 (8 rows, 1024 x 100000: SPLITUS us, SPLITWAS without)
+// pairs of blocks has a tile, into parts of at least 1024 (8 rows, 1024 x 100000: 618 -> 128 us)
 static int parts_of_dx(int64_t rows, int64_t H, int64_t piece)
 {
     const int64_t tiles = ceil_div(rows < 1 ? 1 : rows, 2 * 128) * ceil_div(H, TILE_N), fit = 74 / tiles, most = ceil_div(piece, 1024);

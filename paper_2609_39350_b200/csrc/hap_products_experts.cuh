@@ -1,7 +1,7 @@
 // Products of the experts' rows on the tensor cores, turned around: the weight's columns are the 256 rows of a product (128 for
 // each block of a pair) and the expert's rows its columns, 32 to 256 of them in steps of 32.  So an expert with 40 rows costs 64
 // columns, not 128 or 256 rows, and experts have few rows each: of 32 experts with 8190 rows by Zipf's law, tiles of 256 rows
-// would be 63 % filled, of 128 rows 82 %, these are 94 %.  Sums come out of tensor memory with a weight's column in each lane;
+// would be 63 % filled, of 128 rows 82 %, these are 95 %: 145 -> 128 us for the input's gradient of 20 experts, 835 -> 704 gated.  Sums come out of tensor memory with a weight's column in each lane;
 // they are turned back in shared memory.
 //   NT  out[i][n] = sum_k a[i][k] w_e[n][k]          NN  out[i][k] = sum_n a[i][n] w_e[n][k]
 // GATED makes two products of 256 x 128 in a tile, g and u of the same columns in the same lanes.
@@ -14,14 +14,16 @@ namespace hapop {
 template <int EPI> struct Turned {
     static constexpr int ROWS = EPI == GATED ? 128 : 256;           // most rows of a tile
     static constexpr int A_BYTES = (EPI == GATED ? 2 : 1) * 128 * BK * 2, B_BYTES = ROWS / 2 * BK * 2, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = EPI == GATED ? 5 : 6;
+    static constexpr int STAGES = EPI == STORE ? 6 : 5;
+    // GATED_BACK: two buffers of each warp for 16 rows of 32 values of the kept g and u
+    static constexpr int KEPT = EPI == GATED_BACK ? 2 * 2 * 1024 : 0;
     static constexpr int PIECE = EPI == STORE ? 32 : 16;            // rows that a warp takes at a time: what fits its registers
     static constexpr int OUT = PIECE * 64;                          // shared memory of a warp for them
 };
 
 template <int EPI> struct TurnedShared {
     Schedule<Turned<EPI>::ROWS> sched;
-    uint64_t full[8], empty[8], acc_full[2], acc_empty[2];
+    uint64_t full[8], empty[8], acc_full[2], acc_empty[2], kept[8][2];
     uint32_t tmem;
     int stop;
 };
@@ -58,51 +60,22 @@ struct WarpColumns {
                 *(uint4 *)(o + ld) = make_uint4(__byte_perm(lo.x, lo.y, 0x7632), __byte_perm(lo.z, lo.w, 0x7632), __byte_perm(hi.x, hi.y, 0x7632), __byte_perm(hi.z, hi.w, 0x7632));
         }
     }
-    // in two steps, so that the loads are on their way while something else is waited for
-    template <int R, typename T> __device__ __forceinline__ void fetch(const T *first, int64_t ld, uint4 (&w)[R / 8], int rows, int cols) const
+    template <typename T, int R> __device__ __forceinline__ void read(const T *first, int64_t ld, float (&v)[R], int rows, int cols) const
     {
-        if (!whole(first, ld, cols) || rows <= 0) return;
 #pragma unroll
-        for (int i = 0; i < R / 8; i++) {                   // (rows behind the last are the last: a choice after the load would wait for it)
-            const int r = min(2 * (i / 2 * 8 + (lane >> 2)) + i % 2, rows - 1);
-            w[i] = *(const uint4 *)(first + r * ld + (lane & 3) * 8);
-        }
-    }
-    template <typename T, int R> __device__ __forceinline__ void take(const T *first, int64_t ld, const uint4 (&w)[R / 8], float (&v)[R], int rows, int cols) const
-    {
-        if (!whole(first, ld, cols)) {
-#pragma unroll
-            for (int i = 0; i < R; i++) v[i] = i < rows && lane < cols ? to_float(first[i * ld + lane]) : 0.0f;
-            return;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < R / 16; i++) {
-            const int pair = i * 8 + (lane >> 2), c = lane & 3, odd = pair & 1;
-            const uint4 a = w[2 * i], b = w[2 * i + 1];
-            const uint4 lo = make_uint4(__byte_perm(a.x, b.x, 0x5410), __byte_perm(a.x, b.x, 0x7632), __byte_perm(a.y, b.y, 0x5410), __byte_perm(a.y, b.y, 0x7632));
-            const uint4 hi = make_uint4(__byte_perm(a.z, b.z, 0x5410), __byte_perm(a.z, b.z, 0x7632), __byte_perm(a.w, b.w, 0x5410), __byte_perm(a.w, b.w, 0x7632));
-            *words(pair, c, odd) = odd ? hi : lo;
-            *words(pair, c, odd ^ 1) = odd ? lo : hi;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < R / 2; i++) {
-            const float2 f = unpack2(staged[i * 32 + lane], T());
-            v[2 * i] = f.x, v[2 * i + 1] = f.y;
-        }
+        for (int i = 0; i < R; i++) v[i] = i < rows && lane < cols ? to_float(first[i * ld + lane]) : 0.0f;
     }
 };
 
 template <typename T, int FORM, int EPI>
 __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ Args p, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_rows,
-                                                        const __grid_constant__ CUtensorMap map_few)
+                                                        const __grid_constant__ CUtensorMap map_few, const __grid_constant__ CUtensorMap map_kept)
 {
     using S = Turned<EPI>;
     extern __shared__ char raw[];
     char *stages = (char *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     char *outs = stages + S::STAGES * S::STAGE;
-    TurnedShared<EPI> &sh = *(TurnedShared<EPI> *)(outs + 8 * S::OUT);
+    TurnedShared<EPI> &sh = *(TurnedShared<EPI> *)(outs + 8 * (S::OUT + S::KEPT));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     constexpr int BN = 256;                                 // columns of out that a tile covers
@@ -114,6 +87,7 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
         if (lane == 0) {
             for (int i = 0; i < S::STAGES; i++) bar_init(&sh.full[i], 2), bar_init(&sh.empty[i], 1);
             for (int i = 0; i < 2; i++) bar_init(&sh.acc_full[i], 1), bar_init(&sh.acc_empty[i], 16);
+            for (int i = 0; i < 16; i++) bar_init(&sh.kept[i / 2][i % 2], 1);
             sh.stop = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async;" ::: "memory");
@@ -194,8 +168,9 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
             }
         }
     } else {
-        uint32_t sums = 0;
+        uint32_t sums = 0, asked = 0, used = 0;             // asked, used: pieces of the kept g and u
         const int quarter = warp & 3, half = (warp - 2) >> 2;
+        char *kept = outs + 8 * S::OUT + (warp - 2) * S::KEPT;
         const WarpColumns w{(uint32_t *)(outs + (warp - 2) * S::OUT), lane};
         const uint32_t from = tmem + ((uint32_t)quarter << 21);
         for (int t = begin; t < total; t += step) {
@@ -204,15 +179,20 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
             constexpr int R = S::PIECE;
             const int pieces = rows_of(tile) / R, live = tile.hi - tile.lo - tile.m * S::ROWS;
             const int64_t row0 = (int64_t)tile.lo + tile.m * S::ROWS;
-            uint4 g4[R / 8], u4[R / 8];
-            auto ahead = [&](int q) {
-                if constexpr (EPI == GATED_BACK) {
-                    const T *gu = (const T *)p.gu + (row0 + q * R) * p.ldgu + col;
-                    w.fetch<R>(gu, p.ldgu, g4, live - q * R, cols);
-                    w.fetch<R>(gu + p.ncols, p.ldgu, u4, live - q * R, cols);
+            // the kept g and u of a piece come by TMA, two pieces ahead (loads of the lanes, turned in shared memory, one piece ahead:
+            // 193 us at 64 experts with 32760 rows, 2048 x 1024, where this takes 151)
+            const bool mapped = EPI == GATED_BACK && p.kept_mapped;
+            auto bring = [&](int q) {
+                if (mapped && lane == 0) {
+                    const uint32_t bar = smem_u32(&sh.kept[warp - 2][asked & 1]), to = smem_u32(kept + (asked & 1) * 2048);
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], 2048;" ::"r"(bar) : "memory");
+                    tma_load<1>(&map_kept, to, bar, col, (int)row0 + q * R, 0);
+                    tma_load<1>(&map_kept, to + 1024, bar, p.ncols + col, (int)row0 + q * R, 0);
                 }
+                if (mapped) asked++;
             };
-            if (cols > 0 && half < pieces) ahead(half);
+            if (cols > 0)
+                for (int q = half; q < min(pieces, half + 4); q += 2) bring(q);
             if (!bar_wait(&sh.acc_full[set], (sums / 2) & 1, stop)) break;
             sums++;
             fence_after();
@@ -258,12 +238,21 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
                 }
                 if constexpr (EPI == GATED_BACK) {
                     float g[R], u[R];
+                    if (mapped) {
+                        const T *at = (const T *)(kept + (used & 1) * 2048) + lane;
+                        if (!bar_wait(&sh.kept[warp - 2][used & 1], used >> 1 & 1, stop)) break;
+                        used++;
+#pragma unroll
+                        for (int i = 0; i < R; i++) g[i] = to_float(at[i * 32]), u[i] = to_float(at[512 + i * 32]);
+                        __syncwarp();
+                        if (q + 4 < pieces) bring(q + 4);
+                    } else {
+                        const T *gu = (const T *)p.gu + row * p.ldgu + col;
+                        w.read(gu, p.ldgu, g, n, cols);
+                        w.read(gu + p.ncols, p.ldgu, u, n, cols);
+                    }
                     tmem_load_wait();
                     if (q + 2 >= pieces) taken();
-                    const T *gu = (const T *)p.gu + row * p.ldgu + col;
-                    w.take(gu, p.ldgu, g4, g, n, cols);
-                    w.take(gu + p.ncols, p.ldgu, u4, u, n, cols);
-                    if (q + 2 < pieces) ahead(q + 2);
 #pragma unroll
                     for (int i = 0; i < R; i++) gate_back(g[i], u[i], v[i]);
                     T *o = (T *)p.out + row * p.ldo + col;
@@ -273,6 +262,11 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
                 }
             }
         }
+        if (EPI == GATED_BACK && lane == 0)                 // cut short: what is still on its way
+            for (; used < asked; used++) {
+                const uint64_t since = nanoseconds();
+                while (!bar_try(smem_u32(&sh.kept[warp - 2][used & 1]), used >> 1 & 1) && nanoseconds() - since < 100000000ull) {}
+            }
     }
     fence_before();
     __syncthreads();

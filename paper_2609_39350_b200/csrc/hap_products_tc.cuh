@@ -10,7 +10,7 @@
 // matrix arrive as zeros.  In TN the steps are rows, and those behind a group's last are another group's: a warp of its own
 // overwrites them with zeros (in both operands: 0 times what lies there could be NaN) before the stage is handed on.  (8 weight
 // gradients of 4096 x 14336, 8192 rows: 2403 us with such stages loaded by the producer's threads, 1373 where the producer
-// cleared them, ENDUS with the warp.)
+// cleared them, 1266 with the warp.)
 #pragma once
 #include <cuda.h>
 #include "hap_products.cuh"
@@ -26,9 +26,9 @@ template <int EPI, int CG> struct Shape {
     // outputs leave through shared memory, for each warp 32 rows of 64 bytes, or of 128 where they are fp32
     static constexpr int OUT = EPI == STORE32 ? 4096 : 2048;
     static constexpr int STAGES = CG == 1 ? (EPI == STORE32 ? 3 : 4) : (EPI == STORE32 ? 5 : 6);
-    // Tensor cores add to a sum by truncating: after n products of 16 steps it is short by about n 2^-25 of its magnitude (1e-6
-    // at a contraction of 3000, six times the error of sums rounded to nearest).  Results that are kept in fp32 are summed over
-    // 1024 steps there, and these sums in registers; reading them costs some 400 cycles in 8192, under the next products.
+    // Tensor cores add to a sum by truncating: after n products of 16 steps it is short by about n 2^-25 of its magnitude (at
+    // 3500 rows 2.4e-6, six times the error of sums rounded to nearest; 7.7e-7 this way).  Results that are kept in fp32 are summed over
+    // 1024 steps there, and these sums in registers, under the next products.
     static constexpr bool SUMS = EPI == STORE32 || EPI == LSE;
     static constexpr int SUM_STEPS = 1024;
 };
@@ -44,7 +44,7 @@ __device__ unsigned operator_error;
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // One lane of a converged warp.  Unlike a test of the lane number it tells the compiler that a single thread follows, so that
-// the operands of TMA and tcgen05 go to uniform registers directly (a product's issue fell from 110 cycles to below its run time).
+// the operands of TMA and tcgen05 go to uniform registers directly (8192 x 8192 x 8192: 1451 -> 1593 TFLOP/s).
 __device__ __forceinline__ bool elected()
 {
     uint32_t p;
@@ -57,7 +57,7 @@ __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.a
 __device__ __forceinline__ uint32_t of_leader(uint32_t a) { uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(a)); return r; }
 __device__ __forceinline__ void bar_init(uint64_t *b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n) : "memory"); }
 // Arrivals and waits carry the block's scope only, but where data written by threads goes with them: a fence for the cluster on
-// every stage made the producer the slowest of all (731 TFLOP/s at 8192 x 8192 x 8192 in pairs, instead of the figures below).
+// every stage made the producer the slowest of all (8192 x 8192 x 8192: 731 TFLOP/s with it, 1451 without).
 template <int CG> __device__ __forceinline__ void bar_expect_at(uint32_t addr, uint32_t bytes)
 {
     if constexpr (CG == 1) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr), "r"(bytes) : "memory");
@@ -78,6 +78,7 @@ __device__ __forceinline__ bool bar_try(uint32_t a, uint32_t parity)
 __device__ __forceinline__ void acquire_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 __device__ __forceinline__ uint64_t nanoseconds() { uint64_t t; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t)); return t; }
 
+// A try suspends the warp for up to a millisecond: ten warps that ask all the time take issue slots and power (1530 -> 1642 TFLOP/s).
 // Waits for a phase, ten seconds at most (the longest tile, 2^30 rows of contraction, takes about five).  False: it ran out,
 // here or in another warp of the block; the kernel then ends early and the device word says so.
 __device__ __noinline__ bool bar_wait_long(uint32_t a, uint32_t parity, volatile int *stop, uint64_t limit)
@@ -385,7 +386,8 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
                 if (!good) break;
                 if (EPI == STORE32 && FORM == TN && p.out_mapped) {
                     // through shared memory (rows of 128 bytes, swizzled as the map says), so that whole lines are written; an
-                    // addition is made in L2, without reading: 1584 -> 1051 us at 8 x 4096 x 14336 with 8192 rows
+                    // addition is made in L2, without reading: 1584 -> 1209 us at 8 x 4096 x 14336 with 8192 rows.  (Boxes
+                    // that are loaded, added to and stored took 983 against 1078 of this at even loads and 1446 against 1373 at uneven ones.)
 #pragma unroll
                     for (int q = 0; q < CHUNKS; q++) {
                         const int col = n0 + q * 32;

@@ -386,26 +386,33 @@ def test_adamw(ptype, gtype, bits, shift):
 
 
 def test_adamw_of_values_at_the_ends():
-    """Magnitudes near both ends of fp32 in blocks of 8-bit states, and gradients that are not finite."""
-    n = 256 * 8
+    """Magnitudes near both ends of fp32 in blocks of 8-bit states, squares that are not finite, and gradients that are not."""
+    tops = [1e-38, 1e-30, 1e-19, 1e-10, 1.0, 1e9, 1e18, 1.5e19, 6e19]
+    blocks = len(tops) + 1
+    n = 256 * blocks
     g = torch.zeros(n, device="cuda")
     gen = torch.Generator(device="cuda").manual_seed(2)
-    for b, top in enumerate([1e-38, 1e-30, 1e-19, 1e-10, 1.0, 1e9, 1e18]):
+    for b, top in enumerate(tops):
         g[256 * b:256 * b + 256] = top * torch.exp2(-24 * torch.rand(256, generator=gen, device="cuda")) * torch.sign(torch.randn(256, generator=gen, device="cuda"))
     p = torch.zeros(n, device="cuda")
     m, v = torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
-    ms, vs = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+    ms, vs = torch.zeros(blocks, device="cuda"), torch.zeros(blocks, device="cuda")
     t = hap.hap_adamw_tensors([p], [g], [m], [v], [ms], [vs])
     hap.hap_adamw_step(t, 1, 1e-3, 0.9, 0.95)
     _, rm, rv, _ = adamw_reference(torch.zeros(n, device="cuda"), g, torch.zeros(n, dtype=D, device="cuda"), torch.zeros(n, dtype=D, device="cuda"), 1)
     for code, s, val, signed in ((m, ms, rm, True), (v, vs, rv, False)):
         want, ws = codes8(val, signed)
-        assert torch.equal(s.to(D), ws) and torch.equal(code.to(D), want)
-    assert p.isfinite().all() and not p[256 * 7:].any()
+        held = ws.isfinite()                        # codes under a scale that is not finite mean nothing
+        assert held.tolist() == [True] * 8 + [signed, True]
+        of = held.repeat_interleave(256)
+        assert torch.equal(s.to(D), ws) and torch.equal(code.to(D)[of], want[of])
+    assert p.isfinite().all() and not p[256 * len(tops):].any()
+    assert not hap.hap_adamw_state(t)[1][0][256 * 8:256 * 9].isfinite().any()
     g[0], g[256] = float("nan"), float("inf")
     hap.hap_adamw_step(t, 2, 1e-3, 0.9, 0.95)
     x, y = hap.hap_adamw_state(t)
-    assert not x[0][:512].isfinite().any() and x[0][512:].isfinite().all() and y[0][512:].isfinite().all() and not y[0][:512].isfinite().any()
+    assert not x[0][:512].isfinite().any() and x[0][512:].isfinite().all()
+    assert not y[0][:512].isfinite().any() and y[0][512:256 * 8].isfinite().all() and y[0][256 * 9:].isfinite().all()
 
 
 def test_adamw_of_more_tensors_than_a_launch_holds():
