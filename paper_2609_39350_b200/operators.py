@@ -124,7 +124,7 @@ def _check(status, what):
 def _now():
     """(current device, address of its current stream)"""
     here = torch.cuda.current_device()
-    return here, torch.cuda.current_stream(here).cuda_stream       # (asked for by number, a third of the time)
+    return here, torch._C._cuda_getCurrentRawStream(here)           # (the address alone: a microsecond less than a Stream object)
 
 
 def _offsets(offsets, here):

@@ -512,6 +512,25 @@ def test_repeated_captured_and_on_another_stream(name):
     assert hap.hap_operator_status() == 0
 
 
+def test_calls_on_two_streams_at_once():
+    """Kernels that fill the device, side by side on two streams with work of their own, small ones among them."""
+    table = calls()
+    flat = lambda r: [r] if isinstance(r, torch.Tensor) else list(r)  # noqa: E731
+    names = [n for n in table if not n.startswith("loss")]          # (the two loss calls share a workspace)
+    want = {n: [t.clone() for t in flat(table[n]())] for n in names}
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for turn in range(6):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for n in names if (turn + k) % 2 else names[::-1]:
+                    got.append((n, flat(table[n]())))
+    torch.cuda.synchronize()
+    for n, r in got:
+        assert all(torch.equal(a, b) for a, b in zip(want[n], r))
+    assert hap.hap_operator_status() == 0
+
+
 def test_stream_argument_and_captured_step():
     side = torch.cuda.Stream()
     x, w = normal(64, 128), normal(1, 64, 128, seed=1)
