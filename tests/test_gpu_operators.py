@@ -259,7 +259,7 @@ def test_linear_cross_entropy(rows, H, V, dtype):
 
 def test_loss_in_pieces_against_differences():
     """More than one piece of the vocabulary, and the gradients against differences of the loss."""
-    rows, H, V = 24700, 64, 4500                    # pieces are of 2048 columns here
+    rows, H, V = 24700, 64, 4500                    # pieces are of 3840 columns here
     x, w = normal(rows, H, dtype=FP), normal(V, H, seed=1, dtype=FP, scale=2.0 * H ** -0.5)
     target = torch.randint(0, V, (rows,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
     target[::11] = -1
