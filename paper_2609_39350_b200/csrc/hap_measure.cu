@@ -35,16 +35,18 @@ __global__ void fill_offsets_kernel(int64_t *p, int E, int64_t rows)
 }
 __global__ void fill_one_kernel(float *p, float x) { *p = x; }
 
-// Memory of a workspace in the order it is asked for; without one it only counts.
+// Memory of a workspace in the order it is asked for; without one it only counts.  Nothing may be launched on what was taken
+// unless all of it fits.
 struct Space {
     char *base;
-    uint64_t at = 0;
+    uint64_t bytes = 0, at = 0;
     template <typename T> T *take(uint64_t n)
     {
-        T *p = base ? (T *)(base + at) : nullptr;
+        const uint64_t from = at;
         at = (at + n * sizeof(T) + 255) / 256 * 256;
-        return p;
+        return base && at <= bytes ? (T *)(base + from) : nullptr;
     }
+    bool fits() const { return at <= bytes; }
 };
 
 int64_t shard(int64_t n, int64_t by) { const int64_t s = (n + by - 1) / by; return (s + 7) / 8 * 8; }       // a rank's share, as kernels like it
@@ -176,11 +178,23 @@ bool fits(const hap_model *m, const hap_profile *p)
 }
 
 int64_t tokens(const hap_model &m, int64_t b, int64_t cp) { const int64_t t = b * m.S / cp; return t < 1 ? 1 : t; }
-int least(const int32_t *l, int n) { int v = l[0]; for (int i = 1; i < n; i++) v = l[i] < v ? l[i] : v; return v; }
-int most(const int32_t *l, int n) { int v = l[0]; for (int i = 1; i < n; i++) v = l[i] > v ? l[i] : v; return v; }
+// f(index, tokens, TP) for every entry of the profile's tables
+template <typename F> void each_entry(const hap_model &m, const hap_profile &p, F &&f)
+{
+    for (int itp = 0; itp < p.ntp; itp++)
+        for (int icp = 0; icp < p.ncp; icp++)
+            for (int ib = 0; ib < p.nmb; ib++) f((itp * p.ncp + icp) * p.nmb + ib, tokens(m, p.mb_list[ib], p.cp_list[icp]), (int64_t)p.tp_list[itp]);
+}
+int64_t most_tokens(const hap_model &m, const hap_profile &p)
+{
+    int64_t most = 0;
+    each_entry(m, p, [&](int, int64_t t, int64_t) { most = t > most ? t : most; });
+    return most;
+}
+bool has_experts(const hap_model &m) { return m.E > 0 && m.k > 0 && m.F_exp > 0; }
 
 struct Share { int E; int64_t rows; };
-// of E experts' rows on one micro-batch, those of the measured rank, and twice as many
+// of E experts' rows on one micro-batch, those of the measured rank
 Share rank_share(const hap_model &m, int64_t toks)
 {
     const int e = m.E < RANK_EXPERTS ? m.E : RANK_EXPERTS;
@@ -193,21 +207,28 @@ Share rank_share(const hap_model &m, int64_t toks)
 extern "C" hap_status hap_measure_workspace(const hap_model *m, const hap_profile *p, uint64_t *host_bytes)
 {
     if (!host_bytes || !fits(m, p)) return HAP_E_INVALID;
-    const int64_t t = tokens(*m, most(p->mb_list, p->nmb), least(p->cp_list, p->ncp)), tp = least(p->tp_list, p->ntp);
-    if (t >= (1ll << 29)) return HAP_E_RANGE;
-    const int F = m->F_dense > m->F_exp ? m->F_dense : m->F_exp;
+    const int64_t most = most_tokens(*m, *p);
+    if (most >= (1ll << 29)) return HAP_E_RANGE;
     uint64_t need = 0;
     auto count = [&](auto &&make) {
         Space s{nullptr};
         make(s);
         need = s.at > need ? s.at : need;
     };
-    count([&](Space &s) { Block(s, t, m->H, (int)shard(F, tp), 1); });
-    if (m->E > 0 && m->k > 0 && m->F_exp > 0) {
-        const Share r = rank_share(*m, t);
-        count([&](Space &s) { Block(s, 2 * r.rows, m->H, (int)shard(m->F_exp, 1), r.E); });
+    // Everything that hap_measure_profile lays out.  The most tokens alone do not tell: the head's workspace is not monotone in
+    // its rows, and eta takes a block of the whole width, whatever the degrees are.
+    each_entry(*m, *p, [&](int, int64_t t, int64_t tp) {
+        for (int F : {m->F_dense, m->F_exp})
+            if (F > 0) count([&](Space &s) { Block(s, t, m->H, (int)shard(F, tp), 1); });
+        count([&](Space &s) { Head(s, t, m->H, shard(m->V, tp)); });
+    });
+    if (has_experts(*m)) {
+        const Share r = rank_share(*m, most);
+        const int F = (int)shard(m->F_exp, 1);
+        count([&](Space &s) { Block(s, most, m->H, F, 1); });
+        count([&](Space &s) { Block(s, r.rows, m->H, F, r.E); });
+        count([&](Space &s) { Block(s, 2 * r.rows, m->H, F, r.E); });
     }
-    count([&](Space &s) { Head(s, t, m->H, shard(m->V, tp)); });
     count([&](Space &s) { Update u(s); });
     *host_bytes = need;
     return HAP_OK;
@@ -237,8 +258,9 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
     auto block = [&](int64_t t, int F, int E, double &f, double &b) {
         for (int i = 0; E == 1 && i < n_blocks; i++)
             if (blocks[i].t == t && blocks[i].width == F) { f = blocks[i].f, b = blocks[i].b; return timer.status; }
-        Space sp{(char *)workspace};
+        Space sp{(char *)workspace, bytes};
         Block x(sp, t, m->H, F, E);
+        if (!sp.fits()) return HAP_E_INVALID;
         x.fill(s);
         f = timer.time([&] { return x.forward(stream); });
         b = timer.status == HAP_OK ? timer.time([&] { return x.backward(stream); }) : 0;
@@ -246,33 +268,34 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
         return timer.status;
     };
     hap_status bad = HAP_OK;
-    for (int itp = 0; itp < p->ntp && bad == HAP_OK; itp++)
-        for (int icp = 0; icp < p->ncp && bad == HAP_OK; icp++)
-            for (int ib = 0; ib < p->nmb && bad == HAP_OK; ib++) {
-                const int at = (itp * p->ncp + icp) * p->nmb + ib;
-                const int64_t t = tokens(*m, p->mb_list[ib], p->cp_list[icp]), V = shard(m->V, p->tp_list[itp]);
-                for (int kind = 0; kind < 2 && bad == HAP_OK; kind++) {
-                    const int F = kind == HAP_DENSE ? m->F_dense : m->F_exp;
-                    double f = 0, b = 0;
-                    if (F > 0) bad = block(t, (int)shard(F, p->tp_list[itp]), 1, f, b);
-                    out->tff[2 * at + kind] = f, out->tfb[2 * at + kind] = b;
-                }
-                if (bad != HAP_OK) break;
-                double f = -1;
-                for (int i = 0; i < n_heads; i++)
-                    if (heads[i].t == t && heads[i].width == V) f = heads[i].f;
-                if (f < 0) {
-                    Space sp{(char *)workspace};
-                    Head h(sp, t, m->H, V);
-                    h.fill(s);
-                    f = timer.time([&] { return h.run(stream); });
-                    if ((bad = timer.status) == HAP_OK && n_heads < most_known) heads[n_heads++] = {t, V, f, 0};
-                }
-                out->tpost[at] = f;
+    each_entry(*m, *p, [&](int at, int64_t t, int64_t tp) {
+        for (int kind = 0; kind < 2 && bad == HAP_OK; kind++) {
+            const int F = kind == HAP_DENSE ? m->F_dense : m->F_exp;
+            double f = 0, b = 0;
+            if (F > 0) bad = block(t, (int)shard(F, tp), 1, f, b);
+            out->tff[2 * at + kind] = f, out->tfb[2 * at + kind] = b;
+        }
+        if (bad != HAP_OK) return;
+        const int64_t V = shard(m->V, tp);
+        double f = -1;
+        for (int i = 0; i < n_heads; i++)
+            if (heads[i].t == t && heads[i].width == V) f = heads[i].f;
+        if (f < 0) {
+            Space sp{(char *)workspace, bytes};
+            Head h(sp, t, m->H, V);
+            if (!sp.fits()) {
+                bad = HAP_E_INVALID;
+                return;
             }
+            h.fill(s);
+            f = timer.time([&] { return h.run(stream); });
+            if ((bad = timer.status) == HAP_OK && n_heads < most_known) heads[n_heads++] = {t, V, f, 0};
+        }
+        out->tpost[at] = f;
+    });
     out->eta = 1, out->gamma = 0;
-    if (bad == HAP_OK && m->E > 0 && m->k > 0 && m->F_exp > 0) {
-        const int64_t t = tokens(*m, most(p->mb_list, p->nmb), least(p->cp_list, p->ncp));
+    if (bad == HAP_OK && has_experts(*m)) {
+        const int64_t t = most_tokens(*m, *p);
         const int F = (int)shard(m->F_exp, 1);
         const Share r = rank_share(*m, t);
         double f1 = 0, b1 = 0, f2 = 0, b2 = 0, f = 0, b = 0;
@@ -287,9 +310,9 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
         }
     }
     if (bad == HAP_OK) {
-        Space sp{(char *)workspace};
+        Space sp{(char *)workspace, bytes};
         Update u(sp);
-        bad = u.fill(s);
+        bad = sp.fits() ? u.fill(s) : HAP_E_INVALID;
         if (bad == HAP_OK) {
             out->copt = timer.time([&] { return u.run(stream); }) / (double)PARAMETERS;
             bad = timer.status;
