@@ -28,8 +28,10 @@ template <int EPI, int CG> struct Shape {
     static constexpr int STAGES = CG == 1 ? (EPI == STORE32 ? 3 : 4) : (EPI == STORE32 ? 5 : 6);
     // Tensor cores add to a sum by truncating: after n products of 16 steps it is short by about n 2^-25 of its magnitude (at
     // 3500 rows 2.4e-6, six times the error of sums rounded to nearest; 7.7e-7 this way).  Results that are kept in fp32 are summed over
-    // 1024 steps there, and these sums in registers, under the next products.
-    static constexpr bool SUMS = EPI == STORE32 || EPI == LSE;
+    // 1024 steps there, and these sums in registers, under the next products.  The logits of the loss's two passes have to be the
+    // same sums: what they are off by leaves in z - lse, and p - 1 of a row whose target leads is small (logits of 25 over 8192
+    // steps, one long sum in the backward pass: 9e-4 times the target's row in dx where 1e-8 is right).
+    static constexpr bool SUMS = EPI == STORE32 || EPI == LSE || EPI == DLOGIT;
     static constexpr int SUM_STEPS = 1024;
 };
 
