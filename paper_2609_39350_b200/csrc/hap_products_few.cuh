@@ -21,6 +21,17 @@ template <typename T> __device__ __forceinline__ void unpack8(const uint4 w, flo
     }
 }
 
+// Eight values from p on of which n are there, zeros behind them: the last ones one by one, since a row may end where its buffer does.
+__device__ __forceinline__ uint4 eight(const void *p, int n)
+{
+    if (n >= 8) return *(const uint4 *)p;
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int i = 0; i < 7; i++)
+        if (i < n) w[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << 16 * (i & 1);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 template <typename T, int EPI> __global__ void __launch_bounds__(256) few_rows_kernel(const __grid_constant__ Args p)
 {
     __shared__ int expert[FEW_ROWS], low[FEW_ROWS], high[FEW_ROWS], experts;
@@ -70,12 +81,9 @@ template <typename T, int EPI> __global__ void __launch_bounds__(256) few_rows_k
             for (int r = 0; r < FEW_ROWS; r++) {
                 if (r >= nr) break;
                 float y[8];
-                unpack8<T>(*(const uint4 *)(a + r * p.lda + at), y);
+                unpack8<T>(eight(a + r * p.lda + at, valid), y);
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    if (i >= valid) y[i] = x0[i] = x1[i] = 0.0f;        // (the last step's, where the length is no multiple of 8)
-                    s0[r] = fmaf(x0[i], y[i], s0[r]), s1[r] = fmaf(x1[i], y[i], s1[r]);
-                }
+                for (int i = 0; i < 8; i++) s0[r] = fmaf(x0[i], y[i], s0[r]), s1[r] = fmaf(x1[i], y[i], s1[r]);
             }
         };
         int at = lane * 8;
@@ -87,7 +95,7 @@ template <typename T, int EPI> __global__ void __launch_bounds__(256) few_rows_k
             for (int i = 0; i < 4; i++) step(q0[i], q1[i], at + i * 256, 8);
         }
 #pragma unroll 1
-        for (; at < p.kdim; at += 256) step(*(const uint4 *)(w0 + at), *(const uint4 *)(w1 + at), at, p.kdim - at);
+        for (; at < p.kdim; at += 256) step(eight(w0 + at, p.kdim - at), eight(w1 + at, p.kdim - at), at, p.kdim - at);
 #pragma unroll
         for (int r = 0; r < FEW_ROWS; r++) {
             if (r >= nr) break;
