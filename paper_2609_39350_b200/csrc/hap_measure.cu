@@ -51,11 +51,14 @@ struct Space {
 
 int64_t shard(int64_t n, int64_t by) { const int64_t s = (n + by - 1) / by; return (s + 7) / 8 * 8; }       // a rank's share, as kernels like it
 
+// The status of a CUDA call; a failed one's error is not left behind for the next launch to be blamed for.
+hap_status status_of(cudaError_t e) { return e == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA); }
+
 struct Timer {
     cudaStream_t stream;
     cudaEvent_t from = nullptr, to = nullptr;
     bool good;
-    explicit Timer(cudaStream_t s) : stream(s) { good = cudaEventCreate(&from) == cudaSuccess && cudaEventCreate(&to) == cudaSuccess; }
+    explicit Timer(cudaStream_t s) : stream(s) { good = status_of(cudaEventCreate(&from)) == HAP_OK && status_of(cudaEventCreate(&to)) == HAP_OK; }
     ~Timer() { if (from) cudaEventDestroy(from); if (to) cudaEventDestroy(to); }
     // median time of `run` in ns, < 0 on an error, whose status is kept
     hap_status status = HAP_OK;
@@ -64,9 +67,11 @@ struct Timer {
         double t[TIMES];
         for (int i = -1; i < TIMES; i++) {
             float ms = 0;
-            if (cudaEventRecord(from, stream) != cudaSuccess) status = HAP_E_CUDA;
+            status = status_of(cudaEventRecord(from, stream));
             if (status == HAP_OK) status = run();
-            if (status == HAP_OK && (cudaEventRecord(to, stream) != cudaSuccess || cudaEventSynchronize(to) != cudaSuccess || cudaEventElapsedTime(&ms, from, to) != cudaSuccess)) status = HAP_E_CUDA;
+            if (status == HAP_OK) status = status_of(cudaEventRecord(to, stream));
+            if (status == HAP_OK) status = status_of(cudaEventSynchronize(to));
+            if (status == HAP_OK) status = status_of(cudaEventElapsedTime(&ms, from, to));
             if (status != HAP_OK) return -1;
             if (i >= 0) t[i] = (double)ms * 1e6;
         }
@@ -153,7 +158,7 @@ struct Update {
     {
         fill_kernel<<<1024, 256, 0, st>>>((__nv_bfloat16 *)t.param, PARAMETERS, 0.02f, 7);
         fill_kernel<<<1024, 256, 0, st>>>((__nv_bfloat16 *)t.grad, PARAMETERS, 1e-3f, 8);
-        return cudaMemsetAsync(t.m, 0, PARAMETERS * 4, st) == cudaSuccess && cudaMemsetAsync(t.v, 0, PARAMETERS * 4, st) == cudaSuccess ? HAP_OK : HAP_E_CUDA;
+        return status_of(cudaMemsetAsync(t.m, 0, PARAMETERS * 4, st)) == HAP_OK ? status_of(cudaMemsetAsync(t.v, 0, PARAMETERS * 4, st)) : HAP_E_CUDA;
     }
     hap_status run(void *st)
     {
@@ -242,7 +247,7 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
     if (!out || !out->tff || !out->tfb || !out->tpost || !workspace || bytes < need || ((uintptr_t)workspace & 255)) return HAP_E_INVALID;
     cudaStream_t s = (cudaStream_t)stream;
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
+    if (status_of(cudaStreamIsCapturing(s, &capture)) != HAP_OK) return HAP_E_CUDA;
     if (capture != cudaStreamCaptureStatusNone) return HAP_E_STATE;
     Timer timer(s);
     if (!timer.good) return HAP_E_CUDA;

@@ -10,7 +10,22 @@
 using namespace hapop;
 
 
-static hap_status launched() { return cudaGetLastError() == cudaSuccess ? HAP_OK : HAP_E_CUDA; }
+// The status of a CUDA call.  A failed one also leaves its error behind, for whoever asks for the last error next: it is taken back.
+static hap_status status_of(cudaError_t e) { return e == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA); }
+// Launches, and says whether this launch was made, not whether any call so far left an error behind.  Arguments of the kernel's own
+// types are passed where they are, without a copy.
+template <typename T> struct Same { using type = T; };
+template <typename... P> static hap_status start(void (*kernel)(P...), const cudaLaunchConfig_t &c, const typename Same<P>::type &...args)
+{
+    void *at[] = {(void *)&args...};
+    return status_of(cudaLaunchKernelExC(&c, (const void *)kernel, at));
+}
+static cudaLaunchConfig_t shape_of(int64_t grid, int threads, int smem, cudaStream_t stream)
+{
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)grid), c.blockDim = dim3((unsigned)threads), c.dynamicSmemBytes = (size_t)smem, c.stream = stream;
+    return c;
+}
 
 // The current device and its multiprocessors; 0 of them: no device.  What does not change is asked once for each device.
 struct Device { int id = 0, sms = 0; };
@@ -20,10 +35,10 @@ static Device device()
 {
     static std::atomic<int> known[DEVICES];
     Device d;
-    if (cudaGetDevice(&d.id) != cudaSuccess || d.id < 0) return d;
+    if (status_of(cudaGetDevice(&d.id)) != HAP_OK || d.id < 0) return d;
     if (d.id < DEVICES) d.sms = known[d.id].load(std::memory_order_relaxed);
     if (d.sms) return d;
-    if (cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, d.id) != cudaSuccess) d.sms = 0;
+    if (status_of(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, d.id)) != HAP_OK) d.sms = 0;
     if (d.id < DEVICES) known[d.id].store(d.sms, std::memory_order_relaxed);
     return d;
 }
@@ -39,7 +54,7 @@ static EncodeTiled encode_tiled()
     static const EncodeTiled f = [] {
         void *fn = nullptr;
         cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) fn = nullptr;
+        if (status_of(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &r)) != HAP_OK || r != cudaDriverEntryPointSuccess) fn = nullptr;
         return (EncodeTiled)fn;
     }();
     return f;
@@ -60,15 +75,14 @@ static bool mappable(const void *base, int64_t ld) { return ((uintptr_t)base & 1
 
 // Launches a kernel that may start while its predecessor in the stream still ends: its setup (barriers, tensor memory, maps) and the
 // launch itself then cost nothing (loss of 129 rows: 28.7 -> 25.3 us).  The kernel waits for the predecessor before it reads.
-template <typename... P, typename... A> static hap_status launch_next(void (*kernel)(P...), int64_t grid, int threads, int smem, int cluster, cudaStream_t stream, const A &...args)
+template <typename... P> static hap_status launch_next(void (*kernel)(P...), int64_t grid, int threads, int smem, int cluster, cudaStream_t stream, const typename Same<P>::type &...args)
 {
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)grid), c.blockDim = dim3((unsigned)threads), c.dynamicSmemBytes = (size_t)smem, c.stream = stream;
+    cudaLaunchConfig_t c = shape_of(grid, threads, smem, stream);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization, attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension, attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
     c.attrs = attr, c.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&c, kernel, (P)args...) == cudaSuccess ? HAP_OK : (cudaGetLastError(), HAP_E_CUDA);
+    return start(kernel, c, args...);
 }
 
 // a persistent kernel of blocks or pairs of blocks, as many as fit and `most` tiles need
@@ -77,7 +91,7 @@ template <auto KERNEL, int CG = 2, int THREADS = 320, typename... A> static hap_
     static std::atomic<uint64_t> allowed;                   // devices on which the kernel may have this much shared memory
     const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
+        if (status_of(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != HAP_OK) return HAP_E_CUDA;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
     const int64_t at_once = d.sms / CG;
@@ -134,8 +148,7 @@ template <typename T, int FORM, int EPI> static hap_status launch_plain(const Ar
     const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, PM) : ceil_div(p.rows, PM) + p.groups);
     if (most > INT32_MAX) return HAP_E_RANGE;
-    plain_product_kernel<T, FORM, EPI><<<(unsigned)(most < 4 * sms ? most : 4 * sms), 256, 0, stream>>>(p);
-    return launched();
+    return start(plain_product_kernel<T, FORM, EPI>, shape_of(most < 4 * sms ? most : 4 * sms, 256, 0, stream), p);
 }
 
 template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
@@ -322,7 +335,7 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
     const int parts = (int)ceil_div(whole, split_k);
     if (twice)
         for (int i = 0; i < 2; i++)
-            if (cudaMemcpy2DAsync(x2 + i * rows * H8 * 2, H8 * 2, x, ldx * 2, (size_t)H * 2, (size_t)rows, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return cudaGetLastError(), HAP_E_CUDA;
+            if (status_of(cudaMemcpy2DAsync(x2 + i * rows * H8 * 2, H8 * 2, x, ldx * 2, (size_t)H * 2, (size_t)rows, cudaMemcpyDeviceToDevice, s)) != HAP_OK) return HAP_E_CUDA;
     for (int64_t c0 = 0; c0 < V; c0 += piece) {
         const int64_t cols = V - c0 < piece ? V - c0 : piece;
         const char *wc = (const char *)w + c0 * ldw * 2;
@@ -393,8 +406,7 @@ template <int N, typename F> static hap_status adamw_launches(const hap_adamw_te
             chunks += c;
         }
         if (!list.n) break;
-        launch(list, (unsigned)chunks);
-        const hap_status st = launched();
+        const hap_status st = launch(list, (int64_t)chunks);
         if (st != HAP_OK) return st;
     }
     return HAP_OK;
@@ -402,10 +414,9 @@ template <int N, typename F> static hap_status adamw_launches(const hap_adamw_te
 
 template <typename P, typename G> static hap_status adamw_run(const hap_adamw_tensor *tensors, int32_t n, int bits, const AdamwFactors &f, const float *grad_scale, cudaStream_t s)
 {
-    auto launch = [&](auto &list, unsigned chunks) {
+    auto launch = [&](auto &list, int64_t chunks) {
         constexpr int N = sizeof(list.t) / sizeof(AdamwTensor);
-        if (bits == 8) adamw8_kernel<P, G, N><<<chunks, 256, 0, s>>>(list, f, grad_scale);
-        else adamw_kernel<P, G, N><<<chunks, 256, 0, s>>>(list, f, grad_scale);
+        return start(bits == 8 ? adamw8_kernel<P, G, N> : adamw_kernel<P, G, N>, shape_of(chunks, 256, 0, s), list, f, grad_scale);
     };
     return n <= FEW ? adamw_launches<FEW>(tensors, n, nullptr, nullptr, launch) : adamw_launches<MANY>(tensors, n, nullptr, nullptr, launch);
 }
@@ -446,9 +457,9 @@ extern "C" hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n
         if ((host_m && !aligned(host_m[i], 4)) || (host_v && !aligned(host_v[i], 4))) return HAP_E_INVALID;
     }
     cudaStream_t s = (cudaStream_t)stream;
-    auto launch = [&](auto &list, unsigned chunks) {
+    auto launch = [&](auto &list, int64_t chunks) {
         constexpr int N = sizeof(list.t) / sizeof(AdamwTensor);
-        adamw_values_kernel<N><<<chunks, 256, 0, s>>>(list);
+        return start(adamw_values_kernel<N>, shape_of(chunks, 256, 0, s), list);
     };
     return n <= FEW ? adamw_launches<FEW>(tensors, n, host_m, host_v, launch) : adamw_launches<MANY>(tensors, n, host_m, host_v, launch);
 }
@@ -458,6 +469,6 @@ extern "C" hap_status hap_operator_status(uint32_t *host_bits)
     if (!host_bits) return HAP_E_INVALID;
     *host_bits = 0;
     const unsigned zero = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(host_bits, operator_error, sizeof zero) != cudaSuccess) return HAP_E_CUDA;
-    return cudaMemcpyToSymbol(operator_error, &zero, sizeof zero) == cudaSuccess ? HAP_OK : HAP_E_CUDA;
+    if (status_of(cudaDeviceSynchronize()) != HAP_OK || status_of(cudaMemcpyFromSymbol(host_bits, operator_error, sizeof zero)) != HAP_OK) return HAP_E_CUDA;
+    return status_of(cudaMemcpyToSymbol(operator_error, &zero, sizeof zero));
 }
