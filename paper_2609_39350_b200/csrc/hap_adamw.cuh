@@ -32,10 +32,13 @@ template <int N> __device__ __forceinline__ int adamw_tensor(const AdamwList<N> 
 }
 
 __device__ __forceinline__ float root_of(float x) { float y; asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-// (a root and a quotient that are off by a unit or two in the last place: the parameter's own rounding is larger or as large)
-__device__ __forceinline__ float adamw_value(float p, float m, float v, const AdamwFactors &f)
+// The new parameter.  Held in 16 bits it is rounded by more than a root and a quotient that are off by a unit or two in the last
+// place; held in 32 it may be the update and little else (weights that begin at 0), and both are rounded to nearest.  (100 M
+// parameters in 32 bits: 412 us either way with states in 32 bits, 346 against 318 in 8.)
+template <typename P> __device__ __forceinline__ float adamw_value(float p, float m, float v, const AdamwFactors &f)
 {
-    return p * f.decay - __fdividef(f.step * m, root_of(v) * f.root + f.eps);
+    if constexpr (sizeof(P) == 4) return p * f.decay - __fdiv_rn(f.step * m, __fsqrt_rn(v) * f.root + f.eps);
+    else return p * f.decay - __fdividef(f.step * m, root_of(v) * f.root + f.eps);
 }
 __device__ __forceinline__ float adamw_read_m(float c, float s)
 {
@@ -112,7 +115,7 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
         const float x = to_float(g[i]) * scale;
         const float mi = adamw_first(m[i], x, f), vi = adamw_second(v[i], x, f);
         m[i] = mi, v[i] = vi;
-        const float y = adamw_value(to_float(p[i]), mi, vi, f);
+        const float y = adamw_value<P>(to_float(p[i]), mi, vi, f);
         p[i] = from_float<P>(y);
         if (copy) adamw_copy(copy, f.copy16, i, y);
     };
@@ -132,7 +135,7 @@ template <typename P, typename G, int N> __global__ void __launch_bounds__(256) 
         for (int j = 0; j < 8; j++) {
             x[j] *= scale;
             a[j] = adamw_first(a[j], x[j], f), b[j] = adamw_second(b[j], x[j], f);
-            y[j] = adamw_value(y[j], a[j], b[j], f);
+            y[j] = adamw_value<P>(y[j], a[j], b[j], f);
         }
         store8(m + at, a), store8(v + at, b), store8(p + at, y);
         if (copy) copy8(copy, f.copy16, at, y);
@@ -200,7 +203,7 @@ template <typename P, typename G, bool EIGHTS, bool WHOLE> __device__ __forceinl
         if (!WHOLE && at(j) >= n) x[j] = 0.0f;
         a[j] = adamw_first(adamw_read_m(a[j], ms), x[j], f);
         b[j] = adamw_second(adamw_read_v(b[j], vs), x[j], f);
-        y[j] = adamw_value(y[j], a[j], b[j], f);
+        y[j] = adamw_value<P>(y[j], a[j], b[j], f);
         if (WHOLE || at(j) < n) mt = max(mt, magnitude(a[j])), vt = max(vt, magnitude(b[j]));
     }
     if (EIGHTS) {
