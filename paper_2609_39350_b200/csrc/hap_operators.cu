@@ -145,17 +145,21 @@ template <typename T, int FORM, int EPI> static hap_status launch_experts(Args p
 
 template <typename T, int FORM, int EPI> static hap_status launch_plain(const Args &p, int sms, cudaStream_t stream)
 {
+    if (EPI == SUM32 && p.splits > 1) return HAP_E_INVALID;                     // (it makes one sum)
     const int64_t cols = ceil_div(p.ncols, EPI == GATED ? TILE_N / 2 : TILE_N);
     const int64_t most = cols * (FORM == TN ? p.groups * ceil_div(p.mdim, PM) : ceil_div(p.rows, PM) + p.groups);
     if (most > INT32_MAX) return HAP_E_RANGE;
     return start(plain_product_kernel<T, FORM, EPI>, shape_of(most < 4 * sms ? most : 4 * sms, 256, 0, stream), p);
 }
 
+// whether a product runs on the tensor cores, or in the plain kernel
+static bool on_tensor_cores(const Args &p) { return p.rows > 0 && mappable(p.a, p.lda) && mappable(p.b, p.ldb) && p.bgroup < (1ll << 36) && encode_tiled(); }
+
 template <typename T, int FORM, int EPI> static hap_status launch_product(const Args &p, cudaStream_t stream)
 {
     const Device d = device();
     if (!d.sms) return HAP_E_CUDA;
-    if (p.rows == 0 || !mappable(p.a, p.lda) || !mappable(p.b, p.ldb) || p.bgroup >= (1ll << 36) || !encode_tiled()) return launch_plain<T, FORM, EPI>(p, d.sms, stream);
+    if (!on_tensor_cores(p)) return launch_plain<T, FORM, EPI>(p, d.sms, stream);
     if constexpr (FORM != TN && (EPI == STORE || EPI == GATED || EPI == GATED_BACK)) {
         if constexpr (FORM == NT) {
             if (p.rows <= FEW_ROWS) {
@@ -329,9 +333,11 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
     char *d = (char *)workspace, *x2 = d + at.x2;
     float *acc = (float *)(d + at.acc), *residual = (float *)(d + at.residual);
     const bool twice = rows <= TWICE_ROWS && rows > 0 && dw;
-    // parts of dx's contraction, of the same length in every piece, so that none is empty and those of a later, shorter piece are
-    // among the first one's (the plain kernel makes one sum)
-    const int64_t whole = V < piece ? V : piece, split_k = ceil_div(ceil_div(whole, mappable(w, ldw) ? parts_of_dx(rows, H, piece) : 1), BK) * BK;
+    Args of_dx{};                                           // dx's product, but for the piece
+    of_dx.groups = 1, of_dx.rows = (int)rows, of_dx.ncols = H, of_dx.a = d, of_dx.lda = piece, of_dx.b = w, of_dx.ldb = ldw;
+    // parts of its contraction, of the same length in every piece, so that none is empty and those of a later, shorter piece are
+    // among the first one's (the plain kernel makes one sum; a piece begins at a multiple of 512 bytes of w, so all run as the first)
+    const int64_t whole = V < piece ? V : piece, split_k = ceil_div(ceil_div(whole, on_tensor_cores(of_dx) ? parts_of_dx(rows, H, piece) : 1), BK) * BK;
     const int parts = (int)ceil_div(whole, split_k);
     if (twice)
         for (int i = 0; i < 2; i++)
@@ -349,9 +355,8 @@ extern "C" hap_status hap_linear_cross_entropy_backward(int32_t dtype, int64_t r
             st = HAP_BY_TYPE(NT, DLOGIT);
         }
         if (st == HAP_OK && dx && rows > 0) {
-            Args p{};
-            p.groups = 1, p.rows = (int)rows, p.ncols = H, p.kdim = (int)cols;
-            p.a = d, p.b = wc, p.lda = piece, p.ldb = ldw;
+            Args p = of_dx;
+            p.kdim = (int)cols, p.b = wc;
             const bool last = c0 + cols == V;
             p.splits = (int)ceil_div(cols, split_k), p.split_k = (int)split_k;
             p.out = dx, p.ldo = lddx, p.acc32 = acc, p.first = c0 == 0, p.last = last && parts == 1;
