@@ -302,6 +302,10 @@ class HapAdamWTensors:
                 if t.numel() != (-(-p.numel() // 256) if name.endswith("scale") else p.numel()):
                     _refuse(f"{name}: of another size than its parameter asks for")
             at[name] = [t.data_ptr() for t in tensors]
+            if name != "grads":                         # (weights that are tied are one tensor; two steps at once on it would race)
+                used = [a for a, t in zip(at[name], tensors) if t.numel()]
+                if len(set(used)) != len(used):
+                    _refuse(f"{name}: the same tensor twice")
         for i, p in enumerate(params):
             d = self.array[i]
             d.param, d.grad, d.m, d.v, d.m_scale, d.v_scale, d.copy = (at[k][i] for k in ("params", "grads", "m", "v", "m_scale", "v_scale", "copies"))

@@ -28,3 +28,18 @@ def test_status_asked_for_during_a_capture():
     assert (p < -0.49).all()
     assert (hap.hap_expert_matmul(x, w, off) == 13).all()
     assert hap.hap_operator_status() == 0
+
+
+def test_the_same_tensor_twice_is_refused():
+    """Tied weights listed twice, and states shared by two parameters, would be stepped twice at once."""
+    p, q = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda")
+    g, none = torch.ones(300, device="cuda"), torch.zeros(0, device="cuda")
+    m, v, n, w = (torch.zeros(300, device="cuda") for _ in range(4))
+    c = torch.zeros(300, device="cuda", dtype=torch.bfloat16)
+    for args in (([p, p], [g, g], [m, n], [v, w]), ([p, q], [g, g], [m, m], [v, w]), ([p, q], [g, g], [m, n], [w, w])):
+        with pytest.raises(hap.HapError):
+            hap.hap_adamw_tensors(*args)
+    with pytest.raises(hap.HapError):
+        hap.hap_adamw_tensors([p, q], [g, g], [m, n], [v, w], copies=[c, c])
+    hap.hap_adamw_step(hap.hap_adamw_tensors([p, none, q, none], [g, none, g, none], [m, none, n, none], [v, none, w, none]), 1, 0.5)
+    assert torch.equal(p, q) and (p < -0.49).all()
