@@ -477,3 +477,23 @@ extern "C" hap_status hap_operator_status(uint32_t *host_bits)
     if (status_of(cudaDeviceSynchronize()) != HAP_OK || status_of(cudaMemcpyFromSymbol(host_bits, operator_error, sizeof zero)) != HAP_OK) return HAP_E_CUDA;
     return status_of(cudaMemcpyToSymbol(operator_error, &zero, sizeof zero));
 }
+
+#ifdef HAP_CHECKED
+// Self-checking build: the operators' bounded wait on a barrier that nothing arrives at, for `limit` ns (a second at most), by one warp.
+__global__ void wait_check_kernel(uint64_t limit)
+{
+    __shared__ uint64_t bar;
+    __shared__ int stop;
+    if (threadIdx.x == 0) {
+        bar_init(&bar, 1);
+        stop = 0;
+    }
+    __syncthreads();
+    bar_wait_long(smem_u32(&bar), 0, &stop, limit);
+}
+extern "C" hap_status hap_operator_wait_check(uint64_t limit, void *stream)
+{
+    if (limit > 1000000000ull) return HAP_E_INVALID;
+    return start(wait_check_kernel, shape_of(1, 32, 0, (cudaStream_t)stream), limit);
+}
+#endif
