@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(320, 1) expert_kernel(const __grid_constant__ 
                 __syncwarp();
             }
         }
+        if (good) wait_for_empty<S::STAGES>(sh.empty, at, stop);
         if (*stop && rank == 0) drain(sh.full, at, S::STAGES);
     } else if (warp == 1) {
         if (rank == 0) {

@@ -186,6 +186,14 @@ __device__ __noinline__ void drain(uint64_t *full, uint32_t at, uint32_t stages)
     }
 }
 
+// The products of a pair arrive at the barriers of both blocks: one whose last stages' arrivals are still on their way must not
+// leave its memory.  (What the epilogue waits for comes behind them, but by another barrier.)
+template <int STAGES> __device__ __forceinline__ void wait_for_empty(uint64_t *empty, uint32_t at, volatile int *stop)
+{
+    for (uint32_t i = at; i < at + STAGES; i++)
+        if (!bar_wait(&empty[i % STAGES], (i / STAGES + 1) & 1, stop)) break;
+}
+
 // Shared-memory descriptor under the 128-byte swizzle; lead, stride: bytes between the 1024-byte pieces of 8 rows (K-major: stride
 // along the rows, lead unused; MN-major: stride along the contraction, lead between strips of 64 columns).
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride)
@@ -283,6 +291,7 @@ __global__ void __launch_bounds__(FORM == TN ? 352 : 320, 1) product_kernel(cons
                 __syncwarp();
             }
         }
+        if (CG == 2 && good) wait_for_empty<S::STAGES>(sh.empty, at, stop);
         if (*stop && rank == 0) drain(sh.full, at, S::STAGES);
     } else if (warp == 1) {
         if (rank == 0) {
