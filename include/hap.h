@@ -424,7 +424,8 @@ hap_status hap_launches_per_pass(hap_problem *, uint32_t *host_count);
  *  - They are asynchronous on `stream`, allocate nothing, and may be captured: a captured call replays with the addresses
  *    and numbers it was given.  Calls on different streams may run at the same time; each has its own workspace then.
  *  - Sums are kept in fp32 and rounded once to the output's type.  The order of additions is fixed: the same call gives the
- *    same bits.
+ *    same bits.  The tensor cores truncate as they add: a sum of n steps of one sign is short by up to about n 2^-29 of itself (6e-5
+ *    for 32768, below a 16-bit result's rounding); fp32 results and logits are sums of 1024 steps each, added to nearest.
  *  - Operands whose addresses and row distances are multiples of 16 bytes run on the tensor cores; others on a plain
  *    kernel with the same results up to the order of additions, at a small part of the speed. */
 enum { HAP_BF16 = 0, HAP_FP16 = 1, HAP_FP32 = 2 };   /* element types */
@@ -509,9 +510,11 @@ hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *co
  *             with an equal share of k b S rows, over that rank's time; at most 1
  *   gamma     what that rank's time grows by when its rows are doubled (rho = 2), 0 .. 1
  *   copt      ns per parameter of an AdamW step, bf16 parameters and gradients with 32-bit states
- * Attention, embedding, router and links are not measured.  Runs on `stream` and waits for it; refuses a stream that is being
- * captured with HAP_E_STATE.  Workspace: hap_measure_workspace bytes of 256-byte aligned device memory (some GB for large
- * models). */
+ * Attention, embedding, router and links are not measured.  The runs of an entry are of the same operands, each waited for:
+ * what fits stays in L2, a short block's time holds its launches, and the clock is that of single runs (under lasting load
+ * the products are 15 to 25 % slower, by the power limit).  Runs on `stream` and waits for it; refuses a stream that is being
+ * captured with HAP_E_STATE.  Workspace: hap_measure_workspace bytes of 256-byte aligned device memory, the largest of what is
+ * laid out for one entry (GBs for large models: one block of F_exp is measured undivided whatever the TP degrees are). */
 typedef struct { double *tff, *tfb, *tpost; double eta, gamma, copt; } hap_measured;
 hap_status hap_measure_workspace(const hap_model *, const hap_profile *, uint64_t *host_bytes);
 hap_status hap_measure_profile(const hap_model *, const hap_profile *, hap_measured *host_out, void *dev_workspace, uint64_t bytes,

@@ -2,6 +2,10 @@
 
 Every function enqueues on `stream` (default: the current stream of the current device) and returns without waiting.  Tensors
 live on the current device; rows may be a distance apart (a slice of a wider matrix), elements of a row are side by side.
+
+The functions read and write memory and record nothing: an output does not require a gradient even where an input does.  The
+gradients are functions of their own here, to be called from the backward of whatever the caller differentiates.  A kernel whose
+wait ran out ends early with its outputs unfinished, which only hap_operator_status tells, since it has to wait for the device.
 """
 from __future__ import annotations
 
@@ -321,7 +325,7 @@ class HapAdamWTensors:
 def hap_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None) -> HapAdamWTensors:
     """Descriptors for hap_adamw_step: contiguous tensors, one gradient and two states each; states are fp32, or int8 and uint8
     with fp32 scales of ceil(n / 256) values.  copies: 16-bit tensors that get fp32 parameters rounded.  The object holds the
-    addresses, and the tensors: make it again when a gradient is another tensor."""
+    addresses, and the tensors: make it again when a gradient is another tensor (6 us a parameter).  Only gradients may be listed twice."""
     return HapAdamWTensors(params, grads, m, v, m_scale, v_scale, copies)
 
 
