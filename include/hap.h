@@ -500,6 +500,85 @@ hap_status hap_adamw_step(const hap_adamw_tensor *tensors, int32_t n, int32_t pa
                           const float *dev_grad_scale, void *stream);
 hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *const *host_m, float *const *host_v, void *stream);
 
+/* ---- A token's way to the experts and back, embedding, norms ---------------------------------------------------------------
+ * As the operators above: no handle, device pointers, asynchronous on `stream`, capturable, nothing allocated; and here element
+ * types may be HAP_FP32 too.  Rows may be any distance apart (ld >= the row's length, in elements); where addresses and distances
+ * are multiples of 16 bytes, memory is read and written in such pieces, otherwise value by value at about half the speed.
+ *
+ * Routing: the k of E experts that a row goes to, from its logits z [rows][E].  Scores s = softmax(z) (HAP_SOFTMAX) or
+ * 1 / (1 + exp(-z)) (HAP_SIGMOID); values v = s + bias (fp32 [E], nullable: then experts are in the order of z).  With groups > 1
+ * the experts are that many groups of E / groups that follow one another; a group's value is the sum of its group_best largest v
+ * (of as many as there are), and experts are chosen from the kept_groups groups of the largest values.  Chosen are the k largest v,
+ * written in descending order; equal ones in the order of their index.  Values are compared as the numbers they are: what 32 bits
+ * cannot tell apart is computed in 64.  weight_j = scale s_j, with renormalise scale s_j / (sum of the row's chosen s).
+ * An expert whose logit or bias is -inf is never chosen, nor is a group that has no others; where fewer than k experts are left
+ * the rest of a row's are -1 with weight 0.  A row with a NaN, with a logit +inf under HAP_SOFTMAX, or under a bias that is NaN or
+ * +inf, has no order: its experts are 0 .. k-1 and its weights NaN.
+ * experts int32 [rows][k], weights fp32 [rows][k].  1 <= E <= 1024, 1 <= k <= min(E, 32), 1 <= groups <= 32 dividing E,
+ * 1 <= kept_groups <= groups, 1 <= group_best.
+ * The backward pass gives dlogits [rows][E] (of the logits' type; may not overlap them) from dweights; the bias and the choice have no gradient.
+ * Experts that are not among 0 .. E-1 add nothing; groups are not looked at. */
+enum { HAP_SOFTMAX = 0, HAP_SIGMOID = 1 };
+typedef struct {
+    int32_t E, k, scores, groups, kept_groups, group_best, renormalise;
+    float scale;
+} hap_routing;
+hap_status hap_route(const hap_routing *, int32_t dtype, int64_t rows, const void *dev_logits, int64_t ld, const float *dev_bias,
+                     int32_t *dev_experts, float *dev_weights, void *stream);
+hap_status hap_route_backward(const hap_routing *, int32_t dtype, int64_t rows, const void *dev_logits, int64_t ld,
+                              const int32_t *dev_experts, const float *dev_dweights, void *dev_dlogits, int64_t ldd, void *stream);
+
+/* The order of the chosen (row, j) by expert, as hap_expert_matmul wants rows: a rank has the experts first .. first + E - 1.
+ * offsets int64 [E+1]: the places at which each expert's rows begin, and their number; places int32 [rows][k]: the place of each
+ * chosen (row, j), equal experts in the order of row k + j, -1 where the expert is not among the rank's (it may be any number).
+ * 1 <= E <= 1024, 1 <= k <= 32, rows k < 2^31.  Workspace: hap_expert_order_workspace bytes, 256-byte aligned, during the call. */
+hap_status hap_expert_order_workspace(int64_t rows, int32_t k, int32_t E, uint64_t *host_bytes);
+hap_status hap_expert_order(int64_t rows, int32_t k, int32_t first, int32_t E, const int32_t *dev_experts, int64_t *dev_offsets,
+                            int32_t *dev_places, void *dev_workspace, uint64_t bytes, void *stream);
+/* out[places[i][j]] = x[i] for the places in 0 .. placed - 1 (out [placed][H]); other rows of out are left as they are.  A place that
+ * is there twice gets one of its rows.  Its gradient is hap_expert_combine without weights. */
+hap_status hap_expert_dispatch(int32_t dtype, int64_t rows, int32_t k, int32_t H, int64_t placed, const void *dev_x, int64_t ldx,
+                               const int32_t *dev_places, void *dev_out, int64_t ldo, void *stream);
+/* out[i] = base[i] + sum_j weights[i][j] y[places[i][j]] over the places in 0 .. placed - 1 (y [placed][H]), in the order of j, rounded
+ * once.  base nullable (0), may be out; weights fp32 [rows][k], nullable (1).  Rows of y that no place names are not read. */
+hap_status hap_expert_combine(int32_t dtype, int64_t rows, int32_t k, int32_t H, int64_t placed, const void *dev_y, int64_t ldy,
+                              const int32_t *dev_places, const float *dev_weights, const void *dev_base, int64_t ldbase,
+                              void *dev_out, int64_t ldo, void *stream);
+/* dy[places[i][j]] = weights[i][j] dout[i] (nullable; other rows are left as they are) and dweights[i][j] = <dout[i],
+ * y[places[i][j]]> (fp32 [rows][k], nullable; 0 without a place; y is read for it alone).  dy may be y: a row is read first. */
+hap_status hap_expert_combine_backward(int32_t dtype, int64_t rows, int32_t k, int32_t H, int64_t placed, const void *dev_dout,
+                                       int64_t lddout, const void *dev_y, int64_t ldy, const int32_t *dev_places,
+                                       const float *dev_weights, void *dev_dy, int64_t lddy, float *dev_dweights, void *stream);
+
+/* Embedding: out[i] = scale w[tokens[i] - first] with w [V][H], 0 where that is not a row of w (a rank with a slice of the
+ * vocabulary; a padded token); tokens int64 [n].  Its gradient dw[v] = scale sum of dy[i] over the i with tokens[i] - first = v, in
+ * the order of i: sums in fp32, of up to 32 tokens each and then of these, rounded once to out_dtype (dtype or HAP_FP32).
+ * Without accumulate all of dw is written; with it, what the sums are added to, and rows of no token are left as they are.
+ * n < 2^31, V < 2^28.  Workspace: hap_embedding_backward_workspace bytes, 256-byte aligned, during the call. */
+hap_status hap_embedding(int32_t dtype, int64_t n, int32_t H, int64_t V, int64_t first, const int64_t *dev_tokens, const void *dev_w,
+                         int64_t ldw, float scale, void *dev_out, int64_t ldo, void *stream);
+hap_status hap_embedding_backward_workspace(int64_t n, int32_t H, int64_t V, uint64_t *host_bytes);
+hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, int32_t accumulate, int64_t n, int32_t H, int64_t V, int64_t first,
+                                  const int64_t *dev_tokens, const void *dev_dy, int64_t lddy, float scale, void *dev_dw, int64_t lddw,
+                                  void *dev_workspace, uint64_t bytes, void *stream);
+
+/* Layer norm: y = (x - mean) rstd w + b, rstd = 1 / sqrt(variance + eps) over each row's H values; with centred = 0 the mean counts as 0
+ * (and is not written).  w, b of param_dtype (dtype or HAP_FP32), nullable (1, 0); mean, rstd fp32 [rows], nullable, what the backward
+ * pass needs.  Statistics in fp32, the variance from differences to the mean.
+ * Backward: dx = base + rstd (g - mean(g) - xh mean(g xh)) with g = dy w, xh = (x - mean) rstd (base nullable: the gradient of the
+ * residual stream; with centred = 0 without mean(g)); dw = sum dy xh, db = sum dy over the rows, of grad_dtype (param_dtype or
+ * HAP_FP32), added to what they hold with accumulate.  dx, dw, db nullable; dx may be dy or base.  H <= 16384.
+ * Workspace: hap_layer_norm_backward_workspace bytes, 256-byte aligned, during the call; needed where dw or db is. */
+hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t centred, int64_t rows, int32_t H, const void *dev_x, int64_t ldx,
+                          const void *dev_w, const void *dev_b, float eps, void *dev_y, int64_t ldy, float *dev_mean, float *dev_rstd,
+                          void *stream);
+hap_status hap_layer_norm_backward_workspace(int64_t rows, int32_t H, uint64_t *host_bytes);
+hap_status hap_layer_norm_backward(int32_t dtype, int32_t param_dtype, int32_t grad_dtype, int32_t accumulate, int32_t centred,
+                                   int64_t rows, int32_t H, const void *dev_dy, int64_t lddy, const void *dev_x, int64_t ldx,
+                                   const void *dev_w, const float *dev_mean, const float *dev_rstd, const void *dev_base,
+                                   int64_t ldbase, void *dev_dx, int64_t lddx, void *dev_dw, void *dev_db, void *dev_workspace,
+                                   uint64_t bytes, void *stream);
+
 /* Times of the operators on the current device, as profile entries of a device type (the paper's first step, profiling, for
  * the device the library runs on).  Read from the model: S, H, E, k, F_dense, F_exp, V, beta (2: bf16); from the profile: the
  * lists of TP, CP and micro-batch.  Measured, with CUDA events, the median of five runs after one that is not counted:

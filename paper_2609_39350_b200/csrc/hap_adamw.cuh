@@ -7,7 +7,7 @@
 // keeps a code of at least 1.  Everything up to the codes is one IEEE operation per operator, rounded to nearest, so codes
 // are the same wherever they are computed.
 #pragma once
-#include "hap_products.cuh"
+#include "hap_values.cuh"
 #include "../../include/hap.h"
 
 namespace hapop {
@@ -65,39 +65,11 @@ __device__ __forceinline__ void adamw_copy(void *copy, int fp16, uint64_t i, flo
     else ((__nv_bfloat16 *)copy)[i] = __float2bfloat16_rn(x);
 }
 
-// eight values side by side, at an address that is a multiple of 16 bytes
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    } else {
-        const uint4 a = *(const uint4 *)p;
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float2 f = unpack2(w[i], T());
-            x[2 * i] = f.x, x[2 * i + 1] = f.y;
-        }
-    }
-}
-template <typename T> __device__ __forceinline__ void store8(T *p, const float (&x)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-        ((float4 *)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        ((float4 *)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-    } else {
-        *(uint4 *)p = make_uint4(pack2(x[0], x[1], T()), pack2(x[2], x[3], T()), pack2(x[4], x[5], T()), pack2(x[6], x[7], T()));
-    }
-}
 __device__ __forceinline__ void copy8(void *copy, int fp16, uint64_t i, const float (&x)[8])
 {
     if (fp16) store8((__half *)copy + i, x);
     else store8((__nv_bfloat16 *)copy + i, x);
 }
-// values in front of the first one whose address, and those of the following eights, is a multiple of 16 bytes
-template <typename T> __device__ __forceinline__ int in_front(const T *p) { return (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)); }
-
 // States in 32 bits: 12 to 30 bytes a value and nothing else to do; bound by memory.  Tensors that begin at the same odd place in
 // all of their buffers (views of flat buffers) move in eights from the first aligned value on; others value by value.
 template <typename P, typename G, int N> __global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ AdamwList<N> list, AdamwFactors f, const float *grad_scale)

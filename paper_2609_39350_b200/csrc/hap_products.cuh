@@ -5,10 +5,7 @@
 //   TN  out_e[m][n] = sum over rows i of group e of a[i][m] b[i][n]   (gradient of the weight)
 // Group e holds rows offsets[e] .. offsets[e+1]; without offsets there is one group of all rows.
 #pragma once
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <cuda_runtime.h>
-#include <stdint.h>
+#include "hap_values.cuh"
 
 namespace hapop {
 
@@ -65,23 +62,6 @@ struct Args {
     int first, last;
     int splits, split_k;            // SUM32: the contraction in this many parts of split_k, each with sums of its own in acc32
 };
-
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(float x) { return x; }
-// A kernel that was launched with its predecessor's end still ahead (see launch_next) starts by letting its successor do the same,
-// and touches no memory that others write before the predecessor's work is whole.
-__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ float from_float(float x) { return x; }
-__device__ __forceinline__ uint32_t pack2(float x, float y, __nv_bfloat16) { __nv_bfloat162 v = __floats2bfloat162_rn(x, y); return *(uint32_t *)&v; }
-__device__ __forceinline__ uint32_t pack2(float x, float y, __half) { __half2 v = __floats2half2_rn(x, y); return *(uint32_t *)&v; }
-__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) { return __bfloat1622float2(*(__nv_bfloat162 *)&w); }
-__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*(__half2 *)&w); }
 
 // 32 consecutive values of a row, as many as the row has: in 16-byte pieces where the address allows
 template <typename T> __device__ __forceinline__ void store32(T *p, const float (&v)[32], int n)
