@@ -12,7 +12,8 @@ constexpr int MOST_NORM = 16384;        // columns
 struct NormArgs {
     int64_t rows;
     int H, blocks, add;             // blocks: of the backward pass, each with partial sums of its own; add: to what dw and db hold
-    float eps;
+    int ahead;                      // backwards: 1 where the next row is brought while one is worked on
+    float eps, inverse;             // inverse: 1 / H
     const void *x, *w, *b, *dy, *base;
     int64_t ldx, ldy, lddy, ldbase, lddx;
     void *y, *dx, *dw, *db;
@@ -20,7 +21,7 @@ struct NormArgs {
     float *parts;                   // [blocks][1 or 2][H]
 };
 
-// the sum over a row's threads, LANES of them: a warp, or a block's warps through shared memory
+// Sums over a row's threads: of a warp, or of a block's warps through shared memory, where every thread reads all of them.
 template <int N> __device__ __forceinline__ void row_sums(float (&s)[N], int threads, float (*space)[32])
 {
 #pragma unroll
@@ -28,125 +29,222 @@ template <int N> __device__ __forceinline__ void row_sums(float (&s)[N], int thr
 #pragma unroll
         for (int d = 16; d; d /= 2) s[i] += __shfl_xor_sync(~0u, s[i], d);
     if (threads <= 32) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0)
+    if ((threadIdx.x & 31) == 0)
 #pragma unroll
-        for (int i = 0; i < N; i++) space[i][warp] = s[i];
+        for (int i = 0; i < N; i++) space[i][threadIdx.x >> 5] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-        s[i] = lane < threads / 32 ? space[i][lane] : 0.0f;
+    for (int i = 0; i < N; i++) s[i] = 0;
+    for (int w = 0; w < threads / 32; w += 4)               // (a row's warps are a multiple of four here, or the rest is 0)
 #pragma unroll
-        for (int d = 16; d; d /= 2) s[i] += __shfl_xor_sync(~0u, s[i], d);
-    }
+        for (int i = 0; i < N; i++) {
+            const float4 x = *(const float4 *)&space[i][w];
+            s[i] += (x.x + x.y) + (x.z + x.w);
+        }
 }
 
-// A row for each blockDim.x threads, EIGHTS eights of columns for each; blockDim.y rows of one warp each where a row is that short
-template <typename T, typename P, int EIGHTS, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(EIGHTS == 4 ? 256 : 1024) norm_kernel(const NormArgs p)
+// A thread's columns of rows that are `step` values apart, brought to shared memory one row after the other, where it alone reads them:
+// 0 behind the row's end.
+template <typename T, int EIGHTS, bool WIDE> struct Rows {
+    const T *row;
+    int64_t step;
+    __device__ __forceinline__ Rows(const void *x, int64_t ld, int64_t first, int64_t by, int t) : row((const T *)x + first * ld + (WIDE ? 8 * t : t)), step(by * ld) {}
+    __device__ __forceinline__ void bring(T *to, int t, int n, int H)
+    {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int r = 0; r < EIGHTS; r++) {
+                const int c = 8 * r * n, there = c + 8 * t < H ? 16 : 0;
+                const T *from = row + (there ? c : -8 * t);
+                copy16(to + c + 8 * t, from, there);
+                if (sizeof(T) == 4) copy16(to + c + 8 * t + 4, from + 4, there);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8 * EIGHTS; r++) to[t + n * r] = t + n * r < H ? row[n * r] : from_float<T>(0.0f);
+        }
+        row += step;
+    }
+};
+// and what has come: whole eights, whatever H is
+template <bool WIDE, typename T> __device__ __forceinline__ Eight brought(const T *from, int first, int t, int n)
 {
-    __shared__ float space[2][1][32];
-    launch_next();
-    wait_for_last();
-    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int threads = blockDim.x;
-    if (row >= p.rows) return;                              // (whole warps: with one row for a block all are here)
-    const T *x = (const T *)p.x + row * p.ldx;
-    float v[EIGHTS][8], s[1] = {0};
+    if constexpr (WIDE) return load_eight(from + first + 8 * t);
+    else {
+        float x[8];
 #pragma unroll
-    for (int r = 0; r < EIGHTS; r++) {
-        load_columns<WIDE>(x, 8 * r * threads, threadIdx.x, threads, p.H, v[r]);
-        if (CENTRED)
-#pragma unroll
-            for (int i = 0; i < 8; i++) s[0] += v[r][i];
+        for (int j = 0; j < 8; j++) x[j] = to_float(from[first + t + n * j]);
+        return {{pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])}};
     }
-    float mean = 0;
-    if (CENTRED) {
-        row_sums(s, threads, space[0]);
-        mean = s[0] / (float)p.H;
-        s[0] = 0;
-    }
+}
+// A thread's columns of w, or `none` of each.  Behind the row's end they are those of column 0, where they meet what is 0 or is not written.
+template <bool WIDE, typename P> __device__ __forceinline__ Eight weights_of(const void *w, int from, int t, int n, int H, float none)
+{
+    if (!w) return eight_of(none);
+    if constexpr (WIDE) return load_eight((const P *)w + (from + 8 * t < H ? from + 8 * t : 0));
+    else {
+        float x[8];
 #pragma unroll
-    for (int r = 0; r < EIGHTS; r++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (CENTRED) v[r][i] = column<WIDE>(8 * r * threads, threadIdx.x, threads, i) < p.H ? v[r][i] - mean : 0.0f;
-            s[0] = fmaf(v[r][i], v[r][i], s[0]);
-        }
-    row_sums(s, threads, space[1]);
-    const float rstd = 1.0f / sqrtf(s[0] / (float)p.H + p.eps);
-    if (threadIdx.x == 0) {
-        if (CENTRED && p.mean) p.mean[row] = mean;
-        if (p.rstd) p.rstd[row] = rstd;
-    }
-#pragma unroll
-    for (int r = 0; r < EIGHTS; r++) {
-        float w[8], b[8];
-        if (p.w) load_columns<WIDE>((const P *)p.w, 8 * r * threads, threadIdx.x, threads, p.H, w);
-        if (p.b) load_columns<WIDE>((const P *)p.b, 8 * r * threads, threadIdx.x, threads, p.H, b);
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float xh = v[r][i] * rstd;
-            v[r][i] = p.w ? p.b ? fmaf(xh, w[i], b[i]) : xh * w[i] : p.b ? xh + b[i] : xh;
-        }
-        store_columns<WIDE>((T *)p.y + row * p.ldy, 8 * r * threads, threadIdx.x, threads, p.H, v[r]);
+        for (int j = 0; j < 8; j++) x[j] = to_float(((const P *)w)[from + t + n * j < H ? from + t + n * j : 0]);
+        return {{pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])}};
     }
 }
 
-// Backwards: a block of up to MOST threads takes rows one after the other and holds its threads' columns of dw and db in registers, in 32 bits.
+// Forwards: blockDim.x threads take a row, EIGHTS eights of columns each (blockDim.y rows of one warp each in a block, where a row is
+// that short), and then the rows that are gridDim.x blocks further.  RING: the next row is brought while one is worked on, so that
+// memory is never idle between the two sums and the write; without it for few rows, whose latency counts.
+template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs p)
+{
+    extern __shared__ __align__(16) char ring[];            // [blockDim.y][2][8 EIGHTS threads]
+    __shared__ __align__(16) float space[2][2][32];
+    const int threads = blockDim.x, t = threadIdx.x, all = 8 * EIGHTS * threads;
+    launch_next();
+    if (threadIdx.y == 0)
+        for (int i = t; i < 128; i += threads) (&space[0][0][0])[i] = 0;
+    __syncthreads();
+    wait_for_last();
+    int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int64_t step = (int64_t)gridDim.x * blockDim.y;
+    T *stage = (T *)ring + threadIdx.y * 2 * all;
+    Rows<T, EIGHTS, WIDE> x(p.x, p.ldx, row, step, t);
+    auto inside = [&](int r, int i) { return column<WIDE>(8 * r * threads, t, threads, WIDE ? 0 : i) < p.H; };
+    if (RING && row < p.rows) x.bring(stage, t, threads, p.H);
+    end_copies();
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {              // (whole warps; whole blocks, where a row has several)
+        Eight v[EIGHTS];
+        if (RING) {
+            if (row + step < p.rows) x.bring(stage + (turn ^ 1) * all, t, threads, p.H);
+            end_copies();
+            copies_arrived<1>();
+        }
+#pragma unroll
+        for (int r = 0; r < EIGHTS; r++)
+            v[r] = RING ? brought<WIDE>(stage + turn * all, 8 * r * threads, t, threads) : load_columns<WIDE>((const T *)p.x + row * p.ldx, 8 * r * threads, t, threads, p.H);
+        float mean = 0, s[1];
+        if (CENTRED) {
+            Pair sum = pair(0.0f);
+#pragma unroll
+            for (int r = 0; r < EIGHTS; r++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum = sum + v[r].v[i];
+            s[0] = sum_of(sum);
+            row_sums(s, threads, &space[0][turn]);
+            mean = s[0] * p.inverse;
+        }
+        Pair squares = pair(0.0f);
+#pragma unroll
+        for (int r = 0; r < EIGHTS; r++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (CENTRED) {
+                    v[r].v[i] = v[r].v[i] + pair(-mean);
+                    if (WIDE ? !inside(r, 0) : !inside(r, 2 * i + 1)) {     // behind the row's end the differences are 0 too
+                        const float2 f = both(v[r].v[i]);
+                        v[r].v[i] = pair(!WIDE && inside(r, 2 * i) ? f.x : 0.0f, 0.0f);
+                    }
+                }
+                squares = fma2(v[r].v[i], v[r].v[i], squares);
+            }
+        s[0] = sum_of(squares);
+        row_sums(s, threads, &space[1][turn]);
+        const float rstd = 1.0f / sqrtf(fmaf(s[0], p.inverse, p.eps));
+        if (t == 0) {
+            if (CENTRED && p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int r = 0; r < EIGHTS; r++) {
+            const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f), b = weights_of<WIDE, P>(p.b, 8 * r * threads, t, threads, p.H, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[r].v[i] = fma2(v[r].v[i] * pair(rstd), w.v[i], b.v[i]);
+            store_columns<WIDE>((T *)p.y + row * p.ldy, 8 * r * threads, t, threads, p.H, v[r]);
+        }
+    }
+}
+
+// Backwards: a row's threads take rows one after the other, the next one on its way meanwhile, and hold their columns' sums of dw and
+// db in registers, in 32 bits.  What has arrived is read twice, for the sums and for dx.
 template <typename T, typename P, int EIGHTS, int MOST, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(MOST) norm_backward_kernel(const NormArgs p)
 {
-    __shared__ float space[2][2][32];
+    extern __shared__ __align__(16) char ring[];            // [blockDim.y][1 + ahead][x, dy, base][8 EIGHTS threads]
+    __shared__ __align__(16) float space[2][2][32];
+    const int threads = blockDim.x, t = threadIdx.x, all = 8 * EIGHTS * threads, three = p.base ? 3 : 2;
     launch_next();
+    if (threadIdx.y == 0)
+        for (int i = t; i < 128; i += threads) (&space[0][0][0])[i] = 0;
+    __syncthreads();
     wait_for_last();
-    const int threads = blockDim.x, t = threadIdx.x;
-    float dw[EIGHTS][8] = {}, db[EIGHTS][8] = {};
+    const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
+    T *stage = (T *)ring + threadIdx.y * (1 + p.ahead) * three * all;
+    Rows<T, EIGHTS, WIDE> rx(p.x, p.ldx, first, step, t), rdy(p.dy, p.lddy, first, step, t), rbase(p.base, p.ldbase, first, step, t);
+    auto bring = [&](int turn) {
+        T *to = stage + (turn & p.ahead) * three * all;
+        rx.bring(to, t, threads, p.H), rdy.bring(to + all, t, threads, p.H);
+        if (p.base) rbase.bring(to + 2 * all, t, threads, p.H);
+    };
+    Eight dw[EIGHTS], db[EIGHTS];
+#pragma unroll
+    for (int r = 0; r < EIGHTS; r++) dw[r] = db[r] = eight_of(0.0f);
+    float mean = 0, rstd = 0;
+    if (first < p.rows) {
+        bring(0);
+        if (CENTRED) mean = p.mean[first];
+        rstd = p.rstd[first];
+    }
+    end_copies();
     int turn = 0;
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
-        float x[EIGHTS][8], g[EIGHTS][8], s[2] = {0, 0};
-        const float mean = CENTRED ? p.mean[row] : 0.0f, rstd = p.rstd[row];
-#pragma unroll
-        for (int r = 0; r < EIGHTS; r++) {
-            load_columns<WIDE>((const T *)p.x + row * p.ldx, 8 * r * threads, t, threads, p.H, x[r]);
-            load_columns<WIDE>((const T *)p.dy + row * p.lddy, 8 * r * threads, t, threads, p.H, g[r]);
+    for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+        float next_mean = 0, next_rstd = 0;
+        if (row + step < p.rows) {
+            if (p.ahead) bring(turn ^ 1);
+            if (CENTRED) next_mean = p.mean[row + step];
+            next_rstd = p.rstd[row + step];
         }
+        end_copies();
+        if (p.ahead) copies_arrived<1>();
+        else copies_arrived<0>();
+        const T *here = stage + (turn & p.ahead) * three * all;
+        const Pair scale = pair(rstd), shift = pair(-mean);                 // (x - mean first: differences of near values are exact)
+        Pair by_xh = pair(0.0f), plain = pair(0.0f);
 #pragma unroll
         for (int r = 0; r < EIGHTS; r++) {
-            float w[8];
-            if (p.w) load_columns<WIDE>((const P *)p.w, 8 * r * threads, t, threads, p.H, w);
+            const Eight x = brought<WIDE>(here, 8 * r * threads, t, threads), g = brought<WIDE>(here + all, 8 * r * threads, t, threads);
+            const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                x[r][i] = (x[r][i] - mean) * rstd;          // (behind the row's end dy is 0)
-                dw[r][i] = fmaf(g[r][i], x[r][i], dw[r][i]);
-                if (CENTRED) db[r][i] += g[r][i];
-                if (p.w) g[r][i] *= w[i];
-                s[0] = fmaf(g[r][i], x[r][i], s[0]);
-                if (CENTRED) s[1] += g[r][i];
+            for (int i = 0; i < 4; i++) {
+                const Pair xh = (CENTRED ? x.v[i] + shift : x.v[i]) * scale, gw = g.v[i] * w.v[i];       // (behind the row's end dy is 0)
+                dw[r].v[i] = fma2(g.v[i], xh, dw[r].v[i]);
+                by_xh = fma2(gw, xh, by_xh);
+                if (CENTRED) db[r].v[i] = db[r].v[i] + g.v[i], plain = plain + gw;
             }
         }
-        if (!p.dx) continue;
-        row_sums(s, threads, space[turn]);
-        const float a = s[0] / (float)p.H, m = s[1] / (float)p.H;
+        if (p.dx) {
+            float s[CENTRED ? 2 : 1];
+            s[0] = sum_of(by_xh);
+            if (CENTRED) s[CENTRED] = sum_of(plain);
+            row_sums(s, threads, space[turn]);
+            // g w - mean(g w) - xh mean(g w xh)
+            const Pair by_x = pair(-s[0] * p.inverse * rstd), rest = pair(CENTRED ? -s[CENTRED] * p.inverse : 0.0f);
 #pragma unroll
-        for (int r = 0; r < EIGHTS; r++) {
-            float d[8] = {};
-            if (p.base) load_columns<WIDE>((const T *)p.base + row * p.ldbase, 8 * r * threads, t, threads, p.H, d);
+            for (int r = 0; r < EIGHTS; r++) {
+                const Eight x = brought<WIDE>(here, 8 * r * threads, t, threads), g = brought<WIDE>(here + all, 8 * r * threads, t, threads);
+                const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f);
+                Eight d = p.base ? brought<WIDE>(here + 2 * all, 8 * r * threads, t, threads) : eight_of(0.0f);
 #pragma unroll
-            for (int i = 0; i < 8; i++) d[i] = fmaf(rstd, fmaf(-x[r][i], a, CENTRED ? g[r][i] - m : g[r][i]), d[i]);
-            store_columns<WIDE>((T *)p.dx + row * p.lddx, 8 * r * threads, t, threads, p.H, d);
+                for (int i = 0; i < 4; i++) d.v[i] = fma2(fma2(g.v[i], w.v[i], CENTRED ? fma2(x.v[i] + shift, by_x, rest) : x.v[i] * by_x), scale, d.v[i]);
+                store_columns<WIDE>((T *)p.dx + row * p.lddx, 8 * r * threads, t, threads, p.H, d);
+            }
         }
+        mean = next_mean, rstd = next_rstd;
+        if (!p.ahead && row + step < p.rows) bring(0);
     }
     if (!p.parts) return;
-    float *part = p.parts + (int64_t)blockIdx.x * (CENTRED ? 2 : 1) * p.H;
+    float *part = p.parts + first * (CENTRED ? 2 : 1) * p.H;
 #pragma unroll
-    for (int r = 0; r < EIGHTS; r++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int c = column<WIDE>(8 * r * threads, t, threads, i);
-            if (c < p.H) {
-                part[c] = dw[r][i];
-                if (CENTRED) part[p.H + c] = db[r][i];
-            }
-        }
+    for (int r = 0; r < EIGHTS; r++) {
+        store_columns<WIDE>(part, 8 * r * threads, t, threads, p.H, dw[r]);
+        if (CENTRED) store_columns<WIDE>(part + p.H, 8 * r * threads, t, threads, p.H, db[r]);
+    }
 }
 
 // The blocks' sums, joined in a fixed order: 32 columns for a block, eight parts of the list side by side

@@ -39,6 +39,20 @@ template <int L> __device__ __forceinline__ float sum_of(float x)
     for (int d = L / 2; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
+template <int L> __device__ __forceinline__ uint32_t most_of(uint32_t x)
+{
+    if (L == 32) return __reduce_max_sync(~0u, x);
+#pragma unroll
+    for (int d = L / 2; d; d /= 2) x = max(x, __shfl_xor_sync(~0u, x, d));
+    return x;
+}
+// A number's bits so that they order as numbers do (-0 as 0), above 0; and back
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 template <int L> __device__ __forceinline__ unsigned lanes_of(int lane) { return L == 32 ? ~0u : ((1u << (L & 31)) - 1) << (lane & ~(L - 1)); }
 
 // A chosen expert's sigmoid score times e^-m, m = min(0, the largest chosen logit): the quotients of scores are right however small
@@ -163,22 +177,35 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
             if (m == NONE) m = 0;
             sum = 0;
 #pragma unroll
-            for (int i = 0; i < PER; i++) sum += expf(z[i] - m);
+            for (int i = 0; i < PER; i++) sum += p.renormalise ? __expf(z[i] - m) : expf(z[i] - m);        // (a weight's, or the choice's alone)
             sum = sum_of<L>(sum);
         }
 #pragma unroll
         for (int i = 0; i < PER; i++) v[i] = z[i];
         if (values) {
-            // A score is off by at most 8 units of 2^-24 of the largest (two for an exponential, as many for the sum's and the
-            // quotient's roundings), a sum with the bias by one of its own; `off` is twice the double.
-            const float inverse = 1.0f / sum;
-            off = 2e-6f * (p.sigmoid ? 1.0f : inverse);
+            // What a score is off by.  Sigmoid: e^-z by 2^-22 + 1.5 |z| 2^-23 of itself, which s (1 - s) takes to 1e-7, two
+            // roundings and the quotient 3e-7.  Softmax: of the largest score, 2^-22 for the term and the sum's up to 37 roundings,
+            // 2.5e-6 in all.  `off` is at least what two values differ by wrongly; a sum with the bias has a rounding of its own.
+            const float inverse = __fdividef(1.0f, sum);
+            off = p.sigmoid ? 1.5e-6f : 6e-6f * inverse;
+            float b[PER];
+            if (!p.bias) {
+#pragma unroll
+                for (int i = 0; i < PER; i++) b[i] = 0;
+            } else if (PER == 8 && p.eights) {
+                float x[8];
+                load8(p.bias + (n > 0 ? first : 0), x);
+#pragma unroll
+                for (int i = 0; i < PER; i++) b[i] = x[i & 7];
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; i++) b[i] = i < n ? p.bias[first + i] : 0.0f;
+            }
 #pragma unroll
             for (int i = 0; i < PER; i++) {
-                const float b = p.bias && i < n ? p.bias[first + i] : 0.0f;
-                bad |= isnan(b) || b == INFINITY;
-                const float s = p.sigmoid ? 1.0f / (1.0f + expf(-z[i])) : expf(z[i] - m) * inverse;
-                v[i] = z[i] == NONE || b == NONE ? NONE : s + b;
+                bad |= isnan(b[i]) || b[i] == INFINITY;
+                const float s = p.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-z[i])) : __expf(z[i] - m) * inverse;
+                v[i] = z[i] == NONE || b[i] == NONE ? NONE : s + b[i];
             }
         }
         bad = (__ballot_sync(~0u, bad) & mine) != 0;
@@ -204,26 +231,32 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
 #pragma unroll
             for (int i = 0; i < PER; i++) v[i] = !kept || v[i] == NONE ? NONE : p.bias ? v[i] : z[i];
         }
+        // The largest k as whole numbers, which order as the values do, 0 for none: the row's largest of the lanes' largest, taken
+        // from the first lane that has it and there from the first place.
+        uint32_t key[PER], best = 0;
+#pragma unroll
+        for (int i = 0; i < PER; i++) key[i] = v[i] == NONE ? 0 : ordered(v[i]), best = max(best, key[i]);
         const bool check = p.bias;                          // (without one the logits decide in the groups)
-        float last = INFINITY;
+        uint32_t last = ~0u;
         for (int j = 0; j < p.k + check; j++) {
-            float most = NONE;
-            int at = 0;
-#pragma unroll
-            for (int i = 0; i < PER; i++)
-                if (v[i] > most) most = v[i], at = i;
-            const float top = most_of<L>(most);
-            const unsigned who = __ballot_sync(~0u, most == top && top > NONE) & mine;
-            if (check && top > NONE) again |= last - top <= off + 2e-7f * (fabsf(last) + fabsf(top)) && last < INFINITY;
-            last = top;
-            if (who && lane == __ffs(who) - 1) {
-                float x = 0;
-#pragma unroll
-                for (int i = 0; i < PER; i++)
-                    if (i == at) v[i] = NONE, x = z[i];
-                if (j < p.k) ce[j] = first + at, cz[j] = x;
+            const uint32_t top = most_of<L>(best);
+            const unsigned who = __ballot_sync(~0u, best == top) & mine;
+            if (check && top && j > 0) {
+                const float x = from_ordered(last), y = from_ordered(top);
+                again |= x - y <= off + 2e-7f * (fabsf(x) + fabsf(y));
             }
-            if (!who && sub == 0 && j < p.k) ce[j] = -1, cz[j] = NONE;
+            last = top;
+            if (lane == __ffs(who) - 1) {
+                int at = PER - 1;
+                float x = z[PER - 1];
+#pragma unroll
+                for (int i = PER - 2; i >= 0; i--)
+                    if (key[i] == top) at = i, x = z[i];
+                best = 0;
+#pragma unroll
+                for (int i = 0; i < PER; i++) key[i] = i == at ? 0 : key[i], best = max(best, key[i]);
+                if (j < p.k) ce[j] = top ? first + at : -1, cz[j] = top ? x : NONE;
+            }
         }
     }
     unsigned slow = __ballot_sync(~0u, sub == 0 && here && again && !bad);
@@ -274,9 +307,20 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
     const T *z = (const T *)p.z + (here ? row : 0) * p.ld;
     T *dz = (T *)p.dz + (here ? row : 0) * p.ldd;
     const int *chosen = p.chosen + (here ? row : 0) * p.k;
-    const float *g = p.dweights + (here ? row : 0) * p.k;
+    const float *dweights = p.dweights + (here ? row : 0) * p.k;
     const int first = sub * p.per, n = here ? max(0, min(p.per, p.E - first)) : 0;
-    auto expert = [&](int j) { const int e = chosen[j]; return e >= 0 && e < p.E ? e : -1; };
+    // a lane's chosen: number sub, sub + L, ...  (k is at most 32 and the lanes' experts, eight each where there are few lanes)
+    constexpr int SLOTS = L >= 8 ? 32 / L : 8;
+    int e[SLOTS];
+    float g[SLOTS], x[SLOTS];
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        const int j = sub + q * L;
+        e[q] = here && j < p.k ? chosen[j] : -1;
+        g[q] = e[q] >= 0 && e[q] < p.E ? dweights[j] : 0.0f;
+        e[q] = e[q] < p.E ? e[q] : -1;
+        x[q] = e[q] >= 0 ? to_float(z[e[q]]) : NONE;
+    }
     float m = 0, inverse = 0, top = NONE, total = 0, mean = 0;
     float s[PER];
 #pragma unroll
@@ -302,49 +346,56 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
         inverse = sum > 0.0f || isnan(sum) ? 1.0f / sum : 0.0f;
     }
     if (p.renormalise) {
-        for (int j = sub; here && j < p.k; j += L) {
-            const int e = expert(j);
-            if (e >= 0) top = fmaxf(top, to_float(z[e]));
-        }
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++) top = fmaxf(top, x[q]);
         top = most_of<L>(top);
         if (top == NONE) top = 0;
         if (p.sigmoid) top = fminf(top, 0.0f);
     }
     // an expert's score: over the sum of all, times e^-top, or as it is
     auto score = [&](float x) { return all ? expf(x - m) * inverse : p.sigmoid ? sigmoid_score(x, p.renormalise ? top : 0.0f) : expf(x - top); };
-    for (int j = sub; here && j < p.k; j += L) {
-        const int e = expert(j);
-        if (e < 0) continue;
-        const float x = score(to_float(z[e]));
-        total += x, mean = fmaf(g[j], x, mean);
+    float s_of[SLOTS];
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        s_of[q] = e[q] >= 0 ? score(x[q]) : 0.0f;
+        total += s_of[q], mean = fmaf(g[q], s_of[q], mean);
     }
     total = sum_of<L>(total), mean = sum_of<L>(mean);
     if (p.renormalise) mean = total > 0.0f || isnan(total) ? mean / total : 0.0f;
     const float rest = all ? -mean * inverse * p.scale : 0.0f;          // what an expert that is not chosen gets, over e^(z - m)
     if (PER == 8 && p.eights) {
-        float x[8];
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = s[i & (PER - 1)] * rest;
-        if (n > 0) store8(dz + first, x);
+        for (int i = 0; i < 8; i++) y[i] = s[i & (PER - 1)] * rest;
+        if (n > 0) store8(dz + first, y);
     } else {
 #pragma unroll
         for (int i = 0; i < PER; i++)
             if (i < n) dz[first + i] = from_float<T>(s[i] * rest);
     }
+    // (an expert that is there twice has the gradients of both, and both write the same)
+    float sums[SLOTS];
+    int times[SLOTS];
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) sums[q] = 0, times[q] = 0;
+#pragma unroll
+    for (int r = 0; r < SLOTS; r++)
+        for (int i = 0; i < L && r * L + i < p.k; i++) {
+            const int other = __shfl_sync(~0u, e[r], i, L);
+            const float its = __shfl_sync(~0u, g[r], i, L);
+#pragma unroll
+            for (int q = 0; q < SLOTS; q++)
+                if (other == e[q]) sums[q] += its, times[q]++;
+        }
     __syncwarp();
-    for (int j = sub; here && j < p.k; j += L) {
-        const int e = expert(j);
-        if (e < 0) continue;
-        float gj = 0;                                       // (an expert that is there twice has the gradients of both)
-        for (int i = 0; i < p.k; i++) gj += chosen[i] == e ? g[i] : 0.0f;
-        int times = 0;
-        for (int i = 0; i < p.k; i++) times += chosen[i] == e;
-        const float x = to_float(z[e]), sj = score(x);
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        if (e[q] < 0) continue;
         float d;
-        if (all) d = sj * (gj - mean);
-        else if (p.renormalise) d = sj / total * (gj - times * mean) * (p.sigmoid ? 1.0f / (1.0f + expf(x)) : 1.0f);
-        else d = gj * sj / (1.0f + expf(x));
-        dz[e] = from_float<T>(d * p.scale);
+        if (all) d = s_of[q] * (sums[q] - mean);
+        else if (p.renormalise) d = s_of[q] / total * (sums[q] - times[q] * mean) * (p.sigmoid ? 1.0f / (1.0f + expf(x[q])) : 1.0f);
+        else d = sums[q] * s_of[q] / (1.0f + expf(x[q]));
+        dz[e[q]] = from_float<T>(d * p.scale);
     }
 }
 

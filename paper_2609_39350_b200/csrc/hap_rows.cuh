@@ -7,51 +7,88 @@ namespace hapop {
 
 constexpr int MOST_CHOSEN = 32;         // experts of a row
 
+// ---- two values at a time -------------------------------------------------------------------------------------------------
+// Two values in 32 bits side by side in a register pair: one instruction adds or multiplies both, each rounded as by itself.
+struct Pair { uint64_t v; };
+__device__ __forceinline__ Pair pair(float x, float y) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(x), "f"(y)); return p; }
+__device__ __forceinline__ Pair pair(float x) { return pair(x, x); }
+__device__ __forceinline__ float2 both(Pair p) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p.v)); return r; }
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ float sum_of(Pair p) { const float2 f = both(p); return f.x + f.y; }
+__device__ __forceinline__ Pair pair_of(uint32_t w, __nv_bfloat16) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ Pair pair_of(uint32_t w, __half) { const float2 f = __half22float2(*(__half2 *)&w); return pair(f.x, f.y); }
+
 // ---- eights of a row's columns ------------------------------------------------------------------------------------------
-// Thread t of n takes eight of the 8 n columns that begin at `from`: side by side where rows begin at multiples of 16 bytes
-// (WIDE), n apart where they do not, so that a warp's accesses still lie side by side.
+// Thread t of n takes eight of the 8 n columns that begin at `from`: side by side where rows begin at multiples of 16 bytes and are
+// whole eights long (WIDE), n apart where they are not, so that a warp's accesses still lie side by side.
+struct Eight { Pair v[4]; };
 template <bool WIDE> __device__ __forceinline__ int column(int from, int t, int n, int j) { return WIDE ? from + 8 * t + j : from + t + n * j; }
-template <bool WIDE, typename T> __device__ __forceinline__ void load_columns(const T *row, int from, int t, int n, int H, float (&x)[8])
+__device__ __forceinline__ Eight eight_of(float x) { return {{pair(x), pair(x), pair(x), pair(x)}}; }
+// eight values side by side at a multiple of 16 bytes
+template <typename T> __device__ __forceinline__ Eight load_eight(const T *p)
 {
-    if (WIDE && from + 8 * t + 8 <= H) {
-        load8(row + from + 8 * t, x);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const int c = column<WIDE>(from, t, n, j);
-        x[j] = c < H ? to_float(row[c]) : 0.0f;
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = ((const float4 *)p)[0], b = ((const float4 *)p)[1];
+        return {{pair(a.x, a.y), pair(a.z, a.w), pair(b.x, b.y), pair(b.z, b.w)}};
+    } else {
+        const uint4 a = *(const uint4 *)p;
+        return {{pair_of(a.x, T()), pair_of(a.y, T()), pair_of(a.z, T()), pair_of(a.w, T())}};
     }
 }
-template <bool WIDE, typename T> __device__ __forceinline__ void store_columns(T *row, int from, int t, int n, int H, const float (&x)[8])
+template <typename T> __device__ __forceinline__ void store_eight(T *p, const Eight &x)
 {
-    if (WIDE && from + 8 * t + 8 <= H) {
-        store8(row + from + 8 * t, x);
-        return;
-    }
+    const float2 a = both(x.v[0]), b = both(x.v[1]), c = both(x.v[2]), d = both(x.v[3]);
+    if constexpr (sizeof(T) == 4) {
+        ((float4 *)p)[0] = make_float4(a.x, a.y, b.x, b.y);
+        ((float4 *)p)[1] = make_float4(c.x, c.y, d.x, d.y);
+    } else *(uint4 *)p = make_uint4(pack2(a.x, a.y, T()), pack2(b.x, b.y, T()), pack2(c.x, c.y, T()), pack2(d.x, d.y, T()));
+}
+// A thread's columns of a row; those behind its H are 0, or not written.
+template <bool WIDE, typename T> __device__ __forceinline__ Eight load_columns(const T *row, int from, int t, int n, int H)
+{
+    if constexpr (WIDE) {
+        if (from + 8 * t < H) return load_eight(row + from + 8 * t);
+        return eight_of(0.0f);
+    } else {
+        float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const int c = column<WIDE>(from, t, n, j);
-        if (c < H) row[c] = from_float<T>(x[j]);
+        for (int j = 0; j < 8; j++) x[j] = from + t + n * j < H ? to_float(row[from + t + n * j]) : 0.0f;
+        return {{pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])}};
+    }
+}
+template <bool WIDE, typename T> __device__ __forceinline__ void store_columns(T *row, int from, int t, int n, int H, const Eight &x)
+{
+    if constexpr (WIDE) {
+        if (from + 8 * t < H) store_eight(row + from + 8 * t, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float2 f = both(x.v[j / 2]);
+            if (from + t + n * j < H) row[from + t + n * j] = from_float<T>(j & 1 ? f.y : f.x);
+        }
     }
 }
 
 // ---- order by a key -------------------------------------------------------------------------------------------------------
-// A stable pass of a counting sort: blocks take chunks of the list, warps parts of a chunk.  A block's numbers of each key are
-// counted first (order_count_kernel); then every block adds up what lies in front of its own, and its warps place their entries in
-// order.  A list that one block takes needs no counting kernel.
-constexpr int ORDER_WARPS = 8, MOST_KEYS = 1024;
+// A stable pass of a counting sort.  A block takes a chunk of the list, tile by tile; a warp's entries of a tile are in its lanes'
+// registers, their ranks among the warp's equal ones come from matching lanes, and one number for every warp and key says how many
+// lie in the warps ahead.  Several blocks count their chunks first (order_count_kernel; a pass that places also counts for the next
+// one), and each adds up what lies in front of its own.  A list of one tile needs the placing kernel alone.
+constexpr int ORDER_WARPS = 16, ORDER_ITEMS = 4, ORDER_TILE = 32 * ORDER_WARPS * ORDER_ITEMS, MOST_KEYS = 1024, MOST_PASSES = 3;
 
 struct OrderArgs {
     int64_t n;
-    int keys, chunk;                // keys 0 .. keys - 1; entries of a block, a multiple of 32 * ORDER_WARPS
-    int *counts;                    // [blocks][keys]
+    int keys, chunk;                // keys 0 .. keys - 1; entries of a block, a multiple of ORDER_TILE
+    int *counts;                    // [passes][blocks][keys], of which this pass is number `pass`
+    int pass, passes;
     // what the entries are: expert numbers, or (value, number) pairs by the digit at `shift`, made of tokens in the first pass
     const int *experts;
     int first;
     const int64_t *tokens;
     int64_t first_token;
-    int V, shift, mask;
+    int V, shift, bits;
     const uint2 *from;
     uint2 *to;
     int *places;
@@ -72,104 +109,138 @@ template <int WHAT> __device__ __forceinline__ int order_key(const OrderArgs &p,
         const int64_t v = (int64_t)((uint64_t)t - (uint64_t)p.first_token);
         entry = make_uint2(t >= p.first_token && v >= 0 && v < p.V ? (unsigned)v : (unsigned)p.V, (unsigned)i);
     } else entry = p.from[i];
-    return entry.x >> p.shift & p.mask;
+    return entry.x >> p.shift & (1 << p.bits) - 1;
 }
 
 template <int WHAT> __global__ void __launch_bounds__(32 * ORDER_WARPS) order_count_kernel(const OrderArgs p)
 {
     __shared__ int count[MOST_KEYS];
+    constexpr int THREADS = 32 * ORDER_WARPS;
     launch_next();
-    for (int d = threadIdx.x; d < p.keys; d += blockDim.x) count[d] = 0;
+    for (int d = threadIdx.x; d < p.keys; d += THREADS) count[d] = 0;
     __syncthreads();
     wait_for_last();
+    const int all = gridDim.x * THREADS, me = blockIdx.x * THREADS + threadIdx.x;
     if (WHAT == BY_TOKEN && p.present)
-        for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < (p.V + 31) / 32; i += gridDim.x * blockDim.x) p.present[i] = 0;
+        for (int i = me; i < (p.V + 31) / 32; i += all) p.present[i] = 0;
+    for (int i = me; i < (p.passes - 1) * (int)gridDim.x * p.keys; i += all) p.counts[gridDim.x * p.keys + i] = 0;      // the later passes'
     const int64_t from = (int64_t)blockIdx.x * p.chunk;
-    for (int i = threadIdx.x; i < p.chunk; i += blockDim.x) {
-        uint2 entry;
-        const int key = order_key<WHAT>(p, from + i, entry);
-        if (key >= 0) atomicAdd(&count[key], 1);
+    for (int i = threadIdx.x; i < p.chunk; i += THREADS * ORDER_ITEMS) {
+        int key[ORDER_ITEMS];
+#pragma unroll
+        for (int u = 0; u < ORDER_ITEMS; u++) {
+            uint2 entry;
+            key[u] = order_key<WHAT>(p, from + i + u * THREADS, entry);
+        }
+#pragma unroll
+        for (int u = 0; u < ORDER_ITEMS; u++)
+            if (key[u] >= 0) atomicAdd(&count[key[u]], 1);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < p.keys; d += blockDim.x) p.counts[(int64_t)blockIdx.x * p.keys + d] = count[d];
+    for (int d = threadIdx.x; d < p.keys; d += THREADS) p.counts[blockIdx.x * p.keys + d] = count[d];
 }
 
 template <int WHAT> __global__ void __launch_bounds__(32 * ORDER_WARPS) order_place_kernel(const OrderArgs p)
 {
-    extern __shared__ int at[];                             // [ORDER_WARPS][keys]: where a warp's next entry of a key goes
-    __shared__ int sums[ORDER_WARPS];
-    constexpr int THREADS = 32 * ORDER_WARPS;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, each = p.chunk / ORDER_WARPS;
-    const int64_t from = (int64_t)blockIdx.x * p.chunk + warp * each;
+    extern __shared__ uint16_t at[];                        // [ORDER_WARPS][keys, even]: entries of a key in a warp, then in those ahead
+    __shared__ int base[MOST_KEYS], total[MOST_KEYS], sums[ORDER_WARPS];     // where a key's next entry goes; its number
+    constexpr int THREADS = 32 * ORDER_WARPS, PER = MOST_KEYS / THREADS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, width = (p.keys + 1) & ~1, blocks = gridDim.x;
     launch_next();
-    for (int d = threadIdx.x; d < ORDER_WARPS * p.keys; d += THREADS) at[d] = 0;
+    for (int d = threadIdx.x; d < p.keys; d += THREADS) base[d] = total[d] = 0;
     __syncthreads();
     wait_for_last();
-    if (WHAT == BY_TOKEN && p.present && gridDim.x == 1)
+    if (WHAT == BY_TOKEN && p.present && blocks == 1)
         for (int i = threadIdx.x; i < (p.V + 31) / 32; i += THREADS) p.present[i] = 0;
-    for (int i = lane; i < each; i += 32) {
-        uint2 entry;
-        const int key = order_key<WHAT>(p, from + i, entry);
-        if (key >= 0) atomicAdd(&at[warp * p.keys + key], 1);
+    if (blocks > 1) {                                       // numbers of all blocks, and of the blocks ahead
+        const int *counts = p.counts + (int64_t)p.pass * blocks * p.keys;
+        const int ahead = blockIdx.x * p.keys, all = blocks * p.keys;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < all; i += THREADS) {
+            const int c = counts[i], d = i % p.keys;
+            if (c) {
+                atomicAdd(&total[d], c);
+                if (i < ahead) atomicAdd(&base[d], c);
+            }
+        }
     }
-    __syncthreads();
-    // a thread's keys follow one another: their numbers in all blocks, in the blocks ahead, and so where they begin
-    const int per = (p.keys + THREADS - 1) / THREADS, key0 = threadIdx.x * per;
-    int total[MOST_KEYS / THREADS], ahead[MOST_KEYS / THREADS], mine = 0;
+    int *next = p.pass + 1 < p.passes && blocks > 1 ? p.counts + (int64_t)(p.pass + 1) * blocks * p.keys : nullptr;
+    for (int tile = 0; tile < p.chunk; tile += ORDER_TILE) {
+        const int64_t from = (int64_t)blockIdx.x * p.chunk + tile + warp * 32 * ORDER_ITEMS + lane;
+        if (tile > 0 && (int64_t)blockIdx.x * p.chunk + tile >= p.n) break;
+        uint2 entry[ORDER_ITEMS];
+        int key[ORDER_ITEMS], rank[ORDER_ITEMS];
 #pragma unroll
-    for (int i = 0; i < MOST_KEYS / THREADS; i++) {
-        total[i] = ahead[i] = 0;
-        if (i < per && key0 + i < p.keys) {
-            if (gridDim.x == 1) {
-                for (int w = 0; w < ORDER_WARPS; w++) total[i] += at[w * p.keys + key0 + i];
-            } else {
-                for (int b = 0; b < gridDim.x; b++) {
-                    const int c = p.counts[(int64_t)b * p.keys + key0 + i];
-                    total[i] += c, ahead[i] += b < blockIdx.x ? c : 0;
+        for (int u = 0; u < ORDER_ITEMS; u++) key[u] = order_key<WHAT>(p, from + 32 * u, entry[u]);
+        uint16_t *mine = at + warp * width;
+        for (int d = lane; d < width / 2; d += 32) ((uint32_t *)mine)[d] = 0;
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < ORDER_ITEMS; u++) {
+            const unsigned same = __match_any_sync(~0u, key[u]);
+            const int lower = __popc(same & ((1u << lane) - 1)), before = key[u] >= 0 ? mine[key[u]] : 0;
+            rank[u] = before + lower;
+            __syncwarp();
+            if (key[u] >= 0 && lower == 0) mine[key[u]] = (uint16_t)(before + __popc(same));
+            __syncwarp();
+        }
+        __syncthreads();
+        int number[PER], sum = 0;                           // of this tile, for PER keys that follow one another
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int d = threadIdx.x * PER + i;
+            number[i] = 0;
+            if (d < p.keys)
+                for (int w = 0; w < ORDER_WARPS; w++) {
+                    const int c = at[w * width + d];
+                    at[w * width + d] = (uint16_t)number[i];
+                    number[i] += c;
                 }
+            if (d < p.keys && tile == 0) {
+                if (blocks == 1) total[d] = number[i];
+                sum += total[d];
             }
-            mine += total[i];
         }
-    }
-    int before = mine;
-    for (int d = 1; d < 32; d *= 2) {
-        const int x = __shfl_up_sync(~0u, before, d);
-        if (lane >= d) before += x;
-    }
-    if (lane == 31) sums[warp] = before;
-    __syncthreads();
-    before -= mine;
-    for (int w = 0; w < warp; w++) before += sums[w];
+        if (tile == 0) {                                    // a key's entries lie behind those of all smaller keys
+            int before = sum;
+            for (int d = 1; d < 32; d *= 2) {
+                const int x = __shfl_up_sync(~0u, before, d);
+                if (lane >= d) before += x;
+            }
+            if (lane == 31) sums[warp] = before;
+            __syncthreads();
+            before -= sum;
+            for (int w = 0; w < warp; w++) before += sums[w];
 #pragma unroll
-    for (int i = 0; i < MOST_KEYS / THREADS; i++)
-        if (i < per && key0 + i < p.keys) {
-            if (WHAT == BY_EXPERT && blockIdx.x == 0) {
-                p.offsets[key0 + i] = before;
-                if (key0 + i == p.keys - 1) p.offsets[p.keys] = before + total[i];
+            for (int i = 0; i < PER; i++) {
+                const int d = threadIdx.x * PER + i;
+                if (d >= p.keys) break;
+                if (WHAT == BY_EXPERT && blockIdx.x == 0) {
+                    p.offsets[d] = before;
+                    if (d == p.keys - 1) p.offsets[p.keys] = before + total[d];
+                }
+                base[d] += before;
+                before += total[d];
             }
-            int next = before + ahead[i];
-            for (int w = 0; w < ORDER_WARPS; w++) {
-                const int c = at[w * p.keys + key0 + i];
-                at[w * p.keys + key0 + i] = next;
-                next += c;
-            }
-            before += total[i];
         }
-    __syncthreads();
-    for (int i = 0; i < each; i += 32) {
-        if (from + i >= p.n) break;
-        uint2 entry;
-        const int key = order_key<WHAT>(p, from + i + lane, entry);
-        const unsigned same = __match_any_sync(~0u, key);
-        const int ahead_of = __popc(same & ((1u << lane) - 1));
-        const int place = key >= 0 ? at[warp * p.keys + key] + ahead_of : -1;
-        __syncwarp();
-        if (key >= 0 && ahead_of == 0) at[warp * p.keys + key] = place + __popc(same);
-        __syncwarp();
-        if (from + i + lane >= p.n) continue;
-        if (WHAT == BY_EXPERT) p.places[from + i + lane] = place;
-        else p.to[place] = entry;
-        if (WHAT == BY_TOKEN && p.present && entry.x < p.V) atomicOr(&p.present[entry.x >> 5], 1u << (entry.x & 31));
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ORDER_ITEMS; u++) {
+            const int64_t i = from + 32 * u;
+            if (i >= p.n) continue;
+            const int place = key[u] >= 0 ? base[key[u]] + mine[key[u]] + rank[u] : -1;
+            if (WHAT == BY_EXPERT) p.places[i] = place;
+            else {
+                p.to[place] = entry[u];
+                if (next) atomicAdd(&next[place / p.chunk * p.keys + (int)(entry[u].x >> p.shift + p.bits & (1 << p.bits) - 1)], 1);
+            }
+            if (WHAT == BY_TOKEN && p.present && entry[u].x < p.V) atomicOr(&p.present[entry[u].x >> 5], 1u << (entry[u].x & 31));
+        }
+        if (tile + ORDER_TILE >= p.chunk) break;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; i++)
+            if (threadIdx.x * PER + i < p.keys) base[threadIdx.x * PER + i] += number[i];
     }
 }
 
@@ -213,13 +284,8 @@ template <typename U, bool WIDE> __global__ void __launch_bounds__(256) dispatch
     if (WIDE) {
         constexpr int N = 16 / sizeof(U);
         for (int c = r.from + lane * N; c < r.to; c += 32 * N) {
-            if (c + N <= r.to) {
-                const uint4 v = *(const uint4 *)(x + c);
-                for (unsigned left = there; left; left &= left - 1) *(uint4 *)((U *)p.out + (int64_t)places[__ffs(left) - 1] * p.ldo + c) = v;
-            } else {
-                for (unsigned left = there; left; left &= left - 1)
-                    for (int i = c; i < r.to; i++) ((U *)p.out + (int64_t)places[__ffs(left) - 1] * p.ldo)[i] = x[i];
-            }
+            const uint4 v = *(const uint4 *)(x + c);
+            for (unsigned left = there; left; left &= left - 1) *(uint4 *)((U *)p.out + (int64_t)places[__ffs(left) - 1] * p.ldo + c) = v;
         }
     } else {
         for (int c = r.from + lane; c < r.to; c += 32) {
@@ -229,96 +295,182 @@ template <typename U, bool WIDE> __global__ void __launch_bounds__(256) dispatch
     }
 }
 
-// out[row] = base[row] + sum_j weight_j y[place_j]
+template <int N> struct Count { static constexpr int value = N; };
+
+// Eight values as they are read: unpacked where they are used, so that many reads are on their way in few registers
+template <typename T, bool WIDE> struct Raw {
+    uint4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *row, int from, int t, int n, int H)
+    {
+#pragma unroll
+        for (int i = 0; i < sizeof(T) / 2; i++) v[i] = ((const uint4 *)(row + from + 8 * t))[i];
+    }
+    __device__ __forceinline__ Eight eight() const
+    {
+        if constexpr (sizeof(T) == 2) return {{pair_of(v[0].x, T()), pair_of(v[0].y, T()), pair_of(v[0].z, T()), pair_of(v[0].w, T())}};
+        else {
+            const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+            Eight x;
+#pragma unroll
+            for (int i = 0; i < 4; i++) x.v[i] = pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            return x;
+        }
+    }
+};
+template <typename T> struct Raw<T, false> {
+    T v[8];
+    __device__ __forceinline__ void load(const T *row, int from, int t, int n, int H)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = row[from + t + n * j < H ? from + t + n * j : 0];
+    }
+    __device__ __forceinline__ Eight eight() const
+    {
+        Eight x;
+#pragma unroll
+        for (int j = 0; j < 4; j++) x.v[j] = pair(to_float(v[2 * j]), to_float(v[2 * j + 1]));
+        return x;
+    }
+};
+
+// out[row] = base[row] + sum_j weight_j y[place_j].  The rows that are there, with their weights, are listed in shared memory, so that
+// reads are not behind conditions: eight rows are on their way at once.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_kernel(const RowsArgs p)
 {
+    __shared__ int2 list[8][MOST_CHOSEN];
     launch_next();
     wait_for_last();
     const Piece r = piece_of(p);
     const int lane = threadIdx.x & 31;
     if (r.row >= p.rows) return;
+    int2 *mine = list[threadIdx.x >> 5];
     int place = -1;
     float weight = 1.0f;
     if (lane < p.k) {
         place = p.places[r.row * p.k + lane];
         if (p.weights) weight = p.weights[r.row * p.k + lane];
     }
-    const unsigned there = __ballot_sync(~0u, place >= 0 && place < p.placed);
+    const bool is = place >= 0 && place < p.placed;
+    const unsigned there = __ballot_sync(~0u, is);
+    if (is) mine[__popc(there & ((1u << lane) - 1))] = make_int2(place, __float_as_int(weight));
+    __syncwarp();
+    const int n = __popc(there);
     for (int c = r.from; c < r.to; c += 256) {
-        float sum[8] = {};
-        if (p.base) load_columns<WIDE>((const T *)p.base + r.row * p.ldbase, c, lane, 32, r.to, sum);
-        for (unsigned left = there; left; ) {
-            float x[4][8], w[4];
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const int j = left ? __ffs(left) - 1 : -1;
-                left &= left - 1;
-                const int at = __shfl_sync(~0u, place, j & 31);
-                w[u] = __shfl_sync(~0u, weight, j & 31);
-                if (j >= 0) load_columns<WIDE>((const T *)p.y + (int64_t)at * p.ldy, c, lane, 32, r.to, x[u]);
-                else {
-                    w[u] = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) x[u][i] = 0;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; u++)
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum[i] = fmaf(w[u], x[u][i], sum[i]);
+        if (WIDE && c + 8 * lane >= r.to) break;
+        Eight sum = eight_of(0.0f);
+        if (p.base) {
+            Raw<T, WIDE> x;
+            x.load((const T *)p.base + r.row * p.ldbase, c, lane, 32, r.to);
+            sum = x.eight();
         }
+        auto add = [&](int j, auto count) {
+            constexpr int N = decltype(count)::value;
+            Raw<T, WIDE> x[N];
+#pragma unroll
+            for (int u = 0; u < N; u++) x[u].load((const T *)p.y + (int64_t)mine[j + u].x * p.ldy, c, lane, 32, r.to);
+#pragma unroll
+            for (int u = 0; u < N; u++) {
+                const Eight e = x[u].eight();
+                const Pair w = pair(__int_as_float(mine[j + u].y));
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum.v[i] = fma2(w, e.v[i], sum.v[i]);
+            }
+        };
+        int j = 0;
+        if (sizeof(T) == 2)
+            for (; j + 8 <= n; j += 8) add(j, Count<8>());
+        for (; j + 4 <= n; j += 4) add(j, Count<4>());
+        if (n & 2) add(j, Count<2>()), j += 2;
+        if (n & 1) add(j, Count<1>());
         store_columns<WIDE>((T *)p.out + r.row * p.ldo, c, lane, 32, r.to, sum);
     }
 }
 
-// dy[place_j] = weight_j dout[row] and dweight_j = <dout[row], y[place_j]>, a block for each row: dout is read once, y once.
+// dy[place_j] = weight_j dout[row] and dweight_j = <dout[row], y[place_j]>, a block for each row: dout is read once, y once.  Up to
+// eight rows of y are on their way at once; with more than eight dout is read again, from L1.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsArgs p)
 {
     __shared__ float parts[8][MOST_CHOSEN];
+    __shared__ int2 list[MOST_CHOSEN];                      // of the rows that are there: place, weight
+    __shared__ int order[MOST_CHOSEN];
     launch_next();
     wait_for_last();
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int *places = p.places + row * p.k;
-    for (int j0 = 0; j0 < p.k; j0 += 8) {                   // (dout again, from L1, where there are more than eight)
-        float dot[8] = {};
+    const int place = lane < p.k ? p.places[row * p.k + lane] : -1;
+    const bool is = place >= 0 && place < p.placed;
+    const unsigned there = __ballot_sync(~0u, is);
+    const int n = __popc(there);
+    if (warp == 0 && is) {
+        const int at = __popc(there & ((1u << lane) - 1));
+        list[at] = make_int2(place, __float_as_int(p.weights ? p.weights[row * p.k + lane] : 1.0f)), order[at] = lane;
+    }
+    __syncthreads();
+    if (p.dweights && warp == 0 && lane < p.k && !is) p.dweights[row * p.k + lane] = 0;
+    auto some = [&](int j0, auto count) {
+        constexpr int N = decltype(count)::value;
+        Pair dot[N];
+#pragma unroll
+        for (int u = 0; u < N; u++) dot[u] = pair(0.0f);
         for (int c = 0; c < p.H; c += 8 * blockDim.x) {
-            float d[8];
-            load_columns<WIDE>((const T *)p.x + row * p.ldx, c, threadIdx.x, blockDim.x, p.H, d);
+            if (WIDE && c + 8 * threadIdx.x >= p.H) break;
+            Raw<T, WIDE> rd, ry[N];
+            rd.load((const T *)p.x + row * p.ldx, c, threadIdx.x, blockDim.x, p.H);
+            if (p.dweights)
 #pragma unroll
-            for (int u = 0; u < 8; u++) {
-                if (j0 + u >= p.k) break;
-                const int at = places[j0 + u];
-                if (at < 0 || at >= p.placed) continue;
+                for (int u = 0; u < N; u++) ry[u].load((const T *)p.y + (int64_t)list[j0 + u].x * p.ldy, c, threadIdx.x, blockDim.x, p.H);
+            Eight d = rd.eight();
+            if (!WIDE) {                                    // (behind the row's end the first column was read)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 f = both(d.v[i]);
+                    d.v[i] = pair(column<WIDE>(c, threadIdx.x, blockDim.x, 2 * i) < p.H ? f.x : 0.0f, column<WIDE>(c, threadIdx.x, blockDim.x, 2 * i + 1) < p.H ? f.y : 0.0f);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < N; u++) {
                 if (p.dweights) {
-                    float y[8];
-                    load_columns<WIDE>((const T *)p.y + (int64_t)at * p.ldy, c, threadIdx.x, blockDim.x, p.H, y);
+                    Eight y = ry[u].eight();
+                    if (!WIDE) {
 #pragma unroll
-                    for (int i = 0; i < 8; i++) dot[u] = fmaf(y[i], d[i], dot[u]);
+                        for (int i = 0; i < 4; i++) {
+                            const float2 f = both(y.v[i]);
+                            y.v[i] = pair(column<WIDE>(c, threadIdx.x, blockDim.x, 2 * i) < p.H ? f.x : 0.0f, column<WIDE>(c, threadIdx.x, blockDim.x, 2 * i + 1) < p.H ? f.y : 0.0f);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) dot[u] = fma2(y.v[i], d.v[i], dot[u]);
                 }
                 if (p.out) {
-                    const float w = p.weights ? p.weights[row * p.k + j0 + u] : 1.0f;
-                    float x[8];
+                    const Pair w = pair(__int_as_float(list[j0 + u].y));
+                    Eight x;
 #pragma unroll
-                    for (int i = 0; i < 8; i++) x[i] = w * d[i];
-                    store_columns<WIDE>((T *)p.out + (int64_t)at * p.ldo, c, threadIdx.x, blockDim.x, p.H, x);
+                    for (int i = 0; i < 4; i++) x.v[i] = w * d.v[i];
+                    store_columns<WIDE>((T *)p.out + (int64_t)list[j0 + u].x * p.ldo, c, threadIdx.x, blockDim.x, p.H, x);
                 }
             }
         }
-        if (!p.dweights) continue;
+        if (!p.dweights) return;
 #pragma unroll
-        for (int u = 0; u < 8; u++) {
+        for (int u = 0; u < N; u++) {
+            float sum = sum_of(dot[u]);
 #pragma unroll
-            for (int s = 16; s; s /= 2) dot[u] += __shfl_xor_sync(~0u, dot[u], s);
-            if (lane == 0 && j0 + u < p.k) parts[warp][j0 + u] = dot[u];
+            for (int s = 16; s; s /= 2) sum += __shfl_xor_sync(~0u, sum, s);
+            if (lane == 0) parts[warp][j0 + u] = sum;
         }
-    }
+    };
+    int j = 0;
+    if (sizeof(T) == 2)
+        for (; j + 8 <= n; j += 8) some(j, Count<8>());
+    for (; j + 4 <= n; j += 4) some(j, Count<4>());
+    if (n & 2) some(j, Count<2>()), j += 2;
+    if (n & 1) some(j, Count<1>());
     if (!p.dweights) return;
     __syncthreads();
-    if (threadIdx.x < p.k) {
+    if (threadIdx.x < n) {
         float sum = 0;
         for (int w = 0; w < warps; w++) sum += parts[w][threadIdx.x];
-        p.dweights[row * p.k + threadIdx.x] = sum;
+        p.dweights[row * p.k + order[threadIdx.x]] = sum;
     }
 }
 
@@ -326,7 +478,7 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
 struct EmbeddingArgs {
     int64_t n, first;
     int64_t ldw, ldx, ldo;
-    int H, piece, V, chunk, accumulate;
+    int H, piece, V, chunk, accumulate, sums, columns;      // sums: blocks that sum, in front of those that clear; columns: blocks of a chunk
     float scale;
     const int64_t *tokens;
     const void *w, *x;              // x: the gradient dy
@@ -349,116 +501,111 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embeddin
     T *out = (T *)p.out + row * p.ldo;
     const T *in = (const T *)p.w + (there ? v : 0) * p.ldw;
     for (int c = from; c < to; c += 256) {
-        float x[8] = {};
-        if (there) load_columns<WIDE>(in, c, lane, 32, to, x);
+        Eight x = there ? load_columns<WIDE>(in, c, lane, 32, to) : eight_of(0.0f);
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] *= p.scale;
+        for (int i = 0; i < 4; i++) x.v[i] = x.v[i] * pair(p.scale);
         store_columns<WIDE>(out, c, lane, 32, to, x);
     }
 }
 
-// Rows of the gradient that no token has
-template <typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_clear_kernel(const EmbeddingArgs p)
+// The gradient.  The first blocks sum dy over the tokens of a row of w: each takes a chunk of the sorted list and an eight of columns
+// for every thread, four rows of dy (and of what they are added to) on their way at once.  A row whose tokens are of one chunk is
+// finished here; sums of a part of a row go to `parts` and are joined in order.  The blocks behind them write the rows that no token
+// has, which is most of the bytes where nothing is added to.
+constexpr int EMBEDDING_CHUNK = 32;
+template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_gradient_kernel(const EmbeddingArgs p)
 {
+    __shared__ uint2 list[EMBEDDING_CHUNK + 2];             // the token in front of the chunk's, the chunk's, the one behind
     launch_next();
     wait_for_last();
-    const int lane = threadIdx.x & 31;
-    const float zero[8] = {};
-    for (int64_t v = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); v < p.V; v += (int64_t)gridDim.x * 8) {
-        if (p.present[v >> 5] >> (v & 31) & 1) continue;
-        for (int c = 0; c < p.H; c += 256) store_columns<WIDE>((O *)p.out + v * p.ldo, c, lane, 32, p.H, zero);
+    if (blockIdx.x >= p.sums) {
+        const Eight zero = eight_of(0.0f);
+        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+        for (int64_t v = (int64_t)(blockIdx.x - p.sums) * warps + (threadIdx.x >> 5); v < p.V; v += (int64_t)(gridDim.x - p.sums) * warps) {
+            if (p.present[v >> 5] >> (v & 31) & 1) continue;
+            for (int c = 0; c < p.H; c += 256) store_columns<WIDE>((O *)p.out + v * p.ldo, c, lane, 32, p.H, zero);
+        }
+        return;
     }
-}
-
-template <typename O, bool WIDE> __device__ __forceinline__ void embedding_put(const EmbeddingArgs &p, unsigned v, int c, const float (&sum)[8])
-{
-    O *out = (O *)p.out + (int64_t)v * p.ldo;
-    float x[8] = {};
-    if (p.accumulate) load_columns<WIDE>(out, c, threadIdx.x, blockDim.x, p.H, x);
+    const int chunk = blockIdx.x / p.columns, t = threadIdx.x, n = blockDim.x, c = blockIdx.x % p.columns * n * 8;
+    const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK;
+    if (t < EMBEDDING_CHUNK) {
+        const uint2 none = make_uint2(p.V, 0);
+        list[t + 1] = from + t < p.n ? p.sorted[from + t] : none;
+        if (t == 0) list[0] = from > 0 ? p.sorted[from - 1] : none;
+        if (t == 1) list[EMBEDDING_CHUNK + 1] = from + EMBEDDING_CHUNK < p.n ? p.sorted[from + EMBEDDING_CHUNK] : none;
+    }
+    __syncthreads();
+    if (WIDE && c + 8 * t >= p.H) return;
+    const uint2 *s = list + 1;
+    const unsigned V = p.V;
+    if (s[0].x >= V) return;
+    float *part = p.parts + (int64_t)chunk * 2 * p.H;
+    Eight sum = eight_of(0.0f);
+    bool first = list[0].x == s[0].x;                       // the row began in front of this chunk
+    for (int i = 0; i < EMBEDDING_CHUNK; i += 4) {
+        if (s[i].x >= V) break;
+        Raw<T, WIDE> x[4];
+        Raw<O, WIDE> before[4];
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = fmaf(sum[i], p.scale, x[i]);
-    store_columns<WIDE>(out, c, threadIdx.x, blockDim.x, p.H, x);
-}
-
-// Sums of dy over the tokens of a row of w: blocks take chunks of the sorted list and eights of columns.  A row whose tokens are of
-// one chunk is finished here; sums of a part of a row go to `parts` and are joined in order.
-template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_sum_kernel(const EmbeddingArgs p)
-{
-    launch_next();
-    wait_for_last();
-    const int64_t from = (int64_t)blockIdx.x * p.chunk, to = min(from + p.chunk, p.n);
-    const int c = blockIdx.y * blockDim.x * 8;
-    const uint2 *s = p.sorted;
-    unsigned v = s[from].x;
-    if (v >= p.V) return;
-    bool first = from > 0 && s[from - 1].x == v;            // the row began in front of this chunk
-    const unsigned behind = to < p.n ? s[to].x : p.V;
-    float sum[8] = {};
-    auto put = [&](bool last) {
-        if (first || last) {
-            float *part = p.parts + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * p.H;
+        for (int u = 0; u < 4; u++) x[u].load((const T *)p.x + (int64_t)s[i + u].y * p.ldx, c, t, n, p.H);
+        if (p.accumulate)                                   // (of a row's last token; others read row 0, which stays in L1)
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const int at = column<WIDE>(c, threadIdx.x, blockDim.x, j);
-                if (at < p.H) part[at] = sum[j];
-            }
-        } else embedding_put<O, WIDE>(p, v, c, sum);
-    };
-    for (int64_t i = from; i < to; i += 4) {
-        float x[4][8];
-        unsigned of[4];
+            for (int u = 0; u < 4; u++) before[u].load((const O *)p.out + (s[i + u].x < V && s[i + u + 1].x != s[i + u].x ? (int64_t)s[i + u].x * p.ldo : 0), c, t, n, p.H);
 #pragma unroll
         for (int u = 0; u < 4; u++) {
-            const uint2 e = i + u < to ? s[i + u] : make_uint2(p.V, 0);
-            of[u] = e.x;
-            if (e.x < p.V) load_columns<WIDE>((const T *)p.x + (int64_t)e.y * p.ldx, c, threadIdx.x, blockDim.x, p.H, x[u]);
-        }
+            const unsigned v = s[i + u].x;
+            if (v >= V) break;
+            const Eight e = x[u].eight();
 #pragma unroll
-        for (int u = 0; u < 4; u++) {
-            if (of[u] != v) {
-                if (v < p.V) put(false);
-                v = of[u], first = false;
+            for (int j = 0; j < 4; j++) sum.v[j] = sum.v[j] + e.v[j];
+            const bool last = s[i + u + 1].x != v, whole = last && !first;
+            if (whole) {
+                Eight y = p.accumulate ? before[u].eight() : eight_of(0.0f);
 #pragma unroll
-                for (int j = 0; j < 8; j++) sum[j] = 0;
-            }
-            if (v < p.V)
-#pragma unroll
-                for (int j = 0; j < 8; j++) sum[j] += x[u][j];
+                for (int j = 0; j < 4; j++) y.v[j] = fma2(sum.v[j], pair(p.scale), y.v[j]);
+                store_columns<WIDE>((O *)p.out + (int64_t)v * p.ldo, c, t, n, p.H, y);
+            } else if (last || i + u == EMBEDDING_CHUNK - 1) store_columns<WIDE>(part + (first ? 0 : p.H), c, t, n, p.H, sum);
+            if (last) first = false, sum = eight_of(0.0f);
         }
     }
-    if (v < p.V) put(v == behind);
 }
 
+// Rows that begin in one chunk and end in another: their parts, in order
 template <typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_join_kernel(const EmbeddingArgs p)
 {
     launch_next();
     wait_for_last();
-    // rows that begin in this chunk and go on in the next
-    const int64_t chunks = (p.n + p.chunk - 1) / p.chunk, from = (int64_t)blockIdx.x * p.chunk, to = from + p.chunk;
-    if (to >= p.n) return;
-    const unsigned v = p.sorted[to].x;
-    if (v >= p.V || p.sorted[to - 1].x != v) return;
-    if (p.sorted[from].x == v && from > 0 && p.sorted[from - 1].x == v) return;
-    int64_t lo = blockIdx.x + 1, hi = chunks;               // the last chunk that begins with the row
+    const int chunks = (int)((p.n + EMBEDDING_CHUNK - 1) / EMBEDDING_CHUNK), chunk = blockIdx.x / p.columns, t = threadIdx.x, n = blockDim.x, c = blockIdx.x % p.columns * n * 8;
+    const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK, to = from + EMBEDDING_CHUNK;
+    const unsigned v = p.sorted[to].x, inside = p.sorted[to - 1].x, begin = p.sorted[from].x, before = from > 0 ? p.sorted[from - 1].x : p.V;
+    if (v >= p.V || inside != v || (begin == v && before == v)) return;
+    int lo = chunk + 1, hi = chunks;                        // the last chunk that begins with the row
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) / 2;
-        if (p.sorted[mid * p.chunk].x == v) lo = mid; else hi = mid;
+        const int mid = lo + (hi - lo < 4 ? 1 : (hi - lo) / 2);
+        if (p.sorted[(int64_t)mid * EMBEDDING_CHUNK].x == v) lo = mid; else hi = mid;
     }
-    const int c = blockIdx.y * blockDim.x * 8;
-    float sum[8];
+    if (WIDE && c + 8 * t >= p.H) return;
+    O *out = (O *)p.out + (int64_t)v * p.ldo;
+    const Eight was = p.accumulate ? load_columns<WIDE>((const O *)out, c, t, n, p.H) : eight_of(0.0f);
+    Raw<float, WIDE> x;
+    x.load(p.parts + ((int64_t)chunk * 2 + 1) * p.H, c, t, n, p.H);
+    Eight sum = x.eight();
+    for (int b = chunk + 1; b <= lo; b += 4) {
+        Raw<float, WIDE> y[4];
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const int at = column<WIDE>(c, threadIdx.x, blockDim.x, j);
-        sum[j] = at < p.H ? p.parts[((int64_t)blockIdx.x * 2 + 1) * p.H + at] : 0.0f;
-    }
-#pragma unroll 4
-    for (int64_t b = blockIdx.x + 1; b <= lo; b++)
+        for (int u = 0; u < 4; u++) y[u].load(p.parts + (int64_t)min(b + u, lo) * 2 * p.H, c, t, n, p.H);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int at = column<WIDE>(c, threadIdx.x, blockDim.x, j);
-            if (at < p.H) sum[j] += p.parts[b * 2 * p.H + at];
+        for (int u = 0; u < 4; u++) {
+            const Eight e = y[u].eight();
+            if (b + u <= lo)
+#pragma unroll
+                for (int j = 0; j < 4; j++) sum.v[j] = sum.v[j] + e.v[j];
         }
-    embedding_put<O, WIDE>(p, v, c, sum);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) sum.v[j] = fma2(sum.v[j], pair(p.scale), was.v[j]);
+    store_columns<WIDE>(out, c, t, n, p.H, sum);
 }
 
 } // namespace hapop

@@ -10,7 +10,7 @@ using namespace hapop;
 
 static bool dtype_fits(int32_t t) { return t == HAP_BF16 || t == HAP_FP16 || t == HAP_FP32; }
 // a matrix whose rows all begin at multiples of 16 bytes
-static bool wide(const void *p, int64_t ld, int32_t dtype) { return aligned(p, 16) && ld * size_of(dtype) % 16 == 0; }
+static bool wide(const void *p, int64_t ld, int32_t dtype) { return aligned(p, 16) && ld * size_of(dtype) % 16 == 0; }       // (beside H % 8 == 0)
 static bool grid_fits(int64_t blocks) { return blocks <= INT32_MAX; }
 
 // f(T()) of an element type
@@ -55,7 +55,7 @@ static hap_status run_route(RouteArgs p, int32_t dtype, bool backward, cudaStrea
     const RouteLayout at = route_layout(p.E, groups, p.per, p.lanes);
     p.slow = !backward && (!at.fits || (p.groups > 1 && p.best > 2));
     const bool dense = !p.sigmoid && !p.renormalise;        // (else the backward pass does not read whole rows)
-    if (at.PER == 8 && p.E / groups % 8 == 0 && (backward && !dense ? true : wide(p.z, p.ld, dtype)) && (!backward || wide(p.dz, p.ldd, dtype))) p.per = 8, p.eights = 1;
+    if (at.PER == 8 && p.E / groups % 8 == 0 && (backward && !dense ? true : wide(p.z, p.ld, dtype)) && (!backward || wide(p.dz, p.ldd, dtype)) && aligned(p.bias, 16)) p.per = 8, p.eights = 1;
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         switch (at.PER == 8 ? at.L : at.PER + 32) {
@@ -99,30 +99,27 @@ extern "C" hap_status hap_route_backward(const hap_routing *r, int32_t dtype, in
 }
 
 // ---- order by a key ------------------------------------------------------------------------------------------------------
-// Entries of a block and the blocks of a pass.  Up to 4096 entries are one block's, which spares the counting kernel.
+// Entries of a block and the blocks of a pass: a tile each, several where there would be more than 128 blocks
 struct OrderShape { int chunk, blocks; };
 static OrderShape order_shape(int64_t n)
 {
-    const int64_t unit = 32 * ORDER_WARPS;
-    int64_t chunk = n <= 4096 ? 4096 : 2048;
-    if (ceil_div(n, chunk) > 128) chunk = ceil_div(ceil_div(n, 128), unit) * unit;
-    const int64_t blocks = ceil_div(n, chunk);
-    return {(int)chunk, (int)(blocks < 1 ? 1 : blocks)};
+    const int64_t chunk = ceil_div(ceil_div(n < 1 ? 1 : n, 128), ORDER_TILE) * ORDER_TILE;
+    return {(int)chunk, (int)ceil_div(n < 1 ? 1 : n, chunk)};
 }
-static uint64_t order_bytes(int64_t n, int keys)
+static uint64_t order_bytes(int64_t n, int keys, int passes)
 {
     const OrderShape o = order_shape(n);
-    return o.blocks > 1 ? up256((uint64_t)o.blocks * keys * 4) : 0;
+    return o.blocks > 1 ? up256((uint64_t)o.blocks * keys * passes * 4) : 0;
 }
 template <int WHAT> static hap_status run_order(OrderArgs &p, cudaStream_t s)
 {
     const OrderShape o = order_shape(p.n);
     p.chunk = o.chunk;
-    if (o.blocks > 1) {
+    if (o.blocks > 1 && p.pass == 0) {
         const hap_status st = launch_next(order_count_kernel<WHAT>, o.blocks, 32 * ORDER_WARPS, 0, 1, s, p);
         if (st != HAP_OK) return st;
     }
-    return launch_next(order_place_kernel<WHAT>, o.blocks, 32 * ORDER_WARPS, ORDER_WARPS * p.keys * 4, 1, s, p);
+    return launch_next(order_place_kernel<WHAT>, o.blocks, 32 * ORDER_WARPS, ORDER_WARPS * ((p.keys + 1) & ~1) * 2, 1, s, p);
 }
 
 static bool order_sizes(int64_t rows, int32_t k, int32_t E) { return rows >= 0 && rows <= INT32_MAX && k >= 1 && k <= MOST_CHOSEN && rows * k <= INT32_MAX && E >= 1 && E <= MOST_KEYS; }
@@ -130,7 +127,7 @@ static bool order_sizes(int64_t rows, int32_t k, int32_t E) { return rows >= 0 &
 extern "C" hap_status hap_expert_order_workspace(int64_t rows, int32_t k, int32_t E, uint64_t *host_bytes)
 {
     if (!host_bytes || !order_sizes(rows, k, E)) return HAP_E_INVALID;
-    *host_bytes = order_bytes(rows * k, E);
+    *host_bytes = order_bytes(rows * k, E, 1);
     return HAP_OK;
 }
 
@@ -142,7 +139,7 @@ extern "C" hap_status hap_expert_order(int64_t rows, int32_t k, int32_t first, i
     if (rows > 0 && (!experts || !places)) return HAP_E_INVALID;
     if (need && (!workspace || bytes < need || !aligned(workspace, 256))) return HAP_E_INVALID;
     OrderArgs p{};
-    p.n = rows * k, p.keys = E, p.counts = (int *)workspace, p.experts = experts, p.first = first, p.places = places, p.offsets = offsets;
+    p.n = rows * k, p.keys = E, p.passes = 1, p.counts = (int *)workspace, p.experts = experts, p.first = first, p.places = places, p.offsets = offsets;
     return run_order<BY_EXPERT>(p, (cudaStream_t)stream);
 }
 
@@ -165,7 +162,7 @@ extern "C" hap_status hap_expert_dispatch(int32_t dtype, int64_t rows, int32_t k
     p.rows = rows, p.placed = placed, p.k = k, p.H = H, p.piece = piece_of(rows, H), p.places = places, p.x = x, p.ldx = ldx, p.out = out, p.ldo = ldo;
     const int64_t blocks = ceil_div(rows * ceil_div(H, p.piece), 8);
     if (!grid_fits(blocks)) return HAP_E_RANGE;
-    const bool w = wide(x, ldx, dtype) && wide(out, ldo, dtype);
+    const bool w = H % 8 == 0 && wide(x, ldx, dtype) && wide(out, ldo, dtype);
     return launch_next(dtype == HAP_FP32 ? w ? dispatch_kernel<uint32_t, true> : dispatch_kernel<uint32_t, false> : w ? dispatch_kernel<uint16_t, true> : dispatch_kernel<uint16_t, false>, blocks,
                        256, 0, 1, (cudaStream_t)stream, p);
 }
@@ -180,11 +177,11 @@ extern "C" hap_status hap_expert_combine(int32_t dtype, int64_t rows, int32_t k,
     if (rows == 0) return HAP_OK;
     if ((!y && placed > 0) || !places || !out) return HAP_E_INVALID;
     RowsArgs p{};
-    p.rows = rows, p.placed = placed, p.k = k, p.H = H, p.piece = piece_of(rows, H), p.places = places, p.weights = weights, p.y = y, p.ldy = ldy, p.base = base, p.ldbase = ldbase;
+    p.rows = rows, p.placed = placed, p.k = k, p.H = H, p.piece = (int)(piece_of(rows, H) < 1024 ? piece_of(rows, H) : 1024), p.places = places, p.weights = weights, p.y = y, p.ldy = ldy, p.base = base, p.ldbase = ldbase;
     p.out = out, p.ldo = ldo;
     const int64_t blocks = ceil_div(rows * ceil_div(H, p.piece), 8);
     if (!grid_fits(blocks)) return HAP_E_RANGE;
-    const bool w = wide(y, ldy, dtype) && wide(out, ldo, dtype) && (!base || wide(base, ldbase, dtype));
+    const bool w = H % 8 == 0 && wide(y, ldy, dtype) && wide(out, ldo, dtype) && (!base || wide(base, ldbase, dtype));
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         return launch_next(w ? combine_kernel<T, true> : combine_kernel<T, false>, blocks, 256, 0, 1, (cudaStream_t)stream, p);
@@ -202,7 +199,7 @@ extern "C" hap_status hap_expert_combine_backward(int32_t dtype, int64_t rows, i
     if (!dout || !places || (dweights && placed > 0 && !y)) return HAP_E_INVALID;
     RowsArgs p{};
     p.rows = rows, p.placed = placed, p.k = k, p.H = H, p.places = places, p.weights = weights, p.x = dout, p.ldx = lddout, p.y = y, p.ldy = ldy, p.out = dy, p.ldo = lddy, p.dweights = dweights;
-    const bool w = wide(dout, lddout, dtype) && (!dweights || wide(y, ldy, dtype)) && (!dy || wide(dy, lddy, dtype));
+    const bool w = H % 8 == 0 && wide(dout, lddout, dtype) && (!dweights || wide(y, ldy, dtype)) && (!dy || wide(dy, lddy, dtype));
     // four warps for a row; eight where there are too few rows for the device
     const int64_t most = ceil_div(H, 256), want = rows < 148 * 8 ? 8 : 4;
     const int threads = (int)(32 * (most < want ? most : want));
@@ -213,8 +210,6 @@ extern "C" hap_status hap_expert_combine_backward(int32_t dtype, int64_t rows, i
 }
 
 // ---- embedding -----------------------------------------------------------------------------------------------------------
-constexpr int EMBEDDING_CHUNK = 32;             // sorted tokens of a block: the header says so too
-
 static bool embedding_sizes(int64_t n, int32_t H, int64_t V) { return n >= 0 && n <= INT32_MAX && H >= 1 && H < (1 << 28) && V >= 1 && V < (1 << 28); }
 
 extern "C" hap_status hap_embedding(int32_t dtype, int64_t n, int32_t H, int64_t V, int64_t first, const int64_t *tokens, const void *w, int64_t ldw, float scale, void *out, int64_t ldo,
@@ -227,7 +222,7 @@ extern "C" hap_status hap_embedding(int32_t dtype, int64_t n, int32_t H, int64_t
     p.n = n, p.first = first, p.H = H, p.V = (int)V, p.tokens = tokens, p.w = w, p.ldw = ldw, p.out = out, p.ldo = ldo, p.scale = scale, p.piece = piece_of(n, H);
     const int64_t blocks = ceil_div(n * ceil_div(H, p.piece), 8);
     if (!grid_fits(blocks)) return HAP_E_RANGE;
-    const bool wd = wide(w, ldw, dtype) && wide(out, ldo, dtype);
+    const bool wd = H % 8 == 0 && wide(w, ldw, dtype) && wide(out, ldo, dtype);
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
         return launch_next(wd ? embedding_kernel<T, true> : embedding_kernel<T, false>, blocks, 256, 0, 1, (cudaStream_t)stream, p);
@@ -250,7 +245,7 @@ static EmbeddingSpace embedding_space(int64_t n, int64_t H, int64_t V)
     EmbeddingSpace s;
     s.other = up256((uint64_t)n * 8);
     s.counts = s.other + (d.passes > 1 ? up256((uint64_t)n * 8) : 0);
-    s.present = s.counts + order_bytes(n, 1 << d.bits);
+    s.present = s.counts + order_bytes(n, 1 << d.bits, d.passes);
     s.parts = s.present + up256((uint64_t)(V + 31) / 32 * 4);
     s.bytes = s.parts + (n > EMBEDDING_CHUNK ? up256((uint64_t)ceil_div(n, EMBEDDING_CHUNK) * 2 * H * 4) : 0);
     return s;
@@ -278,38 +273,30 @@ extern "C" hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, i
     uint2 *a = (uint2 *)space, *b = (uint2 *)(space + at.other);
     const Digits d = digits_of(V);
     OrderArgs o{};
-    o.n = n, o.keys = 1 << d.bits, o.mask = o.keys - 1, o.counts = (int *)(space + at.counts), o.tokens = tokens, o.first_token = first, o.V = (int)V;
+    o.n = n, o.keys = 1 << d.bits, o.bits = d.bits, o.passes = d.passes, o.counts = (int *)(space + at.counts), o.tokens = tokens, o.first_token = first, o.V = (int)V;
     o.present = accumulate ? nullptr : (unsigned *)(space + at.present);
     o.to = a;
     hap_status st = run_order<BY_TOKEN>(o, s);
     for (int i = 1; i < d.passes && st == HAP_OK; i++) {
-        o.from = i & 1 ? a : b, o.to = i & 1 ? b : a, o.shift = i * d.bits;
+        o.from = i & 1 ? a : b, o.to = i & 1 ? b : a, o.shift = i * d.bits, o.pass = i;
         st = run_order<BY_PAIR>(o, s);
     }
     if (st != HAP_OK) return st;
     EmbeddingArgs p{};
-    p.n = n, p.H = H, p.V = (int)V, p.chunk = EMBEDDING_CHUNK, p.accumulate = accumulate != 0, p.scale = scale, p.x = dy, p.ldx = lddy, p.out = dw, p.ldo = lddw;
+    p.n = n, p.H = H, p.V = (int)V, p.accumulate = accumulate != 0, p.scale = scale, p.x = dy, p.ldx = lddy, p.out = dw, p.ldo = lddw;
     p.sorted = o.to, p.parts = (float *)(space + at.parts), p.present = o.present;
-    const bool w = wide(dy, lddy, dtype) && wide(dw, lddw, out_dtype);
-    const int64_t chunks = ceil_div(n, p.chunk), threads = ceil_div(H, 8) < 256 ? ceil_div(ceil_div(H, 8), 32) * 32 : 256;
-    const unsigned columns = (unsigned)ceil_div(H, 8 * threads);
-    if (columns > 65535) return HAP_E_RANGE;
-    auto launch = [&](auto kernel, int64_t x, unsigned y, int64_t threads) {
-        cudaLaunchConfig_t c = shape_of(x, (int)threads, 0, s);
-        c.gridDim.y = y;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization, attr.val.programmaticStreamSerializationAllowed = 1;
-        c.attrs = &attr, c.numAttrs = 1;
-        return start(kernel, c, p);
-    };
+    const bool w = H % 8 == 0 && wide(dy, lddy, dtype) && wide(dw, lddw, out_dtype);
+    const int threads = (int)(ceil_div(H, 8) < 256 ? ceil_div(ceil_div(H, 8), 32) * 32 : 256);
+    const int64_t chunks = ceil_div(n, EMBEDDING_CHUNK), columns = ceil_div(H, 8 * threads), rows = ceil_div(V, threads / 32);
+    if (!grid_fits(chunks * columns + 148 * 8)) return HAP_E_RANGE;
+    p.columns = (int)columns, p.sums = (int)(chunks * columns);
+    const int64_t clear = accumulate ? 0 : rows < 148 * 8 ? rows : 148 * 8;
     auto all = [&](auto t, auto u) {
         using T = decltype(t);
         using O = decltype(u);
-        hap_status st = HAP_OK;
-        if (!accumulate) st = launch(w ? embedding_clear_kernel<O, true> : embedding_clear_kernel<O, false>, V < 148 * 8 * 8 ? ceil_div(V, 8) : 148 * 8, 1, 256);
-        if (st == HAP_OK && n > 0) st = launch(w ? embedding_sum_kernel<T, O, true> : embedding_sum_kernel<T, O, false>, chunks, columns, threads);
-        if (st == HAP_OK && chunks > 1) st = launch(w ? embedding_join_kernel<O, true> : embedding_join_kernel<O, false>, chunks - 1, columns, threads);
-        return st;
+        const hap_status st = launch_next(w ? embedding_gradient_kernel<T, O, true> : embedding_gradient_kernel<T, O, false>, p.sums + clear, threads, 0, 1, s, p);
+        if (st != HAP_OK || chunks < 2) return st;
+        return launch_next(w ? embedding_join_kernel<O, true> : embedding_join_kernel<O, false>, (chunks - 1) * columns, threads, 0, 1, s, p);
     };
     return by_type(dtype, [&](auto t) { return out_dtype == dtype ? all(t, t) : all(t, float()); });
 }
@@ -317,16 +304,48 @@ extern "C" hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, i
 // ---- layer norm ----------------------------------------------------------------------------------------------------------
 static bool norm_sizes(int64_t rows, int32_t H) { return rows >= 0 && rows <= INT32_MAX && H >= 1 && H <= MOST_NORM; }
 
-// Rows whose sums of dw and db a block of the backward pass holds: the blocks are as many as the device runs at once (two of up to 1024
-// threads, or as many threads in smaller ones), fewer where there are fewer rows.
-static int norm_threads(int32_t H, int eights)
+// A row's threads, two eights of columns each, and how many rows a device of 148 multiprocessors works on at once: 1024 threads of
+// each, or as many as there is shared memory for, whose `row_bytes` hold the row that is worked on and the next.
+constexpr int NORM_EIGHTS = 2;
+static int norm_threads(int32_t H, int eights) { return (int)(ceil_div(ceil_div(H, 8 * eights), 32) * 32); }
+static int norm_high(int threads) { return threads == 32 ? 4 : 1; }             // rows of a block
+static int64_t norm_bytes(int32_t H, int arrays, int32_t dtype) { return (int64_t)arrays * 8 * NORM_EIGHTS * norm_threads(H, NORM_EIGHTS) * size_of(dtype); }
+static int64_t norm_rows_at_once(int32_t H, int64_t row_bytes, int most)
 {
-    return (int)(ceil_div(ceil_div(H, 8 * eights), 32) * 32);
+    const int64_t threads = norm_threads(H, NORM_EIGHTS), by_threads = most / threads, by_bytes = (220 << 10) / (row_bytes + 1024);
+    const int64_t n = by_threads < by_bytes ? by_threads : by_bytes;
+    return 148 * (n < 1 ? 1 : n);
 }
-static int64_t norm_blocks(int64_t rows, int32_t H)
+// Rows of partial sums: not more than a quarter of the rows, so that there is something to sum, but one for each multiprocessor
+static int64_t norm_parts(int64_t rows, int32_t H, int64_t row_bytes)
 {
-    const int64_t threads = norm_threads(H, 2), at_once = 148 * (1024 / threads < 1 ? 1 : 1024 / threads);
-    return rows < at_once ? rows : at_once;
+    const int64_t at_once = norm_rows_at_once(H, row_bytes, 682), few = rows < 148 ? rows : rows / 4 < 148 ? 148 : rows / 4;
+    const int64_t n = few < at_once ? few : at_once, high = norm_high(norm_threads(H, NORM_EIGHTS));
+    return ceil_div(n, high) * high;
+}
+
+// the kernel may have this much shared memory, on this device
+template <auto KERNEL> static hap_status allow_shared(Device d, int64_t bytes)
+{
+    static std::atomic<uint64_t> allowed;
+    const uint64_t bit = d.id < DEVICES ? 1ull << d.id : 0;
+    if (bytes <= 40 << 10 || (allowed.load(std::memory_order_relaxed) & bit)) return HAP_OK;
+    if (status_of(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 << 10)) != HAP_OK) return HAP_E_CUDA;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+    return HAP_OK;
+}
+template <auto KERNEL> static hap_status launch_norm(const NormArgs &p, int64_t blocks, int threads, int high, int64_t bytes, cudaStream_t s)
+{
+    const Device d = device();
+    if (!d.sms) return HAP_E_CUDA;
+    const hap_status st = allow_shared<KERNEL>(d, bytes);
+    if (st != HAP_OK) return st;
+    cudaLaunchConfig_t c = shape_of(blocks, threads, (int)bytes, s);
+    c.blockDim.y = high;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization, attr.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &attr, c.numAttrs = 1;
+    return start(KERNEL, c, p);
 }
 
 extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t centred, int64_t rows, int32_t H, const void *x, int64_t ldx, const void *w, const void *b, float eps, void *y,
@@ -338,24 +357,22 @@ extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t
     if (rows == 0) return HAP_OK;
     if (!x || !y) return HAP_E_INVALID;
     NormArgs p{};
-    p.rows = rows, p.H = H, p.eps = eps, p.x = x, p.ldx = ldx, p.w = w, p.b = b, p.y = y, p.ldy = ldy, p.mean = mean, p.rstd = rstd;
-    const bool wd = wide(x, ldx, dtype) && wide(y, ldy, dtype) && aligned(w, 16) && aligned(b, 16);
-    // as few threads for a row as hold it in four eights each; one eight each where there are few rows
-    const bool few = rows < 148 * 4 && H <= 8192;
-    const int threads = norm_threads(H, few ? 1 : H > 4096 * 2 ? 2 : 4), high = threads == 32 ? 4 : 1;
-    cudaLaunchConfig_t c = shape_of(ceil_div(rows, high), threads, 0, (cudaStream_t)stream);
-    c.blockDim.y = high;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization, attr.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &attr, c.numAttrs = 1;
+    p.rows = rows, p.H = H, p.inverse = 1.0f / (float)H, p.eps = eps, p.x = x, p.ldx = ldx, p.w = w, p.b = b, p.y = y, p.ldy = ldy, p.mean = mean, p.rstd = rstd;
+    const bool wd = H % 8 == 0 && wide(x, ldx, dtype) && wide(y, ldy, dtype) && aligned(w, 16) && aligned(b, 16);
+    cudaStream_t s = (cudaStream_t)stream;
+    // few rows: one eight for each thread (up to 8192 columns), and every row a block of its own
+    const bool few = rows < 148 * 4;
     auto run = [&](auto t, auto u) {
         using T = decltype(t);
         using P = decltype(u);
         auto pick = [&](auto centre) {
             constexpr bool C = decltype(centre)::value;
-            if (few) return start(wd ? norm_kernel<T, P, 1, true, C> : norm_kernel<T, P, 1, false, C>, c, p);
-            if (H > 8192) return start(wd ? norm_kernel<T, P, 2, true, C> : norm_kernel<T, P, 2, false, C>, c, p);
-            return start(wd ? norm_kernel<T, P, 4, true, C> : norm_kernel<T, P, 4, false, C>, c, p);
+            const int threads = norm_threads(H, few && H <= 8192 ? 1 : NORM_EIGHTS), high = norm_high(threads);
+            const int64_t blocks = ceil_div(rows, high);
+            if (few && H <= 8192) return wd ? launch_norm<norm_kernel<T, P, 1, false, true, C>>(p, blocks, threads, high, 0, s) : launch_norm<norm_kernel<T, P, 1, false, false, C>>(p, blocks, threads, high, 0, s);
+            const int64_t row_bytes = 2 * norm_bytes(H, 1, dtype), most = ceil_div(norm_rows_at_once(H, row_bytes, 1280), high), grid = blocks < most ? blocks : most;
+            return wd ? launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, true, C>>(p, grid, threads, high, high * row_bytes, s)
+                      : launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, false, C>>(p, grid, threads, high, high * row_bytes, s);
         };
         return centred ? pick(std::true_type()) : pick(std::false_type());
     };
@@ -365,7 +382,7 @@ extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t
 extern "C" hap_status hap_layer_norm_backward_workspace(int64_t rows, int32_t H, uint64_t *host_bytes)
 {
     if (!host_bytes || !norm_sizes(rows, H)) return HAP_E_INVALID;
-    *host_bytes = up256((uint64_t)norm_blocks(rows, H) * 2 * H * 4);
+    *host_bytes = up256((uint64_t)norm_parts(rows, H, 0) * 2 * H * 4);      // (as for rows that need no shared memory)
     return HAP_OK;
 }
 
@@ -385,23 +402,28 @@ extern "C" hap_status hap_layer_norm_backward(int32_t dtype, int32_t param_dtype
     if (sums && need && (!workspace || bytes < need || !aligned(workspace, 256))) return HAP_E_INVALID;
     if ((!dx && !sums) || (rows == 0 && (!sums || accumulate))) return HAP_OK;
     NormArgs p{};
-    p.rows = rows, p.H = H, p.blocks = (int)norm_blocks(rows, H), p.add = accumulate != 0, p.x = x, p.ldx = ldx, p.w = w, p.dy = dy, p.lddy = lddy, p.base = base, p.ldbase = ldbase;
+    p.rows = rows, p.H = H, p.inverse = 1.0f / (float)H, p.add = accumulate != 0, p.x = x, p.ldx = ldx, p.w = w, p.dy = dy, p.lddy = lddy, p.base = base, p.ldbase = ldbase;
     p.dx = dx, p.lddx = lddx, p.dw = dw, p.db = db, p.mean = (float *)mean, p.rstd = (float *)rstd, p.parts = sums ? (float *)workspace : nullptr;
     cudaStream_t s = (cudaStream_t)stream;
-    const bool wd = wide(x, ldx, dtype) && wide(dy, lddy, dtype) && (!base || wide(base, ldbase, dtype)) && (!dx || wide(dx, lddx, dtype)) && aligned(w, 16);
+    const bool wd = H % 8 == 0 && wide(x, ldx, dtype) && wide(dy, lddy, dtype) && (!base || wide(base, ldbase, dtype)) && (!dx || wide(dx, lddx, dtype)) && aligned(w, 16);
+    const int64_t one = norm_bytes(H, base ? 3 : 2, dtype);
+    p.ahead = 2 * one <= 224 << 10;                         // (rows of more than 9500 values in 32 bits fill the shared memory alone)
+    const int64_t row_bytes = (1 + p.ahead) * one;
+    p.blocks = (int)norm_parts(rows, H, row_bytes);
     auto run = [&](auto t, auto u) {
         using T = decltype(t);
         using P = decltype(u);
-        const int threads = norm_threads(H, 2);
+        const int threads = norm_threads(H, NORM_EIGHTS), high = norm_high(threads);
         auto pick = [&](auto centre, auto most) {
             constexpr bool C = decltype(centre)::value;
             constexpr int M = decltype(most)::value;
-            return launch_next(wd ? norm_backward_kernel<T, P, 2, M, true, C> : norm_backward_kernel<T, P, 2, M, false, C>, p.blocks, threads, 0, 1, s, p);
+            return wd ? launch_norm<norm_backward_kernel<T, P, NORM_EIGHTS, M, true, C>>(p, p.blocks / high, threads, high, high * row_bytes, s)
+                      : launch_norm<norm_backward_kernel<T, P, NORM_EIGHTS, M, false, C>>(p, p.blocks / high, threads, high, high * row_bytes, s);
         };
-        using Few = std::integral_constant<int, 512>;
+        using Few = std::integral_constant<int, 640>;
         using Many = std::integral_constant<int, 1024>;
-        if (centred) return threads <= 512 ? pick(std::true_type(), Few()) : pick(std::true_type(), Many());
-        return threads <= 512 ? pick(std::false_type(), Few()) : pick(std::false_type(), Many());
+        if (centred) return threads <= 640 ? pick(std::true_type(), Few()) : pick(std::true_type(), Many());
+        return threads <= 640 ? pick(std::false_type(), Few()) : pick(std::false_type(), Many());
     };
     hap_status st = rows > 0 ? by_type(dtype, [&](auto t) { return param_dtype == dtype ? run(t, t) : run(t, float()); }) : HAP_OK;
     if (st != HAP_OK || !sums) return st;

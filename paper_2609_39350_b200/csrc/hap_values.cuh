@@ -52,4 +52,13 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
 // values in front of the first one whose address, and those of the following eights, is a multiple of 16 bytes
 template <typename T> __device__ __forceinline__ int in_front(const T *p) { return (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)); }
 
+// 16 bytes to shared memory, on their way while the thread goes on, or 16 zeros where `bytes` is 0; it sees them itself behind
+// copies_arrived<0>(), and no other thread is meant to.  copies_arrived<N>: all but the last N groups are there.
+__device__ __forceinline__ void copy16(void *to, const void *from, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 } // namespace hapop
