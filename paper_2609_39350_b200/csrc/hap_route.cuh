@@ -8,7 +8,7 @@
 namespace hapop {
 
 constexpr int MOST_EXPERT_GROUPS = 32;
-constexpr int ROUTE_WARPS = 4;
+constexpr int ROUTE_WARPS = 4, ROUTE_BLOCKS = 5;       // of a block; blocks of a multiprocessor
 constexpr float NONE = -INFINITY;
 
 struct RouteArgs {
@@ -17,7 +17,7 @@ struct RouteArgs {
     const float *bias;              // null: none
     int E, k, sigmoid, groups, kept, best, renormalise;
     float scale;
-    int per, lanes;                 // of a row's lanes, `lanes` hold a group, `per` experts each
+    int size, per, lanes_log;       // experts of a group; of a row's lanes, 2^lanes_log hold a group, `per` experts each
     int slow, eights;               // all rows the slow way; logits (and their gradients) are read (written) in eights
     int *experts;                   // [rows][k]
     float *weights;
@@ -62,9 +62,9 @@ __device__ __forceinline__ float sigmoid_score(float z, float m) { return z <= 0
 // One row by a whole warp with values in 64 bits: for rows whose values 32 bits cannot tell apart, and for layouts of groups that do
 // not fit the lanes.  space: E doubles of this warp's own.
 struct RowStart { float m, sum; bool bad; };
-template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteArgs &p, int64_t row, double *space, int *ce, float *cz)
+template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteArgs &p, int64_t row, double *space, int *ce)
 {
-    const int lane = threadIdx.x & 31, size = p.E / p.groups;
+    const int lane = threadIdx.x & 31, size = p.size;
     const T *z = (const T *)p.z + row * p.ld;
     float top = NONE;
     bool bad = false;
@@ -128,7 +128,7 @@ template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteA
         }
         const bool any = most > -INFINITY;
         if (lane == 0) {
-            ce[j] = any ? who : -1, cz[j] = any ? to_float(z[who]) : NONE;
+            ce[j] = any ? who : -1;
             if (any) space[who] = -INFINITY;
         }
         __syncwarp();
@@ -136,158 +136,245 @@ template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteA
     return {(float)m, (float)sum, false};
 }
 
-// L lanes for a row, up to PER experts each.  Values are in 32 bits; the choice is the same as in exact arithmetic where
-// neighbours in the order are further apart than both are off, and the row is done once more in 64 bits where they are not.
-template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(const RouteArgs p)
+// Values that 32 bits cannot tell apart among the chosen of a row and the one behind them (entries of ce, k + 1 at most 32): they are put
+// in order by their values in 64 bits, a lane for each.
+template <typename T> __device__ __noinline__ void route_settle(const RouteArgs &p, int64_t row, int *ce)
 {
-    extern __shared__ double space[];                       // E for each warp, then the chosen of each row
+    const int lane = threadIdx.x & 31;
+    const T *z = (const T *)p.z + row * p.ld;
+    double m = 0, sum = 1;
+    if (!p.sigmoid && p.bias) {
+        float top = NONE;
+        for (int e = lane; e < p.E; e += 32) top = fmaxf(top, to_float(z[e]));
+        m = most_of<32>(top), sum = 0;
+        for (int e = lane; e < p.E; e += 32) sum += exp((double)to_float(z[e]) - m);
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    }
+    const int e = lane <= p.k ? ce[lane] : -1;
+    const double x = e >= 0 ? to_float(z[e]) : 0.0;
+    const double v = e < 0 ? -INFINITY : !p.bias ? x : (p.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - m) / sum) + p.bias[e];
+    int ahead = 0;
+    for (int j = 0; j <= p.k; j++) {
+        const double other = __shfl_sync(~0u, v, j);
+        const int its = __shfl_sync(~0u, e, j);
+        ahead += other > v || (other == v && its < e);
+    }
+    __syncwarp();
+    if (e >= 0) ce[ahead] = e;
+    __syncwarp();
+}
+
+// The larger of two, a NaN where one is
+__device__ __forceinline__ float most_or_nan(float x, float y) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
+
+// Descending order of the N numbers from LO on: halves put in order and merged, Batcher's way.  All of it is laid out at compile time
+// (left as loops the numbers were in local memory, and a row took three times the instructions).
+template <int LO, int N, int R, int ALL> __device__ __forceinline__ void merged(uint32_t (&x)[ALL])
+{
+    auto exchange = [&](int i) { const uint32_t a = x[i], b = x[i + R]; x[i] = max(a, b), x[i + R] = min(a, b); };
+    if constexpr (2 * R < N) {
+        merged<LO, N, 2 * R>(x), merged<LO + R, N, 2 * R>(x);
+#pragma unroll
+        for (int i = LO + R; i + R < LO + N; i += 2 * R) exchange(i);
+    } else exchange(LO);
+}
+template <int LO, int N, int ALL> __device__ __forceinline__ void in_order(uint32_t (&x)[ALL])
+{
+    if constexpr (N > 1) in_order<LO, N / 2>(x), in_order<LO + N / 2, N / 2>(x), merged<LO, N, 1>(x);
+}
+
+// L lanes for a row, up to PER experts each.  Values are in 32 bits, without the last few, where an expert's place in its lane stands;
+// the choice is the same as in exact arithmetic where neighbours in the order are further apart than both are off, and the row is done
+// once more in 64 bits where they are not.  Bound by instructions: a lane's values are put in order once, so that taking the largest
+// k of a row is one maximum over the lanes and a shift in one of them each (600 instructions for a row of 256 with a bias and groups).
+template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROUTE_WARPS, PER == 32 ? 4 : ROUTE_BLOCKS) route_kernel(const RouteArgs p)
+{
+    extern __shared__ double space[];                       // E for each warp, then for each row the chosen and their keys, two more
     constexpr int ROWS = 32 / L;
+    constexpr uint32_t PLACES = PER - 1, LEAST = 0x007fffff;     // (-inf's)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (L - 1);
+    int *ce = (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + lane / L) * 2 * (p.k + 2);
+    uint32_t *keys = (uint32_t *)(ce + p.k + 2);
+    const unsigned mine = lanes_of<L>(lane);
+    const int lanes = 1 << p.lanes_log, group = sub >> p.lanes_log, from = (sub & (lanes - 1)) * p.per, first = group * p.size + from;
+    const int own = group < p.groups ? max(0, min(p.per, p.size - from)) : 0;          // experts of this lane
     launch_next();
     wait_for_last();
-    const int64_t row = ((int64_t)blockIdx.x * ROUTE_WARPS + warp) * ROWS + lane / L;
+    // a row's eights are read while the one before it is worked on
+    constexpr int EIGHTS = PER / 8;
+    Raw<T, true> next[EIGHTS];
+    auto bring = [&](int64_t row) {
+        const T *zr = (const T *)p.z + (row < p.rows ? row : 0) * p.ld;
+#pragma unroll
+        for (int i = 0; i < EIGHTS; i++) next[i].load(zr, own > 8 * i ? first + 8 * i : 0, 0, 0, 0);
+    };
+    const int64_t step = (int64_t)gridDim.x * ROUTE_WARPS * ROWS;
+    int64_t row = ((int64_t)blockIdx.x * ROUTE_WARPS + warp) * ROWS + lane / L;
+    if (p.eights && !p.slow) bring(row);
+  for (; row - lane / L < p.rows; row += step) {            // (a warp's rows together)
     const bool here = row < p.rows;
-    int *ce = (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + lane / L) * 2 * p.k;
-    float *cz = (float *)(ce + p.k);
-    const unsigned mine = lanes_of<L>(lane);
     float m = 0, sum = 1;
     bool bad = false, again = p.slow;
     if (!p.slow) {
-        const int size = p.E / p.groups, group = sub / p.lanes, from = (sub & (p.lanes - 1)) * p.per, first = group * size + from;
-        const int n = here && group < p.groups ? max(0, min(p.per, size - from)) : 0;
-        const T *zr = (const T *)p.z + row * p.ld + first;
+        const int n = here ? own : 0;
         float z[PER], v[PER];
-        if (PER == 8 && p.eights) {
-            float x[8];
-            if (n > 0) load8(zr, x);
+        if (p.eights) {
 #pragma unroll
-            for (int i = 0; i < PER; i++) z[i] = n > 0 ? x[i & 7] : NONE;
+            for (int i = 0; i < EIGHTS; i++) {
+                const Eight x = next[i].eight();
+#pragma unroll
+                for (int j = 0; j < 8; j++) z[8 * i + j] = n > 8 * i ? (j & 1 ? both(x.v[j / 2]).y : both(x.v[j / 2]).x) : NONE;
+            }
+            bring(row + step);
         } else {
+            const T *zr = (const T *)p.z + row * p.ld + first;
 #pragma unroll
             for (int i = 0; i < PER; i++) z[i] = i < n ? to_float(zr[i]) : NONE;
         }
-        const bool values = p.bias || (p.groups > 1 && p.best > 1);         // whether scores decide, or logits do
+        const bool sums = p.groups > 1 && p.best > 1;       // scores are added up
+        float most = z[0];
 #pragma unroll
-        for (int i = 0; i < PER; i++) bad |= isnan(z[i]) || (!p.sigmoid && z[i] == INFINITY);
-        float off = 0;                                                      // two values that are further apart are in order
-        if (!p.sigmoid && (values || !p.renormalise)) {
-#pragma unroll
-            for (int i = 0; i < PER; i++) m = i ? fmaxf(m, z[i]) : z[0];
-            m = most_of<L>(m);
+        for (int i = 1; i < PER; i++) most = most_or_nan(most, z[i]);
+        bad = isnan(most) || (!p.sigmoid && most == INFINITY);
+        if (!p.sigmoid && (p.bias || sums || !p.renormalise)) {
+            m = most_of<L>(most);
             if (m == NONE) m = 0;
             sum = 0;
 #pragma unroll
             for (int i = 0; i < PER; i++) sum += p.renormalise ? __expf(z[i] - m) : expf(z[i] - m);        // (a weight's, or the choice's alone)
             sum = sum_of<L>(sum);
         }
-#pragma unroll
-        for (int i = 0; i < PER; i++) v[i] = z[i];
-        if (values) {
-            // What a score is off by.  Sigmoid: e^-z by 2^-22 + 1.5 |z| 2^-23 of itself, which s (1 - s) takes to 1e-7, two
-            // roundings and the quotient 3e-7.  Softmax: of the largest score, 2^-22 for the term and the sum's up to 37 roundings,
-            // 2.5e-6 in all.  `off` is at least what two values differ by wrongly; a sum with the bias has a rounding of its own.
-            const float inverse = __fdividef(1.0f, sum);
-            off = p.sigmoid ? 1.5e-6f : 6e-6f * inverse;
+        // What a score is off by.  Sigmoid: e^-z by 2^-22 + 1.5 |z| 2^-23 of itself, which s (1 - s) takes to 1e-7, two roundings and
+        // the quotient 3e-7.  Softmax: of the largest score, 2^-22 for the term and the sum's up to 37 roundings, 2.5e-6 in all.
+        // `off` is at least what two values differ by wrongly; a sum with the bias has a rounding of its own.
+        const float inverse = sum > 0.0f ? __fdividef(1.0f, sum) : 0.0f, off = p.sigmoid ? 8e-7f : 6e-6f * inverse;
+        auto score = [&](float x) { return p.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-x)) : __expf(x - m) * inverse; };
+        if (p.bias) {
             float b[PER];
-            if (!p.bias) {
+            if (p.eights) {
 #pragma unroll
-                for (int i = 0; i < PER; i++) b[i] = 0;
-            } else if (PER == 8 && p.eights) {
-                float x[8];
-                load8(p.bias + (n > 0 ? first : 0), x);
+                for (int i = 0; i < EIGHTS; i++) {
+                    float x[8];
+                    load8(p.bias + (n > 8 * i ? first + 8 * i : 0), x);
 #pragma unroll
-                for (int i = 0; i < PER; i++) b[i] = x[i & 7];
+                    for (int j = 0; j < 8; j++) b[8 * i + j] = x[j];
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < PER; i++) b[i] = i < n ? p.bias[first + i] : 0.0f;
             }
+            float top = 0;
 #pragma unroll
-            for (int i = 0; i < PER; i++) {
-                bad |= isnan(b[i]) || b[i] == INFINITY;
-                const float s = p.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-z[i])) : __expf(z[i] - m) * inverse;
-                v[i] = z[i] == NONE || b[i] == NONE ? NONE : s + b[i];
-            }
+            for (int i = 0; i < PER; i++) v[i] = score(z[i]) + b[i], top = most_or_nan(top, v[i]), v[i] = z[i] == NONE ? NONE : v[i];
+            bad |= !(top < INFINITY);                       // (of a bias that is no number, or +inf)
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; i++) v[i] = z[i];
         }
-        bad = (__ballot_sync(~0u, bad) & mine) != 0;
+        bad = (__ballot_sync(~0u, bad && here) & mine) != 0;
         if (p.groups > 1) {
             float a = NONE, b = NONE;                       // a group's largest and the next
 #pragma unroll
             for (int i = 0; i < PER; i++) b = fmaxf(b, fminf(a, v[i])), a = fmaxf(a, v[i]);
-            for (int d = p.lanes / 2; d; d /= 2) {
+            for (int d = lanes / 2; d; d /= 2) {
                 const float c = __shfl_xor_sync(~0u, a, d), e = __shfl_xor_sync(~0u, b, d);
                 b = fmaxf(fminf(a, c), fmaxf(b, e)), a = fmaxf(a, c);
             }
-            const float total = p.best > 1 && b > NONE ? a + b : a;
+            const bool any = a > NONE, two = b > NONE;
+            if (sums && !p.bias) a = score(a), b = score(b);
+            const float total = !any ? NONE : sums && two ? a + b : a;
             int ahead = 0;
-            for (int g = 0; g < L / p.lanes; g++) {
-                const float other = __shfl_sync(~0u, total, (lane & ~(L - 1)) + g * p.lanes);
+            for (int g = 0; g < p.groups; g++) {
+                const float other = __shfl_sync(~0u, total, g << p.lanes_log, L);
                 ahead += other > total || (other == total && g < group);
             }
-            const bool kept = ahead < p.kept;
-            if (values) {
-                const float low = -most_of<L>(kept && total > NONE ? -total : NONE), high = most_of<L>(kept ? NONE : total);
-                again |= low < INFINITY && high > NONE && low - high <= 2 * off + 4e-7f * (fabsf(low) + fabsf(high));
+            const bool kept = ahead < p.kept && any;
+            if (p.bias || sums) {
+                const uint32_t low = ~most_of<L>(kept ? ~ordered(total) : 0u), high = most_of<L>(!kept && any ? ordered(total) : 0u);
+                const float x = from_ordered(low), y = from_ordered(high);
+                again |= high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
             }
+            if (!kept)
 #pragma unroll
-            for (int i = 0; i < PER; i++) v[i] = !kept || v[i] == NONE ? NONE : p.bias ? v[i] : z[i];
+                for (int i = 0; i < PER; i++) v[i] = NONE;
         }
-        // The largest k as whole numbers, which order as the values do, 0 for none: the row's largest of the lanes' largest, taken
-        // from the first lane that has it and there from the first place.
-        uint32_t key[PER], best = 0;
+        // A value as a whole number that orders as it does, up to LEAST for none, with its place among the lane's in the last bits
+        uint32_t key[PER];
 #pragma unroll
-        for (int i = 0; i < PER; i++) key[i] = v[i] == NONE ? 0 : ordered(v[i]), best = max(best, key[i]);
-        const bool check = p.bias;                          // (without one the logits decide in the groups)
-        uint32_t last = ~0u;
-        for (int j = 0; j < p.k + check; j++) {
-            const uint32_t top = most_of<L>(best);
-            const unsigned who = __ballot_sync(~0u, best == top) & mine;
-            if (check && top && j > 0) {
-                const float x = from_ordered(last), y = from_ordered(top);
-                again |= x - y <= off + 2e-7f * (fabsf(x) + fabsf(y));
-            }
-            last = top;
+        for (int i = 0; i < PER; i++) key[i] = (ordered(v[i]) & ~PLACES) | (PLACES - i);
+        in_order<0, PER>(key);
+        const bool check = p.bias || sizeof(T) == 4;        // (logits in 16 bits lose nothing with their last bits)
+        const int rounds = check ? p.k + 2 : p.k;
+        for (int j = 0; j < rounds; j++) {
+            const uint32_t head = key[0] & ~PLACES, top = most_of<L>(head);
+            const unsigned who = __ballot_sync(~0u, head == top) & mine;           // (the first lane of several)
             if (lane == __ffs(who) - 1) {
-                int at = PER - 1;
-                float x = z[PER - 1];
+                ce[j] = top > LEAST ? first + (int)(PLACES - (key[0] & PLACES)) : -1, keys[j] = top;
 #pragma unroll
-                for (int i = PER - 2; i >= 0; i--)
-                    if (key[i] == top) at = i, x = z[i];
-                best = 0;
-#pragma unroll
-                for (int i = 0; i < PER; i++) key[i] = i == at ? 0 : key[i], best = max(best, key[i]);
-                if (j < p.k) ce[j] = top ? first + at : -1, cz[j] = top ? x : NONE;
+                for (int i = 0; i + 1 < PER; i++) key[i] = key[i + 1];
+                key[PER - 1] = 0;
             }
+        }
+        __syncwarp();
+        // Neighbours that may be the other way round: the chosen and the one behind them are settled by themselves; where the one behind
+        // these may be among them too, the whole row is done again.
+        bool near = false, at_end = false, behind = false;
+        for (int j = sub + 1; check && j < rounds; j += L) {
+            if (keys[j] <= LEAST) continue;
+            const float x = from_ordered(keys[j - 1]), y = from_ordered(keys[j]);          // (logits in 32: where what is left is equal)
+            const bool is = p.bias ? x - y <= off + PER * 1.2e-7f * fmaxf(fabsf(x), fabsf(y)) : keys[j - 1] == keys[j];
+            near |= is && j <= p.k, at_end |= is && j == p.k, behind |= is && j == p.k + 1;
+        }
+        near = (__ballot_sync(~0u, near) & mine) != 0, at_end = (__ballot_sync(~0u, at_end) & mine) != 0, behind = (__ballot_sync(~0u, behind) & mine) != 0;
+        again |= (at_end && behind) || (near && p.k == 32);
+        again = (__ballot_sync(~0u, again) & mine) != 0;
+        for (unsigned left = __ballot_sync(~0u, sub == 0 && here && near && !again && !bad); left; left &= left - 1) {
+            const int who = __ffs(left) - 1;
+            route_settle<T>(p, __shfl_sync(~0u, row, who), (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + who / L) * 2 * (p.k + 2));
         }
     }
     unsigned slow = __ballot_sync(~0u, sub == 0 && here && again && !bad);
     while (slow) {
         const int who = __ffs(slow) - 1;
         slow &= slow - 1;
-        int *to = (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + who / L) * 2 * p.k;
         __syncwarp();
-        const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.E, to, (float *)(to + p.k));
+        const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.E, (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + who / L) * 2 * (p.k + 2));
         if (lane / L == who / L) m = r.m, sum = r.sum, bad = r.bad;
     }
     __syncwarp();
-    float top = NONE, total = 0;
+    // the chosen's weights: a lane has number sub, sub + L, ...
+    constexpr int SLOTS = L >= 8 ? 32 / L : 8;              // (k is at most 32 and the lanes' experts, eight each where there are few lanes)
+    const T *z = (const T *)p.z + (here ? row : 0) * p.ld;
+    int e[SLOTS];
+    float x[SLOTS], top = NONE, total = 0;
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        e[q] = sub + q * L < p.k ? ce[sub + q * L] : -1;
+        x[q] = e[q] >= 0 && here ? to_float(z[e[q]]) : NONE;
+        top = fmaxf(top, x[q]);
+    }
     if (p.renormalise) {
-        for (int j = sub; j < p.k; j += L) top = fmaxf(top, cz[j]);
         top = most_of<L>(top);
         if (top == NONE) top = 0;
         if (p.sigmoid) top = fminf(top, 0.0f);
-        for (int j = sub; j < p.k; j += L) total += ce[j] < 0 ? 0.0f : p.sigmoid ? sigmoid_score(cz[j], top) : expf(cz[j] - top);
-        total = sum_of<L>(total);
+    } else top = p.sigmoid ? 0.0f : m;
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        x[q] = e[q] < 0 ? 0.0f : p.sigmoid ? sigmoid_score(x[q], top) : expf(x[q] - top);
+        total += x[q];
     }
-    if (!here) return;
-    for (int j = sub; j < p.k; j += L) {
-        float w = 0;
-        if (ce[j] >= 0) {
-            if (p.renormalise) w = (p.sigmoid ? sigmoid_score(cz[j], top) : expf(cz[j] - top)) / total;
-            else w = p.sigmoid ? sigmoid_score(cz[j], 0.0f) : expf(cz[j] - m) / sum;
-        }
-        p.experts[row * p.k + j] = bad ? j : ce[j];
-        p.weights[row * p.k + j] = bad ? NAN : w * p.scale;
+    if (p.renormalise) total = sum_of<L>(total);
+    else total = p.sigmoid ? 1.0f : sum;
+    const float by = p.scale / total;
+    __syncwarp();                                           // (the next row's chosen go where these were)
+#pragma unroll
+    for (int q = 0; q < SLOTS; q++) {
+        const int j = sub + q * L;
+        if (j >= p.k || !here) break;
+        p.experts[row * p.k + j] = bad ? j : e[q];
+        p.weights[row * p.k + j] = bad ? NAN : e[q] < 0 ? 0.0f : x[q] * by;
     }
+  }
 }
 
 // The gradient of the logits.  With p_j = s_j over the sum of the chosen s and G = sum_j g_j p_j:
@@ -326,11 +413,14 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
 #pragma unroll
     for (int i = 0; i < PER; i++) s[i] = 0;
     if (all) {
-        if (PER == 8 && p.eights) {
-            float x[8];
-            if (n > 0) load8(z + first, x);
+        if (p.eights) {
 #pragma unroll
-            for (int i = 0; i < PER; i++) s[i] = n > 0 ? x[i & 7] : NONE;
+            for (int i = 0; i < PER; i += 8) {
+                float y[8];
+                if (n > i) load8(z + first + i, y);
+#pragma unroll
+                for (int j = 0; j < 8; j++) s[i + j] = n > i ? y[j] : NONE;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < PER; i++) s[i] = i < n ? to_float(z[first + i]) : NONE;
@@ -363,11 +453,14 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
     total = sum_of<L>(total), mean = sum_of<L>(mean);
     if (p.renormalise) mean = total > 0.0f || isnan(total) ? mean / total : 0.0f;
     const float rest = all ? -mean * inverse * p.scale : 0.0f;          // what an expert that is not chosen gets, over e^(z - m)
-    if (PER == 8 && p.eights) {
-        float y[8];
+    if (p.eights) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) y[i] = s[i & (PER - 1)] * rest;
-        if (n > 0) store8(dz + first, y);
+        for (int i = 0; i < PER; i += 8) {
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) y[j] = s[i + j] * rest;
+            if (n > i) store8(dz + first + i, y);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < PER; i++)

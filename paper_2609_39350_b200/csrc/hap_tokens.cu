@@ -26,46 +26,50 @@ static bool routing_fits(const hap_routing *r)
            r->groups <= MOST_EXPERT_GROUPS && r->E % r->groups == 0 && r->kept_groups >= 1 && r->kept_groups <= r->groups && r->group_best >= 1;
 }
 
-// A row's lanes: as few as hold it with eight experts each, so that short rows share a warp.
+// A row's lanes: as few as hold it with eight experts each, so that short rows share a warp; 16 each from 16 lanes on.
 struct RouteLayout { int L, PER; bool fits; };
-static RouteLayout route_layout(int E, int groups, int &per, int &lanes)
+static RouteLayout route_layout(int size, int groups, int &per, int &lanes_log)
 {
     int slots = 1;
     while (slots < groups) slots *= 2;
-    const int size = E / groups;
-    for (int L = slots; L <= 32; L *= 2) {
-        lanes = L / slots, per = (size + lanes - 1) / lanes;
+    lanes_log = 0;
+    for (int L = slots; L <= 16; L *= 2, lanes_log++) {
+        per = (size + (1 << lanes_log) - 1) >> lanes_log;
         if (per <= 8) return {L, 8, true};
+        if (L == 16 && per <= 16) return {L, 16, true};
     }
-    lanes = 32 / slots, per = (size + lanes - 1) / lanes;
+    if (slots == 32) lanes_log = 0;
+    per = (size + (1 << lanes_log) - 1) >> lanes_log;
     return {32, per <= 16 ? 16 : 32, per <= 32};
 }
 
 template <typename T, int L, int PER> static hap_status launch_route(const RouteArgs &p, bool backward, cudaStream_t s)
 {
-    const int64_t blocks = ceil_div(p.rows, ROUTE_WARPS * (32 / L));
+    int64_t blocks = ceil_div(p.rows, ROUTE_WARPS * (32 / L));
     if (!grid_fits(blocks)) return HAP_E_RANGE;
     if (backward) return launch_next(route_backward_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, 0, 1, s, p);
-    return launch_next(route_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, ROUTE_WARPS * (p.E + 32 / L * p.k) * 8, 1, s, p);
+    if (blocks > 148 * ROUTE_BLOCKS) blocks = 148 * ROUTE_BLOCKS;       // (as many as run at once: warps go from row to row)
+    return launch_next(route_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, ROUTE_WARPS * (p.E + 32 / L * (p.k + 2)) * 8, 1, s, p);
 }
 
 static hap_status run_route(RouteArgs p, int32_t dtype, bool backward, cudaStream_t s)
 {
     const int groups = backward ? 1 : p.groups;
-    const RouteLayout at = route_layout(p.E, groups, p.per, p.lanes);
+    p.size = p.E / groups;
+    const RouteLayout at = route_layout(p.size, groups, p.per, p.lanes_log);
     p.slow = !backward && (!at.fits || (p.groups > 1 && p.best > 2));
     const bool dense = !p.sigmoid && !p.renormalise;        // (else the backward pass does not read whole rows)
-    if (at.PER == 8 && p.E / groups % 8 == 0 && (backward && !dense ? true : wide(p.z, p.ld, dtype)) && (!backward || wide(p.dz, p.ldd, dtype)) && aligned(p.bias, 16)) p.per = 8, p.eights = 1;
+    if (p.size % 8 == 0 && (backward && !dense ? true : wide(p.z, p.ld, dtype)) && (!backward || wide(p.dz, p.ldd, dtype)) && aligned(p.bias, 16)) p.per = (p.per + 7) / 8 * 8, p.eights = 1;
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        switch (at.PER == 8 ? at.L : at.PER + 32) {
-        case 1: return launch_route<T, 1, 8>(p, backward, s);
-        case 2: return launch_route<T, 2, 8>(p, backward, s);
-        case 4: return launch_route<T, 4, 8>(p, backward, s);
-        case 8: return launch_route<T, 8, 8>(p, backward, s);
-        case 16: return launch_route<T, 16, 8>(p, backward, s);
-        case 32: return launch_route<T, 32, 8>(p, backward, s);
-        case 48: return launch_route<T, 32, 16>(p, backward, s);
+        switch (at.L + at.PER) {
+        case 1 + 8: return launch_route<T, 1, 8>(p, backward, s);
+        case 2 + 8: return launch_route<T, 2, 8>(p, backward, s);
+        case 4 + 8: return launch_route<T, 4, 8>(p, backward, s);
+        case 8 + 8: return launch_route<T, 8, 8>(p, backward, s);
+        case 16 + 8: return launch_route<T, 16, 8>(p, backward, s);
+        case 16 + 16: return launch_route<T, 16, 16>(p, backward, s);
+        case 32 + 16: return launch_route<T, 32, 16>(p, backward, s);
         default: return launch_route<T, 32, 32>(p, backward, s);
         }
     });
@@ -370,7 +374,7 @@ extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t
             const int threads = norm_threads(H, few && H <= 8192 ? 1 : NORM_EIGHTS), high = norm_high(threads);
             const int64_t blocks = ceil_div(rows, high);
             if (few && H <= 8192) return wd ? launch_norm<norm_kernel<T, P, 1, false, true, C>>(p, blocks, threads, high, 0, s) : launch_norm<norm_kernel<T, P, 1, false, false, C>>(p, blocks, threads, high, 0, s);
-            const int64_t row_bytes = 2 * norm_bytes(H, 1, dtype), most = ceil_div(norm_rows_at_once(H, row_bytes, 1280), high), grid = blocks < most ? blocks : most;
+            const int64_t row_bytes = 2 * norm_bytes(H, 1, dtype), most = ceil_div(norm_rows_at_once(H, row_bytes, 1024), high), grid = blocks < most ? blocks : most;
             return wd ? launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, true, C>>(p, grid, threads, high, high * row_bytes, s)
                       : launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, false, C>>(p, grid, threads, high, high * row_bytes, s);
         };
