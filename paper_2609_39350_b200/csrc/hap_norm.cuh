@@ -77,6 +77,16 @@ template <bool WIDE, typename T> __device__ __forceinline__ Eight brought(const 
         return {{pair(x[0], x[1]), pair(x[2], x[3]), pair(x[4], x[5]), pair(x[6], x[7])}};
     }
 }
+// A thread's columns of w in shared memory, or `none` of each: read by itself alone, without a condition
+template <bool WIDE, typename P> __device__ __forceinline__ void keep_columns(P *to, const void *w, int all, int t, int n, int H, float none)
+{
+    for (int r = 0; r < all; r += 8 * n)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int c = column<WIDE>(r, t, n, j);
+            to[c] = w && c < H ? ((const P *)w)[c] : from_float<P>(none);
+        }
+}
 // A thread's columns of w, or `none` of each.  Behind the row's end they are those of column 0, where they meet what is 0 or is not written.
 template <bool WIDE, typename P> __device__ __forceinline__ Eight weights_of(const void *w, int from, int t, int n, int H, float none)
 {
@@ -95,7 +105,7 @@ template <bool WIDE, typename P> __device__ __forceinline__ Eight weights_of(con
 // memory is never idle between the two sums and the write; without it for few rows, whose latency counts.
 template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(1024) norm_kernel(const NormArgs p)
 {
-    extern __shared__ __align__(16) char ring[];            // [blockDim.y][2][8 EIGHTS threads]
+    extern __shared__ __align__(16) char ring[];            // w, b; [blockDim.y][2][8 EIGHTS threads]
     __shared__ __align__(16) float space[2][2][32];
     const int threads = blockDim.x, t = threadIdx.x, all = 8 * EIGHTS * threads;
     launch_next();
@@ -105,7 +115,10 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
     wait_for_last();
     int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const int64_t step = (int64_t)gridDim.x * blockDim.y;
-    T *stage = (T *)ring + threadIdx.y * 2 * all;
+    P *w_kept = (P *)ring, *b_kept = w_kept + blockDim.y * all;
+    T *stage = (T *)(RING ? (void *)(b_kept + blockDim.y * all) : ring) + threadIdx.y * 2 * all;
+    w_kept += threadIdx.y * all, b_kept += threadIdx.y * all;
+    if (RING) keep_columns<WIDE>(w_kept, p.w, all, t, threads, p.H, 1.0f), keep_columns<WIDE>(b_kept, p.b, all, t, threads, p.H, 0.0f);
     Rows<T, EIGHTS, WIDE> x(p.x, p.ldx, row, step, t);
     auto inside = [&](int r, int i) { return column<WIDE>(8 * r * threads, t, threads, WIDE ? 0 : i) < p.H; };
     if (RING && row < p.rows) x.bring(stage, t, threads, p.H);
@@ -138,7 +151,7 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
             for (int i = 0; i < 4; i++) {
                 if (CENTRED) {
                     v[r].v[i] = v[r].v[i] + pair(-mean);
-                    if (WIDE ? !inside(r, 0) : !inside(r, 2 * i + 1)) {     // behind the row's end the differences are 0 too
+                    if (p.H != all && (WIDE ? !inside(r, 0) : !inside(r, 2 * i + 1))) {    // behind the row's end the differences are 0 too
                         const float2 f = both(v[r].v[i]);
                         v[r].v[i] = pair(!WIDE && inside(r, 2 * i) ? f.x : 0.0f, 0.0f);
                     }
@@ -154,7 +167,8 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
         }
 #pragma unroll
         for (int r = 0; r < EIGHTS; r++) {
-            const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f), b = weights_of<WIDE, P>(p.b, 8 * r * threads, t, threads, p.H, 0.0f);
+            const Eight w = RING ? brought<WIDE>(w_kept, 8 * r * threads, t, threads) : weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f);
+            const Eight b = RING ? brought<WIDE>(b_kept, 8 * r * threads, t, threads) : weights_of<WIDE, P>(p.b, 8 * r * threads, t, threads, p.H, 0.0f);
 #pragma unroll
             for (int i = 0; i < 4; i++) v[r].v[i] = fma2(v[r].v[i] * pair(rstd), w.v[i], b.v[i]);
             store_columns<WIDE>((T *)p.y + row * p.ldy, 8 * r * threads, t, threads, p.H, v[r]);
@@ -166,21 +180,26 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
 // db in registers, in 32 bits.  What has arrived is read twice, for the sums and for dx.
 template <typename T, typename P, int EIGHTS, int MOST, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(MOST) norm_backward_kernel(const NormArgs p)
 {
-    extern __shared__ __align__(16) char ring[];            // [blockDim.y][1 + ahead][x, dy, base][8 EIGHTS threads]
+    extern __shared__ __align__(16) char ring[];            // w; [blockDim.y][1 + ahead][x, dy, base where it fits][8 EIGHTS threads]
     __shared__ __align__(16) float space[2][2][32];
-    const int threads = blockDim.x, t = threadIdx.x, all = 8 * EIGHTS * threads, three = p.base ? 3 : 2;
+    const int threads = blockDim.x, t = threadIdx.x, all = 8 * EIGHTS * threads;
+    constexpr int three = MOST < 1024 ? 3 : 2;              // (long rows leave no shared memory for base)
     launch_next();
     if (threadIdx.y == 0)
         for (int i = t; i < 128; i += threads) (&space[0][0][0])[i] = 0;
     __syncthreads();
     wait_for_last();
     const int64_t first = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, step = (int64_t)gridDim.x * blockDim.y;
-    T *stage = (T *)ring + threadIdx.y * (1 + p.ahead) * three * all;
+    P *w_kept = (P *)ring + threadIdx.y * all;
+    T *stage = (T *)((P *)ring + blockDim.y * all) + threadIdx.y * (1 + p.ahead) * three * all;
+    keep_columns<WIDE>(w_kept, p.w, all, t, threads, p.H, 1.0f);
+    if (three == 3 && !p.base)
+        for (int s = 0; s <= p.ahead; s++) keep_columns<WIDE>(stage + (s * three + 2) * all, nullptr, all, t, threads, 0, 0.0f);
     Rows<T, EIGHTS, WIDE> rx(p.x, p.ldx, first, step, t), rdy(p.dy, p.lddy, first, step, t), rbase(p.base, p.ldbase, first, step, t);
     auto bring = [&](int turn) {
         T *to = stage + (turn & p.ahead) * three * all;
         rx.bring(to, t, threads, p.H), rdy.bring(to + all, t, threads, p.H);
-        if (p.base) rbase.bring(to + 2 * all, t, threads, p.H);
+        if (three == 3 && p.base) rbase.bring(to + 2 * all, t, threads, p.H);
     };
     Eight dw[EIGHTS], db[EIGHTS];
 #pragma unroll
@@ -209,7 +228,7 @@ template <typename T, typename P, int EIGHTS, int MOST, bool WIDE, bool CENTRED>
 #pragma unroll
         for (int r = 0; r < EIGHTS; r++) {
             const Eight x = brought<WIDE>(here, 8 * r * threads, t, threads), g = brought<WIDE>(here + all, 8 * r * threads, t, threads);
-            const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f);
+            const Eight w = brought<WIDE>(w_kept, 8 * r * threads, t, threads);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const Pair xh = (CENTRED ? x.v[i] + shift : x.v[i]) * scale, gw = g.v[i] * w.v[i];       // (behind the row's end dy is 0)
@@ -228,8 +247,9 @@ template <typename T, typename P, int EIGHTS, int MOST, bool WIDE, bool CENTRED>
 #pragma unroll
             for (int r = 0; r < EIGHTS; r++) {
                 const Eight x = brought<WIDE>(here, 8 * r * threads, t, threads), g = brought<WIDE>(here + all, 8 * r * threads, t, threads);
-                const Eight w = weights_of<WIDE, P>(p.w, 8 * r * threads, t, threads, p.H, 1.0f);
-                Eight d = p.base ? brought<WIDE>(here + 2 * all, 8 * r * threads, t, threads) : eight_of(0.0f);
+                const Eight w = brought<WIDE>(w_kept, 8 * r * threads, t, threads);
+                Eight d = three == 3 ? brought<WIDE>(here + 2 * all, 8 * r * threads, t, threads)
+                        : p.base ? load_columns<WIDE>((const T *)p.base + row * p.ldbase, 8 * r * threads, t, threads, p.H) : eight_of(0.0f);
 #pragma unroll
                 for (int i = 0; i < 4; i++) d.v[i] = fma2(fma2(g.v[i], w.v[i], CENTRED ? fma2(x.v[i] + shift, by_x, rest) : x.v[i] * by_x), scale, d.v[i]);
                 store_columns<WIDE>((T *)p.dx + row * p.lddx, 8 * r * threads, t, threads, p.H, d);

@@ -18,6 +18,7 @@ struct RouteArgs {
     int E, k, sigmoid, groups, kept, best, renormalise;
     float scale;
     int size, per, lanes_log;       // experts of a group; of a row's lanes, 2^lanes_log hold a group, `per` experts each
+    int room;                       // doubles of a warp's own: a row's values, or its lanes' keys in order
     int slow, eights;               // all rows the slow way; logits (and their gradients) are read (written) in eights
     int *experts;                   // [rows][k]
     float *weights;
@@ -164,6 +165,41 @@ template <typename T> __device__ __noinline__ void route_settle(const RouteArgs 
     __syncwarp();
 }
 
+// Whether this lane's group is kept, by sums of up to two values in 64 bits: for rows whose groups 32 bits cannot tell apart.  The lanes of
+// a row hold its groups as in route_kernel, n experts from `first` on for each.
+template <typename T, int L> __device__ __noinline__ bool route_groups(const RouteArgs &p, int64_t row, int first, int n, int group)
+{
+    const T *z = (const T *)p.z + row * p.ld;
+    double m = 0, sum = 1;
+    if (!p.sigmoid) {
+        float top = NONE;
+        for (int i = 0; i < n; i++) top = fmaxf(top, to_float(z[first + i]));
+        top = most_of<L>(top);
+        m = top > NONE ? top : 0.0f, sum = 0;
+#pragma unroll 4
+        for (int i = 0; i < n; i++) sum += exp((double)to_float(z[first + i]) - m);
+        for (int d = L / 2; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    }
+    double a = -INFINITY, b = -INFINITY;
+#pragma unroll 4
+    for (int i = 0; i < n; i++) {
+        const double x = to_float(z[first + i]), add = p.bias ? p.bias[first + i] : 0.0;
+        const double v = x == -INFINITY || add == -INFINITY ? -INFINITY : (p.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - m) / sum) + add;
+        b = fmax(b, fmin(a, v)), a = fmax(a, v);
+    }
+    for (int d = (1 << p.lanes_log) / 2; d; d /= 2) {
+        const double c = __shfl_xor_sync(~0u, a, d), e = __shfl_xor_sync(~0u, b, d);
+        b = fmax(fmin(a, c), fmax(b, e)), a = fmax(a, c);
+    }
+    const double total = p.best > 1 && b > -INFINITY ? a + b : a;
+    int ahead = 0;
+    for (int g = 0; g < p.groups; g++) {
+        const double other = __shfl_sync(~0u, total, g << p.lanes_log, L);
+        ahead += other > total || (other == total && g < group);
+    }
+    return ahead < p.kept && total > -INFINITY;
+}
+
 // The larger of two, a NaN where one is
 __device__ __forceinline__ float most_or_nan(float x, float y) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y)); return r; }
 
@@ -189,11 +225,11 @@ template <int LO, int N, int ALL> __device__ __forceinline__ void in_order(uint3
 // k of a row is one maximum over the lanes and a shift in one of them each (600 instructions for a row of 256 with a bias and groups).
 template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROUTE_WARPS, PER == 32 ? 4 : ROUTE_BLOCKS) route_kernel(const RouteArgs p)
 {
-    extern __shared__ double space[];                       // E for each warp, then for each row the chosen and their keys, two more
+    extern __shared__ double space[];                       // `room` for each warp, then for each row the chosen and their keys, two more
     constexpr int ROWS = 32 / L;
     constexpr uint32_t PLACES = PER - 1, LEAST = 0x007fffff;     // (-inf's)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & (L - 1);
-    int *ce = (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + lane / L) * 2 * (p.k + 2);
+    int *ce = (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + lane / L) * 2 * (p.k + 2);
     uint32_t *keys = (uint32_t *)(ce + p.k + 2);
     const unsigned mine = lanes_of<L>(lane);
     const int lanes = 1 << p.lanes_log, group = sub >> p.lanes_log, from = (sub & (lanes - 1)) * p.per, first = group * p.size + from;
@@ -288,11 +324,12 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
                 const float other = __shfl_sync(~0u, total, g << p.lanes_log, L);
                 ahead += other > total || (other == total && g < group);
             }
-            const bool kept = ahead < p.kept && any;
+            bool kept = ahead < p.kept && any;
             if (p.bias || sums) {
                 const uint32_t low = ~most_of<L>(kept ? ~ordered(total) : 0u), high = most_of<L>(!kept && any ? ordered(total) : 0u);
                 const float x = from_ordered(low), y = from_ordered(high);
-                again |= high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
+                const bool near = !bad && high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
+                if (__any_sync(~0u, near)) kept = route_groups<T, L>(p, here ? row : 0, first, n, group);
             }
             if (!kept)
 #pragma unroll
@@ -305,14 +342,17 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
         in_order<0, PER>(key);
         const bool check = p.bias || sizeof(T) == 4;        // (logits in 16 bits lose nothing with their last bits)
         const int rounds = check ? p.k + 2 : p.k;
-        for (int j = 0; j < rounds; j++) {
-            const uint32_t head = key[0] & ~PLACES, top = most_of<L>(head);
-            const unsigned who = __ballot_sync(~0u, head == top) & mine;           // (the first lane of several)
-            if (lane == __ffs(who) - 1) {
-                ce[j] = top > LEAST ? first + (int)(PLACES - (key[0] & PLACES)) : -1, keys[j] = top;
+        uint32_t *rest = (uint32_t *)(space + warp * p.room) + lane, head = key[0];           // (the others wait in shared memory)
 #pragma unroll
-                for (int i = 0; i + 1 < PER; i++) key[i] = key[i + 1];
-                key[PER - 1] = 0;
+        for (int i = 1; i < PER; i++) rest[32 * i] = key[i];
+        rest[32 * PER] = 0;
+        int taken = 0;
+        for (int j = 0; j < rounds; j++) {
+            const uint32_t value = head & ~PLACES, top = most_of<L>(value);
+            const unsigned who = __ballot_sync(~0u, value == top) & mine;          // (the first lane of several)
+            if (lane == __ffs(who) - 1) {
+                ce[j] = top > LEAST ? first + (int)(PLACES - (head & PLACES)) : -1, keys[j] = top;
+                taken += taken < PER, head = rest[32 * taken];
             }
         }
         __syncwarp();
@@ -330,7 +370,7 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
         again = (__ballot_sync(~0u, again) & mine) != 0;
         for (unsigned left = __ballot_sync(~0u, sub == 0 && here && near && !again && !bad); left; left &= left - 1) {
             const int who = __ffs(left) - 1;
-            route_settle<T>(p, __shfl_sync(~0u, row, who), (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + who / L) * 2 * (p.k + 2));
+            route_settle<T>(p, __shfl_sync(~0u, row, who), (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
         }
     }
     unsigned slow = __ballot_sync(~0u, sub == 0 && here && again && !bad);
@@ -338,7 +378,7 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
         const int who = __ffs(slow) - 1;
         slow &= slow - 1;
         __syncwarp();
-        const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.E, (int *)(space + ROUTE_WARPS * p.E) + (warp * ROWS + who / L) * 2 * (p.k + 2));
+        const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.room, (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
         if (lane / L == who / L) m = r.m, sum = r.sum, bad = r.bad;
     }
     __syncwarp();

@@ -379,9 +379,10 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
         int j = 0;
         if (sizeof(T) == 2)
             for (; j + 8 <= n; j += 8) add(j, Count<8>());
+        if (sizeof(T) == 2 && n - j >= 6) add(j, Count<6>()), j += 6;
         for (; j + 4 <= n; j += 4) add(j, Count<4>());
-        if (n & 2) add(j, Count<2>()), j += 2;
-        if (n & 1) add(j, Count<1>());
+        if (n - j >= 2) add(j, Count<2>()), j += 2;
+        if (n - j) add(j, Count<1>());
         store_columns<WIDE>((T *)p.out + r.row * p.ldo, c, lane, 32, r.to, sum);
     }
 }
@@ -462,9 +463,10 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
     int j = 0;
     if (sizeof(T) == 2)
         for (; j + 8 <= n; j += 8) some(j, Count<8>());
+    if (sizeof(T) == 2 && n - j >= 6) some(j, Count<6>()), j += 6;
     for (; j + 4 <= n; j += 4) some(j, Count<4>());
-    if (n & 2) some(j, Count<2>()), j += 2;
-    if (n & 1) some(j, Count<1>());
+    if (n - j >= 2) some(j, Count<2>()), j += 2;
+    if (n - j) some(j, Count<1>());
     if (!p.dweights) return;
     __syncthreads();
     if (threadIdx.x < n) {
@@ -478,7 +480,7 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
 struct EmbeddingArgs {
     int64_t n, first;
     int64_t ldw, ldx, ldo;
-    int H, piece, V, chunk, accumulate, sums, columns;      // sums: blocks that sum, in front of those that clear; columns: blocks of a chunk
+    int H, piece, V, accumulate, sums, columns;             // sums: blocks that sum, others clear; columns: eights of threads in a row
     float scale;
     const int64_t *tokens;
     const void *w, *x;              // x: the gradient dy
@@ -508,27 +510,31 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embeddin
     }
 }
 
-// The gradient.  The first blocks sum dy over the tokens of a row of w: each takes a chunk of the sorted list and an eight of columns
+// The gradient.  The first blocks sum dy over the tokens of a row of w: they take chunks of the sorted list and an eight of columns
 // for every thread, four rows of dy (and of what they are added to) on their way at once.  A row whose tokens are of one chunk is
-// finished here; sums of a part of a row go to `parts` and are joined in order.  The blocks behind them write the rows that no token
-// has, which is most of the bytes where nothing is added to.
+// finished here; sums of a part of a row go to `parts` and are joined in order.  The blocks behind them write the rows that no
+// token has, which is most of the bytes where nothing is added to (beside the sums they took a tenth longer); where something is, there are none.
 constexpr int EMBEDDING_CHUNK = 32;
 template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_gradient_kernel(const EmbeddingArgs p)
 {
     __shared__ uint2 list[EMBEDDING_CHUNK + 2];             // the token in front of the chunk's, the chunk's, the one behind
     launch_next();
     wait_for_last();
+    const int t = threadIdx.x, n = blockDim.x;
     if (blockIdx.x >= p.sums) {
         const Eight zero = eight_of(0.0f);
-        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        for (int64_t v = (int64_t)(blockIdx.x - p.sums) * warps + (threadIdx.x >> 5); v < p.V; v += (int64_t)(gridDim.x - p.sums) * warps) {
+        const int lane = t & 31, warps = n >> 5;
+        for (int64_t v = (int64_t)(blockIdx.x - p.sums) * warps + (t >> 5); v < p.V; v += (int64_t)(gridDim.x - p.sums) * warps) {
             if (p.present[v >> 5] >> (v & 31) & 1) continue;
             for (int c = 0; c < p.H; c += 256) store_columns<WIDE>((O *)p.out + v * p.ldo, c, lane, 32, p.H, zero);
         }
         return;
     }
-    const int chunk = blockIdx.x / p.columns, t = threadIdx.x, n = blockDim.x, c = blockIdx.x % p.columns * n * 8;
+    const int64_t tasks = (p.n + EMBEDDING_CHUNK - 1) / EMBEDDING_CHUNK * p.columns;
+  for (int64_t task = blockIdx.x; task < tasks; task += p.sums) {
+    const int chunk = (int)(task / p.columns), c = (int)(task % p.columns) * n * 8;
     const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK;
+    __syncthreads();
     if (t < EMBEDDING_CHUNK) {
         const uint2 none = make_uint2(p.V, 0);
         list[t + 1] = from + t < p.n ? p.sorted[from + t] : none;
@@ -536,10 +542,10 @@ template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(2
         if (t == 1) list[EMBEDDING_CHUNK + 1] = from + EMBEDDING_CHUNK < p.n ? p.sorted[from + EMBEDDING_CHUNK] : none;
     }
     __syncthreads();
-    if (WIDE && c + 8 * t >= p.H) return;
     const uint2 *s = list + 1;
     const unsigned V = p.V;
-    if (s[0].x >= V) return;
+    if (s[0].x >= V) return;                                // (tokens of no row are behind all others)
+    if (WIDE && c + 8 * t >= p.H) continue;
     float *part = p.parts + (int64_t)chunk * 2 * p.H;
     Eight sum = eight_of(0.0f);
     bool first = list[0].x == s[0].x;                       // the row began in front of this chunk
@@ -569,6 +575,7 @@ template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(2
             if (last) first = false, sum = eight_of(0.0f);
         }
     }
+  }
 }
 
 // Rows that begin in one chunk and end in another: their parts, in order

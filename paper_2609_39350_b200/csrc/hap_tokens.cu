@@ -48,8 +48,10 @@ template <typename T, int L, int PER> static hap_status launch_route(const Route
     int64_t blocks = ceil_div(p.rows, ROUTE_WARPS * (32 / L));
     if (!grid_fits(blocks)) return HAP_E_RANGE;
     if (backward) return launch_next(route_backward_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, 0, 1, s, p);
+    RouteArgs a = p;
+    a.room = p.E > 16 * (PER + 1) ? p.E : 16 * (PER + 1);   // (a lane's keys and a 0 behind them)
     if (blocks > 148 * ROUTE_BLOCKS) blocks = 148 * ROUTE_BLOCKS;       // (as many as run at once: warps go from row to row)
-    return launch_next(route_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, ROUTE_WARPS * (p.E + 32 / L * (p.k + 2)) * 8, 1, s, p);
+    return launch_next(route_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, ROUTE_WARPS * (a.room + 32 / L * (p.k + 2)) * 8, 1, s, a);
 }
 
 static hap_status run_route(RouteArgs p, int32_t dtype, bool backward, cudaStream_t s)
@@ -291,14 +293,16 @@ extern "C" hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, i
     p.sorted = o.to, p.parts = (float *)(space + at.parts), p.present = o.present;
     const bool w = H % 8 == 0 && wide(dy, lddy, dtype) && wide(dw, lddw, out_dtype);
     const int threads = (int)(ceil_div(H, 8) < 256 ? ceil_div(ceil_div(H, 8), 32) * 32 : 256);
-    const int64_t chunks = ceil_div(n, EMBEDDING_CHUNK), columns = ceil_div(H, 8 * threads), rows = ceil_div(V, threads / 32);
-    if (!grid_fits(chunks * columns + 148 * 8)) return HAP_E_RANGE;
-    p.columns = (int)columns, p.sums = (int)(chunks * columns);
-    const int64_t clear = accumulate ? 0 : rows < 148 * 8 ? rows : 148 * 8;
+    const int64_t chunks = ceil_div(n, EMBEDDING_CHUNK), columns = ceil_div(H, 8 * threads), tasks = chunks * columns;
+    if (!grid_fits(tasks)) return HAP_E_RANGE;
+    // blocks that sum: as many as run at once; behind them those that clear
+    const int64_t most = 148 * 3, rows = ceil_div(V, threads / 32), clear = accumulate ? 0 : rows < 148 * 8 ? rows : 148 * 8;
+    p.columns = (int)columns, p.sums = (int)(tasks < most ? tasks : most);
+    const int64_t grid = p.sums + clear;
     auto all = [&](auto t, auto u) {
         using T = decltype(t);
         using O = decltype(u);
-        const hap_status st = launch_next(w ? embedding_gradient_kernel<T, O, true> : embedding_gradient_kernel<T, O, false>, p.sums + clear, threads, 0, 1, s, p);
+        const hap_status st = launch_next(w ? embedding_gradient_kernel<T, O, true> : embedding_gradient_kernel<T, O, false>, grid, threads, 0, 1, s, p);
         if (st != HAP_OK || chunks < 2) return st;
         return launch_next(w ? embedding_join_kernel<O, true> : embedding_join_kernel<O, false>, (chunks - 1) * columns, threads, 0, 1, s, p);
     };
@@ -374,7 +378,12 @@ extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t
             const int threads = norm_threads(H, few && H <= 8192 ? 1 : NORM_EIGHTS), high = norm_high(threads);
             const int64_t blocks = ceil_div(rows, high);
             if (few && H <= 8192) return wd ? launch_norm<norm_kernel<T, P, 1, false, true, C>>(p, blocks, threads, high, 0, s) : launch_norm<norm_kernel<T, P, 1, false, false, C>>(p, blocks, threads, high, 0, s);
-            const int64_t row_bytes = 2 * norm_bytes(H, 1, dtype), most = ceil_div(norm_rows_at_once(H, row_bytes, 1024), high), grid = blocks < most ? blocks : most;
+            const int64_t row_bytes = 2 * norm_bytes(H, 1, dtype) + norm_bytes(H, 2, param_dtype);
+            if (high * row_bytes > 220 << 10) {             // (long rows in 32 bits: each a block of its own)
+                if constexpr (sizeof(T) == 4) return wd ? launch_norm<norm_kernel<T, P, NORM_EIGHTS, false, true, C>>(p, blocks, threads, high, 0, s) : launch_norm<norm_kernel<T, P, NORM_EIGHTS, false, false, C>>(p, blocks, threads, high, 0, s);
+                return HAP_E_INVALID;
+            }
+            const int64_t most = ceil_div(norm_rows_at_once(H, row_bytes, 1024), high), grid = blocks < most ? blocks : most;
             return wd ? launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, true, C>>(p, grid, threads, high, high * row_bytes, s)
                       : launch_norm<norm_kernel<T, P, NORM_EIGHTS, true, false, C>>(p, grid, threads, high, high * row_bytes, s);
         };
@@ -410,14 +419,14 @@ extern "C" hap_status hap_layer_norm_backward(int32_t dtype, int32_t param_dtype
     p.dx = dx, p.lddx = lddx, p.dw = dw, p.db = db, p.mean = (float *)mean, p.rstd = (float *)rstd, p.parts = sums ? (float *)workspace : nullptr;
     cudaStream_t s = (cudaStream_t)stream;
     const bool wd = H % 8 == 0 && wide(x, ldx, dtype) && wide(dy, lddy, dtype) && (!base || wide(base, ldbase, dtype)) && (!dx || wide(dx, lddx, dtype)) && aligned(w, 16);
-    const int64_t one = norm_bytes(H, base ? 3 : 2, dtype);
-    p.ahead = 2 * one <= 224 << 10;                         // (rows of more than 9500 values in 32 bits fill the shared memory alone)
-    const int64_t row_bytes = (1 + p.ahead) * one;
+    const int threads = norm_threads(H, NORM_EIGHTS), high = norm_high(threads);
+    const int64_t one = norm_bytes(H, threads <= 640 ? 3 : 2, dtype), kept = norm_bytes(H, 1, param_dtype);
+    p.ahead = 2 * one + kept <= 220 << 10;                  // (long rows in 32 bits fill the shared memory alone)
+    const int64_t row_bytes = (1 + p.ahead) * one + kept;
     p.blocks = (int)norm_parts(rows, H, row_bytes);
     auto run = [&](auto t, auto u) {
         using T = decltype(t);
         using P = decltype(u);
-        const int threads = norm_threads(H, NORM_EIGHTS), high = norm_high(threads);
         auto pick = [&](auto centre, auto most) {
             constexpr bool C = decltype(centre)::value;
             constexpr int M = decltype(most)::value;

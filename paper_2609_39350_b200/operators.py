@@ -83,6 +83,12 @@ def _here(name, t, here, dtypes, dims):
 
 def _matrix(name, t, here, dtypes, rows=None, cols=None):
     """(address, distance of two rows) of a matrix."""
+    try:                                            # what is usual, asked for in as few steps as there are; the rest below
+        (r, c), (ld, one) = t.shape, t.stride()
+        if t.get_device() == here and t.dtype in dtypes and one == 1 and r > 1 and ld >= c and (rows is None or r == rows) and (cols is None or c == cols):
+            return t.data_ptr(), ld
+    except (AttributeError, TypeError, ValueError):
+        pass
     _here(name, t, here, dtypes, 2)
     (r, c), (ld, one) = t.shape, t.stride()
     if (rows is not None and r != rows) or (cols is not None and c != cols):
@@ -112,6 +118,12 @@ def _matrices(name, t, here, dtypes, batch, rows=None, cols=None):
 
 
 def _vector(name, t, here, dtype, n=None):
+    try:
+        (m,), (one,) = t.shape, t.stride()
+        if t.get_device() == here and t.dtype == dtype and one == 1 and (n is None or m == n):
+            return t.data_ptr()
+    except (AttributeError, TypeError, ValueError):
+        pass
     _here(name, t, here, (dtype,), 1)
     if n is not None and t.numel() != n:
         _refuse(f"{name}: {t.numel()} elements where {n} are needed")

@@ -54,6 +54,12 @@ def _lib():
 
 def _table(name, t, here, dtype, rows=None, cols=None):
     """Address of a table [rows][cols] whose rows follow one another."""
+    try:
+        r, c = t.shape
+        if t.get_device() == here and t.dtype == dtype and (rows is None or r == rows) and (cols is None or c == cols) and t.is_contiguous():
+            return t.data_ptr()
+    except (AttributeError, TypeError, ValueError):
+        pass
     _here(name, t, here, (dtype,), 2)
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
         _refuse(f"{name}: shape {tuple(t.shape)} where {(rows, cols)} is needed")
