@@ -536,7 +536,7 @@ hap_status hap_expert_order_workspace(int64_t rows, int32_t k, int32_t E, uint64
 hap_status hap_expert_order(int64_t rows, int32_t k, int32_t first, int32_t E, const int32_t *dev_experts, int64_t *dev_offsets,
                             int32_t *dev_places, void *dev_workspace, uint64_t bytes, void *stream);
 /* out[places[i][j]] = x[i] for the places in 0 .. placed - 1 (out [placed][H]); other rows of out are left as they are.  A place that
- * is there twice gets one of its rows.  Its gradient is hap_expert_combine without weights. */
+ * is there twice gets values of either row.  Its gradient is hap_expert_combine without weights. */
 hap_status hap_expert_dispatch(int32_t dtype, int64_t rows, int32_t k, int32_t H, int64_t placed, const void *dev_x, int64_t ldx,
                                const int32_t *dev_places, void *dev_out, int64_t ldo, void *stream);
 /* out[i] = base[i] + sum_j weights[i][j] y[places[i][j]] over the places in 0 .. placed - 1 (y [placed][H]), in the order of j, rounded
@@ -589,7 +589,7 @@ hap_status hap_layer_norm_backward(int32_t dtype, int32_t param_dtype, int32_t g
  *             with an equal share of k b S rows, over that rank's time; at most 1
  *   gamma     what that rank's time grows by when its rows are doubled (rho = 2), 0 .. 1
  *   copt      ns per parameter of an AdamW step, bf16 parameters and gradients with 32-bit states
- * Attention, embedding, router and links are not measured.  The runs of an entry are of the same operands, each waited for:
+ * Attention and links are not measured (embedding, norms and router: hap_measure_tokens).  The runs of an entry are of the same operands, each waited for:
  * what fits stays in L2, a short block's time holds its launches, and the clock is that of single runs (under lasting load
  * the products are 15 to 25 % slower, by the power limit).  Runs on `stream` and waits for it; refuses a stream that is being
  * captured with HAP_E_STATE.  Workspace: hap_measure_workspace bytes of 256-byte aligned device memory, the largest of what is
@@ -598,6 +598,18 @@ typedef struct { double *tff, *tfb, *tpost; double eta, gamma, copt; } hap_measu
 hap_status hap_measure_workspace(const hap_model *, const hap_profile *, uint64_t *host_bytes);
 hap_status hap_measure_profile(const hap_model *, const hap_profile *, hap_measured *host_out, void *dev_workspace, uint64_t bytes,
                                void *stream);
+
+/* Times of the operators on a token's way, as further profile entries of a device type; measured and refused as above.
+ *   tpre    [ntp][ncp][nmb]: embedding lookup and its gradient, b S / CP tokens spread over all V words, V / TP rows of them here
+ *   tnorm   [ntp][ncp][nmb][2]: a layer norm of b S / CP tokens, forward and backward (part of tdf and tdb; 0 above H = 16384)
+ *   croute  ns per token and hidden element of a layer of experts beside their products, on a device that has all of them: the
+ *           router's logits and choice (softmax, top k, renormalised), the rows' order, dispatch and combine, and all of it backwards;
+ *           a third of both, since the cost model charges the backward pass as twice the forward.  On the most tokens of the
+ *           lists, up to 8192.  0 without experts, or with more than hap_route takes. */
+typedef struct { double *tpre, *tnorm; double croute; } hap_measured_tokens;
+hap_status hap_measure_tokens_workspace(const hap_model *, const hap_profile *, uint64_t *host_bytes);
+hap_status hap_measure_tokens(const hap_model *, const hap_profile *, hap_measured_tokens *host_out, void *dev_workspace, uint64_t bytes,
+                              void *stream);
 
 /* Waits inside the operators' kernels are bounded; one that runs out ends its kernel early and sets a bit in a device word.
  * Waits for the current device, returns that word in *host_bits (0: none, results are whole) and clears it. */

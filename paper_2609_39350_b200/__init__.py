@@ -17,4 +17,5 @@ from .operators import (EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT, H
                         hap_measure_workspace, hap_measure_profile)
 from .tokens import (SOFTMAX, SIGMOID, HapRouting, hap_routing, hap_route, hap_route_backward, hap_expert_order_workspace, hap_expert_order,  # noqa: F401,E402
                      hap_expert_dispatch, hap_expert_combine, hap_expert_combine_backward, hap_embedding, hap_embedding_backward_workspace,
-                     hap_embedding_backward, hap_layer_norm, hap_layer_norm_backward_workspace, hap_layer_norm_backward)
+                     hap_embedding_backward, hap_layer_norm, hap_layer_norm_backward_workspace, hap_layer_norm_backward, hap_measure_tokens_workspace,
+                     hap_measure_tokens)

@@ -26,7 +26,7 @@ EXPORTS = ["hap_problem_create", "hap_problem_destroy", "hap_enumerate", "hap_ge
            "hap_measure_workspace", "hap_measure_profile",
            "hap_route", "hap_route_backward", "hap_expert_order_workspace", "hap_expert_order", "hap_expert_dispatch", "hap_expert_combine",
            "hap_expert_combine_backward", "hap_embedding", "hap_embedding_backward_workspace", "hap_embedding_backward", "hap_layer_norm",
-           "hap_layer_norm_backward_workspace", "hap_layer_norm_backward"]
+           "hap_layer_norm_backward_workspace", "hap_layer_norm_backward", "hap_measure_tokens_workspace", "hap_measure_tokens"]
 
 
 class HapError(RuntimeError):

@@ -167,6 +167,109 @@ struct Update {
     }
 };
 
+struct Embedding {
+    int64_t rows, V, words;
+    int H;
+    uint64_t bytes = 0;
+    int64_t *tokens;
+    __nv_bfloat16 *w, *out, *dy, *dw;
+    void *space;
+    Embedding(Space &s, int64_t rows, int H, int64_t V, int64_t words) : rows(rows), V(V), words(words), H(H)
+    {
+        hap_embedding_backward_workspace(rows, H, V, &bytes);
+        tokens = s.take<int64_t>(rows), w = s.take<__nv_bfloat16>((uint64_t)V * H), out = s.take<__nv_bfloat16>((uint64_t)rows * H);
+        dy = s.take<__nv_bfloat16>((uint64_t)rows * H), dw = s.take<__nv_bfloat16>((uint64_t)V * H), space = s.take<char>(bytes);
+    }
+    void fill(cudaStream_t st)
+    {
+        fill_targets_kernel<<<64, 256, 0, st>>>(tokens, rows, words);
+        fill_kernel<<<1024, 256, 0, st>>>(w, (uint64_t)V * H, 0.02f, 9);
+        fill_kernel<<<1024, 256, 0, st>>>(dy, (uint64_t)rows * H, 1.0f, 10);
+    }
+    hap_status run(void *st)
+    {
+        const hap_status s = hap_embedding(HAP_BF16, rows, H, V, 0, tokens, w, H, 1.0f, out, H, st);
+        return s != HAP_OK ? s : hap_embedding_backward(HAP_BF16, HAP_BF16, 0, rows, H, V, 0, tokens, dy, H, 1.0f, dw, H, space, bytes, st);
+    }
+};
+
+struct Norm {
+    int64_t rows;
+    int H;
+    uint64_t bytes = 0;
+    __nv_bfloat16 *x, *w, *b, *y, *dy, *dx, *dw, *db;
+    float *mean, *rstd;
+    void *space;
+    Norm(Space &s, int64_t rows, int H) : rows(rows), H(H)
+    {
+        hap_layer_norm_backward_workspace(rows, H, &bytes);
+        const uint64_t n = (uint64_t)rows * H;
+        x = s.take<__nv_bfloat16>(n), y = s.take<__nv_bfloat16>(n), dy = s.take<__nv_bfloat16>(n), dx = s.take<__nv_bfloat16>(n);
+        w = s.take<__nv_bfloat16>(H), b = s.take<__nv_bfloat16>(H), dw = s.take<__nv_bfloat16>(H), db = s.take<__nv_bfloat16>(H);
+        mean = s.take<float>(rows), rstd = s.take<float>(rows), space = s.take<char>(bytes);
+    }
+    void fill(cudaStream_t st)
+    {
+        fill_kernel<<<1024, 256, 0, st>>>(x, (uint64_t)rows * H, 1.0f, 11);
+        fill_kernel<<<1024, 256, 0, st>>>(dy, (uint64_t)rows * H, 1.0f, 12);
+        fill_kernel<<<16, 256, 0, st>>>(w, H, 1.0f, 13);
+        fill_kernel<<<16, 256, 0, st>>>(b, H, 0.1f, 14);
+    }
+    hap_status forward(void *st) { return hap_layer_norm(HAP_BF16, HAP_BF16, 1, rows, H, x, H, w, b, 1e-5f, y, H, mean, rstd, st); }
+    hap_status backward(void *st)
+    {
+        return hap_layer_norm_backward(HAP_BF16, HAP_BF16, HAP_BF16, 0, 1, rows, H, dy, H, x, H, w, mean, rstd, nullptr, 0, dx, H, dw, db, space, bytes, st);
+    }
+};
+
+// What a layer of experts does beside their products, on a device that has all of them: the router's logits and choice, the rows' way
+// to the experts and back, and all of it backwards.
+struct Router {
+    int64_t rows;
+    int H, E, k, ld;
+    uint64_t bytes = 0;
+    hap_routing how;
+    __nv_bfloat16 *x, *w, *z, *dz, *there, *back, *y, *dx, *dw;
+    int32_t *experts, *places;
+    int64_t *offsets, *all;
+    float *weights, *dweights;
+    void *space;
+    Router(Space &s, int64_t rows, int H, int E, int k) : rows(rows), H(H), E(E), k(k), ld((E + 7) / 8 * 8), how{E, k, HAP_SOFTMAX, 1, 1, 1, 1, 1.0f}
+    {
+        hap_expert_order_workspace(rows, k, E, &bytes);
+        const uint64_t n = (uint64_t)rows * H, c = (uint64_t)rows * k;
+        x = s.take<__nv_bfloat16>(n), w = s.take<__nv_bfloat16>((uint64_t)E * H), z = s.take<__nv_bfloat16>((uint64_t)rows * ld), dz = s.take<__nv_bfloat16>((uint64_t)rows * ld);
+        there = s.take<__nv_bfloat16>(c * H), back = s.take<__nv_bfloat16>(c * H), y = s.take<__nv_bfloat16>(n), dx = s.take<__nv_bfloat16>(n), dw = s.take<__nv_bfloat16>((uint64_t)E * H);
+        experts = s.take<int32_t>(c), places = s.take<int32_t>(c), offsets = s.take<int64_t>(E + 1), all = s.take<int64_t>(2);
+        weights = s.take<float>(c), dweights = s.take<float>(c), space = s.take<char>(bytes);
+    }
+    void fill(cudaStream_t st)
+    {
+        fill_offsets_kernel<<<1, 32, 0, st>>>(all, 1, rows);
+        fill_kernel<<<1024, 256, 0, st>>>(x, (uint64_t)rows * H, 1.0f, 15);
+        fill_kernel<<<1024, 256, 0, st>>>(w, (uint64_t)E * H, 1.0f / sqrtf((float)H), 16);
+        fill_kernel<<<1024, 256, 0, st>>>(y, (uint64_t)rows * H, 1.0f, 17);
+    }
+    hap_status forward(void *st)
+    {
+        hap_status s = hap_expert_matmul(HAP_EXPERT_FORWARD, HAP_BF16, HAP_BF16, 0, 1, rows, E, H, all, x, H, w, H, z, ld, st);
+        if (s == HAP_OK) s = hap_route(&how, HAP_BF16, rows, z, ld, nullptr, experts, weights, st);
+        if (s == HAP_OK) s = hap_expert_order(rows, k, 0, E, experts, offsets, places, space, bytes, st);
+        if (s == HAP_OK) s = hap_expert_dispatch(HAP_BF16, rows, k, H, rows * k, x, H, places, there, H, st);
+        if (s == HAP_OK) s = hap_expert_combine(HAP_BF16, rows, k, H, rows * k, there, H, places, weights, x, H, y, H, st);
+        return s;
+    }
+    hap_status backward(void *st)
+    {
+        hap_status s = hap_expert_combine_backward(HAP_BF16, rows, k, H, rows * k, y, H, there, H, places, weights, back, H, dweights, st);
+        if (s == HAP_OK) s = hap_expert_combine(HAP_BF16, rows, k, H, rows * k, back, H, places, nullptr, y, H, dx, H, st);
+        if (s == HAP_OK) s = hap_route_backward(&how, HAP_BF16, rows, z, ld, experts, dweights, dz, ld, st);
+        if (s == HAP_OK) s = hap_expert_matmul(HAP_EXPERT_GRAD_INPUT, HAP_BF16, HAP_BF16, 1, 1, rows, E, H, all, dz, ld, w, H, dx, H, st);
+        if (s == HAP_OK) s = hap_expert_matmul(HAP_EXPERT_GRAD_WEIGHT, HAP_BF16, HAP_BF16, 0, 1, rows, E, H, all, dz, ld, x, H, dw, H, st);
+        return s;
+    }
+};
+
 bool list_fits(const int32_t *l, int n)
 {
     if (n < 1 || n > HAP_MAX_LIST || !l) return false;
@@ -205,6 +308,19 @@ Share rank_share(const hap_model &m, int64_t toks)
     const int e = m.E < RANK_EXPERTS ? m.E : RANK_EXPERTS;
     const int64_t rows = toks * m.k * e / m.E;
     return {e, rows < e ? e : rows};
+}
+
+constexpr int64_t ROUTED_TOKENS = 8192;     // of the router's measurement, at most: its time is proportional to them
+bool has_router(const hap_model &m) { return m.E > 0 && m.E <= 1024 && m.k > 0 && m.k <= 32; }
+bool has_norm(const hap_model &m) { return m.H <= 16384; }
+int64_t routed_tokens(const hap_model &m, const hap_profile &p) { const int64_t t = most_tokens(m, p); return t < ROUTED_TOKENS ? t : ROUTED_TOKENS; }
+
+// A stream that may be measured on
+hap_status not_captured(cudaStream_t s)
+{
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (status_of(cudaStreamIsCapturing(s, &capture)) != HAP_OK) return HAP_E_CUDA;
+    return capture == cudaStreamCaptureStatusNone ? HAP_OK : HAP_E_STATE;
 }
 
 } // namespace
@@ -246,9 +362,8 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
     if (st != HAP_OK) return st;
     if (!out || !out->tff || !out->tfb || !out->tpost || !workspace || bytes < need || ((uintptr_t)workspace & 255)) return HAP_E_INVALID;
     cudaStream_t s = (cudaStream_t)stream;
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    if (status_of(cudaStreamIsCapturing(s, &capture)) != HAP_OK) return HAP_E_CUDA;
-    if (capture != cudaStreamCaptureStatusNone) return HAP_E_STATE;
+    const hap_status free_stream = not_captured(s);
+    if (free_stream != HAP_OK) return free_stream;
     Timer timer(s);
     if (!timer.good) return HAP_E_CUDA;
     // the same sizes come up under several degrees (tokens b S / CP): each is measured once
@@ -324,5 +439,85 @@ extern "C" hap_status hap_measure_profile(const hap_model *m, const hap_profile 
         }
     }
     free(heads), free(blocks);
+    return bad;
+}
+
+extern "C" hap_status hap_measure_tokens_workspace(const hap_model *m, const hap_profile *p, uint64_t *host_bytes)
+{
+    if (!host_bytes || !fits(m, p)) return HAP_E_INVALID;
+    if (most_tokens(*m, *p) >= (1ll << 29)) return HAP_E_RANGE;
+    uint64_t need = 0;
+    auto count = [&](auto &&make) {
+        Space s{nullptr};
+        make(s);
+        need = s.at > need ? s.at : need;
+    };
+    each_entry(*m, *p, [&](int, int64_t t, int64_t tp) {
+        count([&](Space &s) { Embedding(s, t, m->H, shard(m->V, tp), m->V); });
+        if (has_norm(*m)) count([&](Space &s) { Norm(s, t, m->H); });
+    });
+    if (has_router(*m)) count([&](Space &s) { Router(s, routed_tokens(*m, *p), m->H, m->E, m->k); });
+    *host_bytes = need;
+    return HAP_OK;
+}
+
+extern "C" hap_status hap_measure_tokens(const hap_model *m, const hap_profile *p, hap_measured_tokens *out, void *workspace, uint64_t bytes, void *stream)
+{
+    uint64_t need = 0;
+    hap_status bad = hap_measure_tokens_workspace(m, p, &need);
+    if (bad != HAP_OK) return bad;
+    if (!out || !out->tpre || !out->tnorm || !workspace || bytes < need || ((uintptr_t)workspace & 255)) return HAP_E_INVALID;
+    cudaStream_t s = (cudaStream_t)stream;
+    if ((bad = not_captured(s)) != HAP_OK) return bad;
+    Timer timer(s);
+    if (!timer.good) return HAP_E_CUDA;
+    // entry 0 of a table is made whatever was before it: sizes that came up are looked for among the entries that are done
+    auto before = [&](int at, int64_t t, int64_t V) {
+        int found = -1;
+        each_entry(*m, *p, [&](int i, int64_t t2, int64_t tp2) {
+            if (i < at && found < 0 && t2 == t && (V < 0 || shard(m->V, tp2) == V)) found = i;
+        });
+        return found;
+    };
+    each_entry(*m, *p, [&](int at, int64_t t, int64_t tp) {
+        if (bad != HAP_OK) return;
+        const int64_t V = shard(m->V, tp);
+        int was = before(at, t, V);
+        if (was >= 0) out->tpre[at] = out->tpre[was];
+        else {
+            Space sp{(char *)workspace, bytes};
+            Embedding e(sp, t, m->H, V, m->V);
+            if (!sp.fits()) { bad = HAP_E_INVALID; return; }
+            e.fill(s);
+            out->tpre[at] = timer.time([&] { return e.run(stream); });
+            if ((bad = timer.status) != HAP_OK) return;
+        }
+        was = before(at, t, -1);
+        double *norm = out->tnorm + 2 * at;
+        if (!has_norm(*m)) norm[0] = norm[1] = 0;
+        else if (was >= 0) norm[0] = out->tnorm[2 * was], norm[1] = out->tnorm[2 * was + 1];
+        else {
+            Space sp{(char *)workspace, bytes};
+            Norm n(sp, t, m->H);
+            if (!sp.fits()) { bad = HAP_E_INVALID; return; }
+            n.fill(s);
+            norm[0] = timer.time([&] { return n.forward(stream); });
+            if ((bad = timer.status) == HAP_OK) norm[1] = timer.time([&] { return n.backward(stream); });
+            if (bad == HAP_OK) bad = timer.status;
+        }
+    });
+    out->croute = 0;
+    if (bad == HAP_OK && has_router(*m)) {
+        const int64_t t = routed_tokens(*m, *p);
+        Space sp{(char *)workspace, bytes};
+        Router r(sp, t, m->H, m->E, m->k);
+        if (!sp.fits()) return HAP_E_INVALID;
+        r.fill(s);
+        const double f = timer.time([&] { return r.forward(stream); });
+        if ((bad = timer.status) != HAP_OK) return bad;
+        const double b = timer.time([&] { return r.backward(stream); });
+        if ((bad = timer.status) != HAP_OK) return bad;
+        out->croute = (f + b) / (3.0 * (double)t * (double)m->H);
+    }
     return bad;
 }

@@ -42,10 +42,12 @@ template <int L> __device__ __forceinline__ float sum_of(float x)
 }
 template <int L> __device__ __forceinline__ uint32_t most_of(uint32_t x)
 {
-    if (L == 32) return __reduce_max_sync(~0u, x);
+    if constexpr (L == 32) return __reduce_max_sync(~0u, x);
+    else {
 #pragma unroll
-    for (int d = L / 2; d; d /= 2) x = max(x, __shfl_xor_sync(~0u, x, d));
-    return x;
+        for (int d = L / 2; d; d /= 2) x = max(x, __shfl_xor_sync(~0u, x, d));
+        return x;
+    }
 }
 // A number's bits so that they order as numbers do (-0 as 0), above 0; and back
 __device__ __forceinline__ uint32_t ordered(float x)

@@ -76,7 +76,7 @@ template <bool WIDE, typename T> __device__ __forceinline__ void store_columns(T
 // registers, their ranks among the warp's equal ones come from matching lanes, and one number for every warp and key says how many
 // lie in the warps ahead.  Several blocks count their chunks first (order_count_kernel; a pass that places also counts for the next
 // one), and each adds up what lies in front of its own.  A list of one tile needs the placing kernel alone.
-constexpr int ORDER_WARPS = 16, ORDER_ITEMS = 4, ORDER_TILE = 32 * ORDER_WARPS * ORDER_ITEMS, MOST_KEYS = 1024, MOST_PASSES = 3;
+constexpr int ORDER_WARPS = 16, ORDER_ITEMS = 4, ORDER_TILE = 32 * ORDER_WARPS * ORDER_ITEMS, MOST_KEYS = 1024;
 
 struct OrderArgs {
     int64_t n;

@@ -12,8 +12,10 @@ One layer, forwards:
 """
 from __future__ import annotations
 
+import copy
 import ctypes as C
 
+import numpy as np
 import torch
 
 from . import operators
@@ -328,3 +330,39 @@ def hap_layer_norm_backward(dy, x, w, rstd, mean=None, base=None, dx=None, dw=No
     _check(_lib().hap_layer_norm_backward(_TYPES[x.dtype], _TYPES[kind], _TYPES[grads], bool(accumulate), mean is not None, rows, H, pd, ldd, px, ldx, pw, pm, pr, pb, ldb, pdx, lddx,
                                           *at, ps, n or 0, stream), "hap_layer_norm_backward")
     return dx, dw, db
+
+
+class _MeasuredTokens(C.Structure):
+    _fields_ = [("tpre", C.c_void_p), ("tnorm", C.c_void_p), ("croute", C.c_double)]
+
+
+def hap_measure_tokens_workspace(pb) -> int:
+    """Bytes of device memory that hap_measure_tokens needs for a problem."""
+    model, profile, keep = operators._measured_parts(pb)
+    n = C.c_uint64()
+    _check(_lib().hap_measure_tokens_workspace(model, profile, C.byref(n)), "hap_measure_tokens_workspace")
+    return int(n.value)
+
+
+@_on_stream
+def hap_measure_tokens(pb, device_type, workspace=None):
+    """Times embedding, norms and router on the current device and returns (problem, measured): a copy of the problem whose tpre and
+    croute of one device type are these times, and what was measured as a dict; the norms' times (tnorm, forward and backward) are a
+    part of tdf and tdb, which are not changed."""
+    T = int(pb.P.shape[0])
+    if not 0 <= device_type < T:
+        _refuse(f"device_type: {device_type} of {T}")
+    if workspace is None:
+        workspace = torch.empty(hap_measure_tokens_workspace(pb), dtype=torch.uint8, device="cuda")
+    here, stream = _now()
+    ps = _vector("workspace", workspace, here, torch.uint8)
+    n = tuple(len(x) for x in (pb.tp_list, pb.cp_list, pb.mb_list))
+    tpre, tnorm = np.zeros(n), np.zeros((*n, 2))
+    out = _MeasuredTokens(tpre.ctypes.data, tnorm.ctypes.data)
+    model, profile, keep = operators._measured_parts(pb)
+    _check(_lib().hap_measure_tokens(model, profile, C.byref(out), C.c_void_p(ps), C.c_uint64(workspace.numel()), C.c_void_p(stream)), "hap_measure_tokens")
+    new = copy.copy(pb)
+    for name in ("tpre", "croute"):
+        setattr(new, name, np.array(getattr(pb, name), dtype=np.float64))
+    new.tpre[device_type], new.croute[device_type] = tpre, out.croute
+    return new, dict(tpre=tpre, tnorm=tnorm, croute=out.croute)

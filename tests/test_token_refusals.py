@@ -49,7 +49,7 @@ def test_order_refuses():
         assert L.hap_expert_order_workspace(rows, k, E, C.byref(n)) == 0
         return n.value
 
-    assert space(0, 1, 1) == 0 and space(512, 8, 64) == 0 and 0 < space(32768, 8, 256) < 1 << 20
+    assert space(0, 1, 1) == 0 and space(256, 8, 64) == 0 and 0 < space(32768, 8, 256) < 1 << 20
     for bad in ((-1, 1, 1), (1, 0, 1), (1, 33, 1), (1, 1, 0), (1, 1, 1025), (1 << 30, 2, 1)):
         assert L.hap_expert_order_workspace(*bad, C.byref(n)) == INVALID, bad
     assert L.hap_expert_order_workspace(1, 1, 1, None) == INVALID
