@@ -283,9 +283,17 @@ template <typename U, bool WIDE> __global__ void __launch_bounds__(256) dispatch
     const U *x = (const U *)p.x + r.row * p.ldx;
     if (WIDE) {
         constexpr int N = 16 / sizeof(U);
-        for (int c = r.from + lane * N; c < r.to; c += 32 * N) {
-            const uint4 v = *(const uint4 *)(x + c);
-            for (unsigned left = there; left; left &= left - 1) *(uint4 *)((U *)p.out + (int64_t)places[__ffs(left) - 1] * p.ldo + c) = v;
+        for (int c = r.from + lane * N; c < r.to; c += 4 * 32 * N) {
+            uint4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (c + u * 32 * N < r.to) v[u] = *(const uint4 *)(x + c + u * 32 * N);
+            for (unsigned left = there; left; left &= left - 1) {
+                U *out = (U *)p.out + (int64_t)places[__ffs(left) - 1] * p.ldo + c;
+#pragma unroll
+                for (int u = 0; u < 4; u++)
+                    if (c + u * 32 * N < r.to) *(uint4 *)(out + u * 32 * N) = v[u];
+            }
         }
     } else {
         for (int c = r.from + lane; c < r.to; c += 32) {
@@ -502,12 +510,27 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embeddin
     const bool there = t >= p.first && v >= 0 && v < p.V;
     T *out = (T *)p.out + row * p.ldo;
     const T *in = (const T *)p.w + (there ? v : 0) * p.ldw;
-    for (int c = from; c < to; c += 256) {
-        Eight x = there ? load_columns<WIDE>(in, c, lane, 32, to) : eight_of(0.0f);
-#pragma unroll
-        for (int i = 0; i < 4; i++) x.v[i] = x.v[i] * pair(p.scale);
-        store_columns<WIDE>(out, c, lane, 32, to, x);
+    if (!there) {
+        for (int c = from; c < to; c += 256) store_columns<WIDE>(out, c, lane, 32, to, eight_of(0.0f));
+        return;
     }
+    auto some = [&](int c, auto count) {
+        constexpr int N = decltype(count)::value;
+        Raw<T, WIDE> x[N];
+#pragma unroll
+        for (int u = 0; u < N; u++) x[u].load(in, c + 256 * u, lane, 32, to);
+#pragma unroll
+        for (int u = 0; u < N; u++) {
+            Eight y = x[u].eight();
+#pragma unroll
+            for (int i = 0; i < 4; i++) y.v[i] = y.v[i] * pair(p.scale);
+            store_columns<WIDE>(out, c + 256 * u, lane, 32, to, y);
+        }
+    };
+    int c = from;
+    for (; c + 1024 <= to; c += 1024) some(c, Count<4>());
+    for (; c < to; c += 256)
+        if (!WIDE || c + 8 * lane < to) some(c, Count<1>());
 }
 
 // The gradient.  The first blocks sum dy over the tokens of a row of w: they take chunks of the sorted list and an eight of columns

@@ -85,8 +85,11 @@ def _matrix(name, t, here, dtypes, rows=None, cols=None):
     """(address, distance of two rows) of a matrix."""
     try:                                            # what is usual, asked for in as few steps as there are; the rest below
         (r, c), (ld, one) = t.shape, t.stride()
-        if t.get_device() == here and t.dtype in dtypes and one == 1 and r > 1 and ld >= c and (rows is None or r == rows) and (cols is None or c == cols):
-            return t.data_ptr(), ld
+        if t.get_device() == here and t.dtype in dtypes and one == 1 and r > 0 and (rows is None or r == rows) and (cols is None or c == cols):
+            if r == 1:
+                return t.data_ptr(), (c + 7) & ~7
+            if ld >= c:
+                return t.data_ptr(), ld
     except (AttributeError, TypeError, ValueError):
         pass
     _here(name, t, here, dtypes, 2)
