@@ -80,12 +80,26 @@ template <bool WIDE, typename T> __device__ __forceinline__ Eight brought(const 
 // A thread's columns of w in shared memory, or `none` of each: read by itself alone, without a condition
 template <bool WIDE, typename P> __device__ __forceinline__ void keep_columns(P *to, const void *w, int all, int t, int n, int H, float none)
 {
-    for (int r = 0; r < all; r += 8 * n)
+    const P fill = from_float<P>(none);
+    for (int r = 0; r < all; r += 8 * n) {
+        if (WIDE && w && r + 8 * t < H) {
+#pragma unroll
+            for (int i = 0; i < sizeof(P) / 2; i++) ((uint4 *)(to + r + 8 * t))[i] = ((const uint4 *)((const P *)w + r + 8 * t))[i];
+            continue;
+        }
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const int c = column<WIDE>(r, t, n, j);
-            to[c] = w && c < H ? ((const P *)w)[c] : from_float<P>(none);
+            to[c] = w && c < H ? ((const P *)w)[c] : fill;
         }
+    }
+}
+// 1 / sqrt(x) to a unit in the last place: the approximation and a step of Newton's (a root and a quotient to nearest are six times as
+// many instructions, which every thread of a row has to make)
+__device__ __forceinline__ float inverse_root(float x)
+{
+    const float y = rsqrtf(x), z = y * fmaf(-0.5f * x * y, y, 1.5f);
+    return x > 0.0f && x < INFINITY ? z : y;
 }
 // A thread's columns of w, or `none` of each.  Behind the row's end they are those of column 0, where they meet what is 0 or is not written.
 template <bool WIDE, typename P> __device__ __forceinline__ Eight weights_of(const void *w, int from, int t, int n, int H, float none)
@@ -160,7 +174,7 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
             }
         s[0] = sum_of(squares);
         row_sums(s, threads, &space[1][turn]);
-        const float rstd = 1.0f / sqrtf(fmaf(s[0], p.inverse, p.eps));
+        const float rstd = inverse_root(fmaf(s[0], p.inverse, p.eps));
         if (t == 0) {
             if (CENTRED && p.mean) p.mean[row] = mean;
             if (p.rstd) p.rstd[row] = rstd;
