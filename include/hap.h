@@ -503,7 +503,8 @@ hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *co
 /* ---- A token's way to the experts and back, embedding, norms ---------------------------------------------------------------
  * As the operators above: no handle, device pointers, asynchronous on `stream`, capturable, nothing allocated; and here element
  * types may be HAP_FP32 too.  Rows may be any distance apart (ld >= the row's length, in elements); where addresses and distances
- * are multiples of 16 bytes, memory is read and written in such pieces, otherwise value by value at about half the speed.
+ * are multiples of 16 bytes and rows are whole eights of values, memory is moved in such pieces, otherwise value by value at a
+ * third to nine tenths of the speed.
  *
  * Routing: the k of E experts that a row goes to, from its logits z [rows][E].  Scores s = softmax(z) (HAP_SOFTMAX) or
  * 1 / (1 + exp(-z)) (HAP_SIGMOID); values v = s + bias (fp32 [E], nullable: then experts are in the order of z).  With groups > 1

@@ -75,7 +75,8 @@ template <bool WIDE, typename T> __device__ __forceinline__ void store_columns(T
 // A stable pass of a counting sort.  A block takes a chunk of the list, tile by tile; a warp's entries of a tile are in its lanes'
 // registers, their ranks among the warp's equal ones come from matching lanes, and one number for every warp and key says how many
 // lie in the warps ahead.  Several blocks count their chunks first (order_count_kernel; a pass that places also counts for the next
-// one), and each adds up what lies in front of its own.  A list of one tile needs the placing kernel alone.
+// one), and each adds up what lies in front of its own.  A list of one tile needs the placing kernel alone.  Bound by latency: three
+// rounds of reads and barriers (196602 entries: 4 and 5 us; with a warp's entries read one after the other 6 and 9).
 constexpr int ORDER_WARPS = 16, ORDER_ITEMS = 4, ORDER_TILE = 32 * ORDER_WARPS * ORDER_ITEMS, MOST_KEYS = 1024;
 
 struct OrderArgs {
@@ -267,7 +268,8 @@ __device__ __forceinline__ Piece piece_of(const RowsArgs &p)
     return r;
 }
 
-// out[place] = x[row]: a row is read once and written to its places.  U: values of the size, copied as they are.
+// out[place] = x[row]: a row is read once and written to its places, four pieces at a time.  U: values of the size, copied as they are.
+// Bound by memory: 8192 rows of 5120 to six places each, 105 us, 5.6 TB/s.
 template <typename U, bool WIDE> __global__ void __launch_bounds__(256) dispatch_kernel(const RowsArgs p)
 {
     launch_next();
@@ -342,7 +344,8 @@ template <typename T> struct Raw<T, false> {
 };
 
 // out[row] = base[row] + sum_j weight_j y[place_j].  The rows that are there, with their weights, are listed in shared memory, so that
-// reads are not behind conditions: eight rows are on their way at once.
+// reads are not behind conditions: eight rows are on their way at once.  Bound by memory: 65536 rows of 8192 in 16 bits, weighted, 229 us,
+// 5.9 TB/s (read under conditions, four at a time, 366; a warp's columns 256, 1024, 2048 and 8192 of a row 247, 232, 230 and 267).
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_kernel(const RowsArgs p)
 {
     __shared__ int2 list[8][MOST_CHOSEN];
@@ -396,7 +399,8 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
 }
 
 // dy[place_j] = weight_j dout[row] and dweight_j = <dout[row], y[place_j]>, a block for each row: dout is read once, y once.  Up to
-// eight rows of y are on their way at once; with more than eight dout is read again, from L1.
+// eight rows of y are on their way at once; with more than eight dout is read again, from L1.  Bound by memory: 4001 rows of 5120 with
+// six places each 96 us, 5.6 TB/s.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsArgs p)
 {
     __shared__ float parts[8][MOST_CHOSEN];
@@ -498,6 +502,7 @@ struct EmbeddingArgs {
     const unsigned *present;
 };
 
+// out[i] = scale w[token_i - first]: a warp for a row or a piece of one, four reads on their way (8192 rows of 5120: 35 us; one 45)
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embedding_kernel(const EmbeddingArgs p)
 {
     launch_next();
@@ -536,7 +541,9 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) embeddin
 // The gradient.  The first blocks sum dy over the tokens of a row of w: they take chunks of the sorted list and an eight of columns
 // for every thread, four rows of dy (and of what they are added to) on their way at once.  A row whose tokens are of one chunk is
 // finished here; sums of a part of a row go to `parts` and are joined in order.  The blocks behind them write the rows that no
-// token has, which is most of the bytes where nothing is added to (beside the sums they took a tenth longer); where something is, there are none.
+// token has, which is most of the bytes where nothing is added to; where something is, there are none.  Bound by memory: 16384 tokens
+// into 102400 rows of 5120, 198 us for 168 MB read and 1.05 GB written, which a plain fill takes 270 for (sums and clearing side by
+// side: 250; chunks of 16 and 8 tokens: 5 and 17 us more).
 constexpr int EMBEDDING_CHUNK = 32;
 template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_gradient_kernel(const EmbeddingArgs p)
 {
@@ -601,7 +608,8 @@ template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(2
   }
 }
 
-// Rows that begin in one chunk and end in another: their parts, in order
+// Rows that begin in one chunk and end in another: their parts, in order.  (As many chunks are asked at once for the row's end as there are
+// threads.)
 template <typename O, bool WIDE> __global__ void __launch_bounds__(256) embedding_join_kernel(const EmbeddingArgs p)
 {
     launch_next();
@@ -610,11 +618,8 @@ template <typename O, bool WIDE> __global__ void __launch_bounds__(256) embeddin
     const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK, to = from + EMBEDDING_CHUNK;
     const unsigned v = p.sorted[to].x, inside = p.sorted[to - 1].x, begin = p.sorted[from].x, before = from > 0 ? p.sorted[from - 1].x : p.V;
     if (v >= p.V || inside != v || (begin == v && before == v)) return;
-    int lo = chunk + 1, hi = chunks;                        // the last chunk that begins with the row
-    while (hi - lo > 1) {
-        const int mid = lo + (hi - lo < 4 ? 1 : (hi - lo) / 2);
-        if (p.sorted[(int64_t)mid * EMBEDDING_CHUNK].x == v) lo = mid; else hi = mid;
-    }
+    int lo = chunk;                                         // the last chunk that begins with the row: as many are asked as there are threads
+    for (int some = n; some == n; lo += some) some = __syncthreads_count(lo + 1 + t < chunks && p.sorted[(int64_t)(lo + 1 + t) * EMBEDDING_CHUNK].x == v);
     if (WIDE && c + 8 * t >= p.H) return;
     O *out = (O *)p.out + (int64_t)v * p.ldo;
     const Eight was = p.accumulate ? load_columns<WIDE>((const O *)out, c, t, n, p.H) : eight_of(0.0f);
