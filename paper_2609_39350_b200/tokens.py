@@ -148,6 +148,8 @@ def hap_expert_order(experts, E, first=0, offsets=None, places=None, workspace=N
     here, stream = _now()
     pe = _table("experts", experts, here, torch.int32)
     rows, k = experts.shape
+    if not -(1 << 31) <= first < 1 << 31 or not 1 <= E <= 1024:
+        _refuse(f"first, E: {E} experts from {first} on")
     if offsets is None:
         offsets = torch.empty(E + 1, dtype=torch.int64, device=experts.device)
     if places is None:
@@ -318,6 +320,8 @@ def hap_layer_norm_backward(dy, x, w, rstd, mean=None, base=None, dx=None, dw=No
     pdx, lddx = _matrix("dx", dx, here, same, rows, H) if dx is not None else (None, 0)
     given = dw if dw is not None else db
     grads = given.dtype if given is not None else kind if w is not None else torch.float32
+    if accumulate and want_dw and given is None:
+        _refuse("dw, db: needed where sums are added to them")
     if want_dw and not accumulate:
         dw = torch.empty(H, dtype=grads, device=x.device) if dw is None else dw
         db = torch.empty(H, dtype=grads, device=x.device) if db is None and mean is not None else db

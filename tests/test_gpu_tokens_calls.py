@@ -160,7 +160,8 @@ def test_what_is_refused():
         lambda: hap.hap_embedding_backward(tokens, x[:4], x), lambda: hap.hap_embedding_backward(tokens, x, x, workspace=torch.empty(1, dtype=torch.uint8, device="cuda")),
         lambda: hap.hap_layer_norm(x, w=x[0].half()), lambda: hap.hap_layer_norm(x, w=mean), lambda: hap.hap_layer_norm(x, y=x.float()), lambda: hap.hap_layer_norm(x, eps=-1.0),
         lambda: hap.hap_layer_norm_backward(x, x, None, mean[:4]), lambda: hap.hap_layer_norm_backward(x, x, None, mean, db=torch.zeros(64, device="cuda")),
-        lambda: hap.hap_layer_norm_backward(x, x, x[0], mean, dw=x[0].half()),
+        lambda: hap.hap_layer_norm_backward(x, x, x[0], mean, dw=x[0].half()), lambda: hap.hap_layer_norm_backward(x, x, None, mean, accumulate=True),
+        lambda: hap.hap_expert_order(places, 4, first=1 << 31), lambda: hap.hap_expert_order(places, 1025),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(hap.HapError):
