@@ -252,174 +252,174 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
     const int64_t step = (int64_t)gridDim.x * ROUTE_WARPS * ROWS;
     int64_t row = ((int64_t)blockIdx.x * ROUTE_WARPS + warp) * ROWS + lane / L;
     if (p.eights && !p.slow) bring(row);
-  for (; row - lane / L < p.rows; row += step) {            // (a warp's rows together)
-    const bool here = row < p.rows;
-    float m = 0, sum = 1;
-    bool bad = false, again = p.slow;
-    if (!p.slow) {
-        const int n = here ? own : 0;
-        float z[PER], v[PER];
-        if (p.eights) {
-#pragma unroll
-            for (int i = 0; i < EIGHTS; i++) {
-                const Eight x = next[i].eight();
-#pragma unroll
-                for (int j = 0; j < 8; j++) z[8 * i + j] = n > 8 * i ? (j & 1 ? both(x.v[j / 2]).y : both(x.v[j / 2]).x) : NONE;
-            }
-            bring(row + step);
-        } else {
-            const T *zr = (const T *)p.z + row * p.ld + first;
-#pragma unroll
-            for (int i = 0; i < PER; i++) z[i] = i < n ? to_float(zr[i]) : NONE;
-        }
-        const bool sums = p.groups > 1 && p.best > 1;       // scores are added up
-        float most = z[0];
-#pragma unroll
-        for (int i = 1; i < PER; i++) most = most_or_nan(most, z[i]);
-        bad = isnan(most) || (!p.sigmoid && most == INFINITY);
-        if (!p.sigmoid && (p.bias || sums || !p.renormalise)) {
-            m = most_of<L>(most);
-            if (m == NONE) m = 0;
-            sum = 0;
-#pragma unroll
-            for (int i = 0; i < PER; i++) sum += p.renormalise ? __expf(z[i] - m) : expf(z[i] - m);        // (a weight's, or the choice's alone)
-            sum = sum_of<L>(sum);
-        }
-        // What a score is off by.  Sigmoid: e^-z by 2^-22 + 1.5 |z| 2^-23 of itself, which s (1 - s) takes to 1e-7, two roundings and
-        // the quotient 3e-7.  Softmax: of the largest score, 2^-22 for the term and the sum's up to 37 roundings, 2.5e-6 in all.
-        // `off` is at least what two values differ by wrongly; a sum with the bias has a rounding of its own.
-        const float inverse = sum > 0.0f ? __fdividef(1.0f, sum) : 0.0f, off = p.sigmoid ? 8e-7f : 6e-6f * inverse;
-        auto score = [&](float x) { return p.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-x)) : __expf(x - m) * inverse; };
-        if (p.bias) {
-            float b[PER];
+    for (; row - lane / L < p.rows; row += step) {            // (a warp's rows together)
+        const bool here = row < p.rows;
+        float m = 0, sum = 1;
+        bool bad = false, again = p.slow;
+        if (!p.slow) {
+            const int n = here ? own : 0;
+            float z[PER], v[PER];
             if (p.eights) {
 #pragma unroll
                 for (int i = 0; i < EIGHTS; i++) {
-                    float x[8];
-                    load8(p.bias + (n > 8 * i ? first + 8 * i : 0), x);
+                    const Eight x = next[i].eight();
 #pragma unroll
-                    for (int j = 0; j < 8; j++) b[8 * i + j] = x[j];
+                    for (int j = 0; j < 8; j++) z[8 * i + j] = n > 8 * i ? (j & 1 ? both(x.v[j / 2]).y : both(x.v[j / 2]).x) : NONE;
                 }
+                bring(row + step);
+            } else {
+                const T *zr = (const T *)p.z + row * p.ld + first;
+#pragma unroll
+                for (int i = 0; i < PER; i++) z[i] = i < n ? to_float(zr[i]) : NONE;
+            }
+            const bool sums = p.groups > 1 && p.best > 1;       // scores are added up
+            float most = z[0];
+#pragma unroll
+            for (int i = 1; i < PER; i++) most = most_or_nan(most, z[i]);
+            bad = isnan(most) || (!p.sigmoid && most == INFINITY);
+            if (!p.sigmoid && (p.bias || sums || !p.renormalise)) {
+                m = most_of<L>(most);
+                if (m == NONE) m = 0;
+                sum = 0;
+#pragma unroll
+                for (int i = 0; i < PER; i++) sum += p.renormalise ? __expf(z[i] - m) : expf(z[i] - m);        // (a weight's, or the choice's alone)
+                sum = sum_of<L>(sum);
+            }
+            // What a score is off by.  Sigmoid: e^-z by 2^-22 + 1.5 |z| 2^-23 of itself, which s (1 - s) takes to 1e-7, two roundings and
+            // the quotient 3e-7.  Softmax: of the largest score, 2^-22 for the term and the sum's up to 37 roundings, 2.5e-6 in all.
+            // `off` is at least what two values differ by wrongly; a sum with the bias has a rounding of its own.
+            const float inverse = sum > 0.0f ? __fdividef(1.0f, sum) : 0.0f, off = p.sigmoid ? 8e-7f : 6e-6f * inverse;
+            auto score = [&](float x) { return p.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-x)) : __expf(x - m) * inverse; };
+            if (p.bias) {
+                float b[PER];
+                if (p.eights) {
+#pragma unroll
+                    for (int i = 0; i < EIGHTS; i++) {
+                        float x[8];
+                        load8(p.bias + (n > 8 * i ? first + 8 * i : 0), x);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) b[8 * i + j] = x[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PER; i++) b[i] = i < n ? p.bias[first + i] : 0.0f;
+                }
+                float top = 0;
+#pragma unroll
+                for (int i = 0; i < PER; i++) v[i] = score(z[i]) + b[i], top = most_or_nan(top, v[i]), v[i] = z[i] == NONE ? NONE : v[i];
+                bad |= !(top < INFINITY);                       // (of a bias that is no number, or +inf)
             } else {
 #pragma unroll
-                for (int i = 0; i < PER; i++) b[i] = i < n ? p.bias[first + i] : 0.0f;
+                for (int i = 0; i < PER; i++) v[i] = z[i];
             }
-            float top = 0;
+            bad = (__ballot_sync(~0u, bad && here) & mine) != 0;
+            if (p.groups > 1) {
+                float a = NONE, b = NONE;                       // a group's largest and the next
 #pragma unroll
-            for (int i = 0; i < PER; i++) v[i] = score(z[i]) + b[i], top = most_or_nan(top, v[i]), v[i] = z[i] == NONE ? NONE : v[i];
-            bad |= !(top < INFINITY);                       // (of a bias that is no number, or +inf)
-        } else {
+                for (int i = 0; i < PER; i++) b = fmaxf(b, fminf(a, v[i])), a = fmaxf(a, v[i]);
+                for (int d = lanes / 2; d; d /= 2) {
+                    const float c = __shfl_xor_sync(~0u, a, d), e = __shfl_xor_sync(~0u, b, d);
+                    b = fmaxf(fminf(a, c), fmaxf(b, e)), a = fmaxf(a, c);
+                }
+                const bool any = a > NONE, two = b > NONE;
+                if (sums && !p.bias) a = score(a), b = score(b);
+                const float total = !any ? NONE : sums && two ? a + b : a;
+                int ahead = 0;
+                for (int g = 0; g < p.groups; g++) {
+                    const float other = __shfl_sync(~0u, total, g << p.lanes_log, L);
+                    ahead += other > total || (other == total && g < group);
+                }
+                bool kept = ahead < p.kept && any;
+                if (p.bias || sums) {
+                    const uint32_t low = ~most_of<L>(kept ? ~ordered(total) : 0u), high = most_of<L>(!kept && any ? ordered(total) : 0u);
+                    const float x = from_ordered(low), y = from_ordered(high);
+                    const bool near = !bad && high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
+                    if (__any_sync(~0u, near)) kept = route_groups<T, L>(p, here ? row : 0, first, n, group);
+                }
+                if (!kept)
 #pragma unroll
-            for (int i = 0; i < PER; i++) v[i] = z[i];
+                    for (int i = 0; i < PER; i++) v[i] = NONE;
+            }
+            // A value as a whole number that orders as it does, up to LEAST for none, with its place among the lane's in the last bits
+            uint32_t key[PER];
+#pragma unroll
+            for (int i = 0; i < PER; i++) key[i] = (ordered(v[i]) & ~PLACES) | (PLACES - i);
+            in_order<0, PER>(key);
+            const bool check = p.bias || sizeof(T) == 4;        // (logits in 16 bits lose nothing with their last bits)
+            const int rounds = check ? p.k + 2 : p.k;
+            uint32_t *rest = (uint32_t *)(space + warp * p.room) + lane, head = key[0];           // (the others wait in shared memory)
+#pragma unroll
+            for (int i = 1; i < PER; i++) rest[32 * i] = key[i];
+            rest[32 * PER] = 0;
+            int taken = 0;
+            for (int j = 0; j < rounds; j++) {
+                const uint32_t value = head & ~PLACES, top = most_of<L>(value);
+                const unsigned who = __ballot_sync(~0u, value == top) & mine;          // (the first lane of several)
+                if (lane == __ffs(who) - 1) {
+                    ce[j] = top > LEAST ? first + (int)(PLACES - (head & PLACES)) : -1, keys[j] = top;
+                    taken += taken < PER, head = rest[32 * taken];
+                }
+            }
+            __syncwarp();
+            // Neighbours that may be the other way round: the chosen and the one behind them are settled by themselves; where the one behind
+            // these may be among them too, the whole row is done again.
+            bool near = false, at_end = false, behind = false;
+            for (int j = sub + 1; check && j < rounds; j += L) {
+                if (keys[j] <= LEAST) continue;
+                const float x = from_ordered(keys[j - 1]), y = from_ordered(keys[j]);          // (logits in 32: where what is left is equal)
+                const bool is = p.bias ? x - y <= off + PER * 1.2e-7f * fmaxf(fabsf(x), fabsf(y)) : keys[j - 1] == keys[j];
+                near |= is && j <= p.k, at_end |= is && j == p.k, behind |= is && j == p.k + 1;
+            }
+            near = (__ballot_sync(~0u, near) & mine) != 0, at_end = (__ballot_sync(~0u, at_end) & mine) != 0, behind = (__ballot_sync(~0u, behind) & mine) != 0;
+            again |= (at_end && behind) || (near && p.k == 32);
+            again = (__ballot_sync(~0u, again) & mine) != 0;
+            for (unsigned left = __ballot_sync(~0u, sub == 0 && here && near && !again && !bad); left; left &= left - 1) {
+                const int who = __ffs(left) - 1;
+                route_settle<T>(p, __shfl_sync(~0u, row, who), (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
+            }
         }
-        bad = (__ballot_sync(~0u, bad && here) & mine) != 0;
-        if (p.groups > 1) {
-            float a = NONE, b = NONE;                       // a group's largest and the next
-#pragma unroll
-            for (int i = 0; i < PER; i++) b = fmaxf(b, fminf(a, v[i])), a = fmaxf(a, v[i]);
-            for (int d = lanes / 2; d; d /= 2) {
-                const float c = __shfl_xor_sync(~0u, a, d), e = __shfl_xor_sync(~0u, b, d);
-                b = fmaxf(fminf(a, c), fmaxf(b, e)), a = fmaxf(a, c);
-            }
-            const bool any = a > NONE, two = b > NONE;
-            if (sums && !p.bias) a = score(a), b = score(b);
-            const float total = !any ? NONE : sums && two ? a + b : a;
-            int ahead = 0;
-            for (int g = 0; g < p.groups; g++) {
-                const float other = __shfl_sync(~0u, total, g << p.lanes_log, L);
-                ahead += other > total || (other == total && g < group);
-            }
-            bool kept = ahead < p.kept && any;
-            if (p.bias || sums) {
-                const uint32_t low = ~most_of<L>(kept ? ~ordered(total) : 0u), high = most_of<L>(!kept && any ? ordered(total) : 0u);
-                const float x = from_ordered(low), y = from_ordered(high);
-                const bool near = !bad && high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
-                if (__any_sync(~0u, near)) kept = route_groups<T, L>(p, here ? row : 0, first, n, group);
-            }
-            if (!kept)
-#pragma unroll
-                for (int i = 0; i < PER; i++) v[i] = NONE;
-        }
-        // A value as a whole number that orders as it does, up to LEAST for none, with its place among the lane's in the last bits
-        uint32_t key[PER];
-#pragma unroll
-        for (int i = 0; i < PER; i++) key[i] = (ordered(v[i]) & ~PLACES) | (PLACES - i);
-        in_order<0, PER>(key);
-        const bool check = p.bias || sizeof(T) == 4;        // (logits in 16 bits lose nothing with their last bits)
-        const int rounds = check ? p.k + 2 : p.k;
-        uint32_t *rest = (uint32_t *)(space + warp * p.room) + lane, head = key[0];           // (the others wait in shared memory)
-#pragma unroll
-        for (int i = 1; i < PER; i++) rest[32 * i] = key[i];
-        rest[32 * PER] = 0;
-        int taken = 0;
-        for (int j = 0; j < rounds; j++) {
-            const uint32_t value = head & ~PLACES, top = most_of<L>(value);
-            const unsigned who = __ballot_sync(~0u, value == top) & mine;          // (the first lane of several)
-            if (lane == __ffs(who) - 1) {
-                ce[j] = top > LEAST ? first + (int)(PLACES - (head & PLACES)) : -1, keys[j] = top;
-                taken += taken < PER, head = rest[32 * taken];
-            }
+        unsigned slow = __ballot_sync(~0u, sub == 0 && here && again && !bad);
+        while (slow) {
+            const int who = __ffs(slow) - 1;
+            slow &= slow - 1;
+            __syncwarp();
+            const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.room, (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
+            if (lane / L == who / L) m = r.m, sum = r.sum, bad = r.bad;
         }
         __syncwarp();
-        // Neighbours that may be the other way round: the chosen and the one behind them are settled by themselves; where the one behind
-        // these may be among them too, the whole row is done again.
-        bool near = false, at_end = false, behind = false;
-        for (int j = sub + 1; check && j < rounds; j += L) {
-            if (keys[j] <= LEAST) continue;
-            const float x = from_ordered(keys[j - 1]), y = from_ordered(keys[j]);          // (logits in 32: where what is left is equal)
-            const bool is = p.bias ? x - y <= off + PER * 1.2e-7f * fmaxf(fabsf(x), fabsf(y)) : keys[j - 1] == keys[j];
-            near |= is && j <= p.k, at_end |= is && j == p.k, behind |= is && j == p.k + 1;
+        // the chosen's weights: a lane has number sub, sub + L, ...
+        constexpr int SLOTS = L >= 8 ? 32 / L : 8;              // (k is at most 32 and the lanes' experts, eight each where there are few lanes)
+        const T *z = (const T *)p.z + (here ? row : 0) * p.ld;
+        int e[SLOTS];
+        float x[SLOTS], top = NONE, total = 0;
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++) {
+            e[q] = sub + q * L < p.k ? ce[sub + q * L] : -1;
+            x[q] = e[q] >= 0 && here ? to_float(z[e[q]]) : NONE;
+            top = fmaxf(top, x[q]);
         }
-        near = (__ballot_sync(~0u, near) & mine) != 0, at_end = (__ballot_sync(~0u, at_end) & mine) != 0, behind = (__ballot_sync(~0u, behind) & mine) != 0;
-        again |= (at_end && behind) || (near && p.k == 32);
-        again = (__ballot_sync(~0u, again) & mine) != 0;
-        for (unsigned left = __ballot_sync(~0u, sub == 0 && here && near && !again && !bad); left; left &= left - 1) {
-            const int who = __ffs(left) - 1;
-            route_settle<T>(p, __shfl_sync(~0u, row, who), (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
+        if (p.renormalise) {
+            top = most_of<L>(top);
+            if (top == NONE) top = 0;
+            if (p.sigmoid) top = fminf(top, 0.0f);
+        } else top = p.sigmoid ? 0.0f : m;
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++) {
+            x[q] = e[q] < 0 ? 0.0f : p.sigmoid ? sigmoid_score(x[q], top) : expf(x[q] - top);
+            total += x[q];
+        }
+        if (p.renormalise) total = sum_of<L>(total);
+        else total = p.sigmoid ? 1.0f : sum;
+        const float by = p.scale / total;
+        __syncwarp();                                           // (the next row's chosen go where these were)
+#pragma unroll
+        for (int q = 0; q < SLOTS; q++) {
+            const int j = sub + q * L;
+            if (j >= p.k || !here) break;
+            p.experts[row * p.k + j] = bad ? j : e[q];
+            p.weights[row * p.k + j] = bad ? NAN : e[q] < 0 ? 0.0f : x[q] * by;
         }
     }
-    unsigned slow = __ballot_sync(~0u, sub == 0 && here && again && !bad);
-    while (slow) {
-        const int who = __ffs(slow) - 1;
-        slow &= slow - 1;
-        __syncwarp();
-        const RowStart r = route_slowly<T>(p, __shfl_sync(~0u, row, who), space + warp * p.room, (int *)(space + ROUTE_WARPS * p.room) + (warp * ROWS + who / L) * 2 * (p.k + 2));
-        if (lane / L == who / L) m = r.m, sum = r.sum, bad = r.bad;
-    }
-    __syncwarp();
-    // the chosen's weights: a lane has number sub, sub + L, ...
-    constexpr int SLOTS = L >= 8 ? 32 / L : 8;              // (k is at most 32 and the lanes' experts, eight each where there are few lanes)
-    const T *z = (const T *)p.z + (here ? row : 0) * p.ld;
-    int e[SLOTS];
-    float x[SLOTS], top = NONE, total = 0;
-#pragma unroll
-    for (int q = 0; q < SLOTS; q++) {
-        e[q] = sub + q * L < p.k ? ce[sub + q * L] : -1;
-        x[q] = e[q] >= 0 && here ? to_float(z[e[q]]) : NONE;
-        top = fmaxf(top, x[q]);
-    }
-    if (p.renormalise) {
-        top = most_of<L>(top);
-        if (top == NONE) top = 0;
-        if (p.sigmoid) top = fminf(top, 0.0f);
-    } else top = p.sigmoid ? 0.0f : m;
-#pragma unroll
-    for (int q = 0; q < SLOTS; q++) {
-        x[q] = e[q] < 0 ? 0.0f : p.sigmoid ? sigmoid_score(x[q], top) : expf(x[q] - top);
-        total += x[q];
-    }
-    if (p.renormalise) total = sum_of<L>(total);
-    else total = p.sigmoid ? 1.0f : sum;
-    const float by = p.scale / total;
-    __syncwarp();                                           // (the next row's chosen go where these were)
-#pragma unroll
-    for (int q = 0; q < SLOTS; q++) {
-        const int j = sub + q * L;
-        if (j >= p.k || !here) break;
-        p.experts[row * p.k + j] = bad ? j : e[q];
-        p.weights[row * p.k + j] = bad ? NAN : e[q] < 0 ? 0.0f : x[q] * by;
-    }
-  }
 }
 
 // The gradient of the logits.  With p_j = s_j over the sum of the chosen s and G = sum_j g_j p_j:

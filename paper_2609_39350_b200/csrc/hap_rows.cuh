@@ -561,51 +561,51 @@ template <typename T, typename O, bool WIDE> __global__ void __launch_bounds__(2
         return;
     }
     const int64_t tasks = (p.n + EMBEDDING_CHUNK - 1) / EMBEDDING_CHUNK * p.columns;
-  for (int64_t task = blockIdx.x; task < tasks; task += p.sums) {
-    const int chunk = (int)(task / p.columns), c = (int)(task % p.columns) * n * 8;
-    const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK;
-    __syncthreads();
-    if (t < EMBEDDING_CHUNK) {
-        const uint2 none = make_uint2(p.V, 0);
-        list[t + 1] = from + t < p.n ? p.sorted[from + t] : none;
-        if (t == 0) list[0] = from > 0 ? p.sorted[from - 1] : none;
-        if (t == 1) list[EMBEDDING_CHUNK + 1] = from + EMBEDDING_CHUNK < p.n ? p.sorted[from + EMBEDDING_CHUNK] : none;
-    }
-    __syncthreads();
-    const uint2 *s = list + 1;
-    const unsigned V = p.V;
-    if (s[0].x >= V) return;                                // (tokens of no row are behind all others)
-    if (WIDE && c + 8 * t >= p.H) continue;
-    float *part = p.parts + (int64_t)chunk * 2 * p.H;
-    Eight sum = eight_of(0.0f);
-    bool first = list[0].x == s[0].x;                       // the row began in front of this chunk
-    for (int i = 0; i < EMBEDDING_CHUNK; i += 4) {
-        if (s[i].x >= V) break;
-        Raw<T, WIDE> x[4];
-        Raw<O, WIDE> before[4];
+    for (int64_t task = blockIdx.x; task < tasks; task += p.sums) {
+        const int chunk = (int)(task / p.columns), c = (int)(task % p.columns) * n * 8;
+        const int64_t from = (int64_t)chunk * EMBEDDING_CHUNK;
+        __syncthreads();
+        if (t < EMBEDDING_CHUNK) {
+            const uint2 none = make_uint2(p.V, 0);
+            list[t + 1] = from + t < p.n ? p.sorted[from + t] : none;
+            if (t == 0) list[0] = from > 0 ? p.sorted[from - 1] : none;
+            if (t == 1) list[EMBEDDING_CHUNK + 1] = from + EMBEDDING_CHUNK < p.n ? p.sorted[from + EMBEDDING_CHUNK] : none;
+        }
+        __syncthreads();
+        const uint2 *s = list + 1;
+        const unsigned V = p.V;
+        if (s[0].x >= V) return;                                // (tokens of no row are behind all others)
+        if (WIDE && c + 8 * t >= p.H) continue;
+        float *part = p.parts + (int64_t)chunk * 2 * p.H;
+        Eight sum = eight_of(0.0f);
+        bool first = list[0].x == s[0].x;                       // the row began in front of this chunk
+        for (int i = 0; i < EMBEDDING_CHUNK; i += 4) {
+            if (s[i].x >= V) break;
+            Raw<T, WIDE> x[4];
+            Raw<O, WIDE> before[4];
 #pragma unroll
-        for (int u = 0; u < 4; u++) x[u].load((const T *)p.x + (int64_t)s[i + u].y * p.ldx, c, t, n, p.H);
-        if (p.accumulate)                                   // (of a row's last token; others read row 0, which stays in L1)
+            for (int u = 0; u < 4; u++) x[u].load((const T *)p.x + (int64_t)s[i + u].y * p.ldx, c, t, n, p.H);
+            if (p.accumulate)                                   // (of a row's last token; others read row 0, which stays in L1)
 #pragma unroll
-            for (int u = 0; u < 4; u++) before[u].load((const O *)p.out + (s[i + u].x < V && s[i + u + 1].x != s[i + u].x ? (int64_t)s[i + u].x * p.ldo : 0), c, t, n, p.H);
+                for (int u = 0; u < 4; u++) before[u].load((const O *)p.out + (s[i + u].x < V && s[i + u + 1].x != s[i + u].x ? (int64_t)s[i + u].x * p.ldo : 0), c, t, n, p.H);
 #pragma unroll
-        for (int u = 0; u < 4; u++) {
-            const unsigned v = s[i + u].x;
-            if (v >= V) break;
-            const Eight e = x[u].eight();
+            for (int u = 0; u < 4; u++) {
+                const unsigned v = s[i + u].x;
+                if (v >= V) break;
+                const Eight e = x[u].eight();
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum.v[j] = sum.v[j] + e.v[j];
-            const bool last = s[i + u + 1].x != v, whole = last && !first;
-            if (whole) {
-                Eight y = p.accumulate ? before[u].eight() : eight_of(0.0f);
+                for (int j = 0; j < 4; j++) sum.v[j] = sum.v[j] + e.v[j];
+                const bool last = s[i + u + 1].x != v, whole = last && !first;
+                if (whole) {
+                    Eight y = p.accumulate ? before[u].eight() : eight_of(0.0f);
 #pragma unroll
-                for (int j = 0; j < 4; j++) y.v[j] = fma2(sum.v[j], pair(p.scale), y.v[j]);
-                store_columns<WIDE>((O *)p.out + (int64_t)v * p.ldo, c, t, n, p.H, y);
-            } else if (last || i + u == EMBEDDING_CHUNK - 1) store_columns<WIDE>(part + (first ? 0 : p.H), c, t, n, p.H, sum);
-            if (last) first = false, sum = eight_of(0.0f);
+                    for (int j = 0; j < 4; j++) y.v[j] = fma2(sum.v[j], pair(p.scale), y.v[j]);
+                    store_columns<WIDE>((O *)p.out + (int64_t)v * p.ldo, c, t, n, p.H, y);
+                } else if (last || i + u == EMBEDDING_CHUNK - 1) store_columns<WIDE>(part + (first ? 0 : p.H), c, t, n, p.H, sum);
+                if (last) first = false, sum = eight_of(0.0f);
+            }
         }
     }
-  }
 }
 
 // Rows that begin in one chunk and end in another: their parts, in order.  (As many chunks are asked at once for the row's end as there are
