@@ -84,7 +84,11 @@ template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteA
         for (int e = lane; e < p.E; e += 32) sum += exp((double)to_float(z[e]) - m);
         for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
     }
-    if (bad) return {(float)m, (float)sum, true};
+    if (bad) {                                                      // (the experts of a row without an order: the weights' logits are read by them)
+        if (lane < p.k) ce[lane] = lane;
+        __syncwarp();
+        return {(float)m, (float)sum, true};
+    }
     for (int e = lane; e < p.E; e += 32) {
         const double x = to_float(z[e]), b = p.bias ? p.bias[e] : 0.0;
         const double s = p.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - m) / sum;
