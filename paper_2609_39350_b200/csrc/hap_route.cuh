@@ -5,6 +5,8 @@
 #pragma once
 #include "hap_rows.cuh"
 
+#include <float.h>
+
 namespace hapop {
 
 constexpr int MOST_EXPERT_GROUPS = 32;
@@ -335,9 +337,11 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
                 }
                 bool kept = ahead < p.kept && any;
                 if (p.bias || sums) {
-                    const uint32_t low = ~most_of<L>(kept ? ~ordered(total) : 0u), high = most_of<L>(!kept && any ? ordered(total) : 0u);
-                    const float x = from_ordered(low), y = from_ordered(high);
-                    const bool near = !bad && high && low != ~0u && x - y <= 2 * off + 4e-7f * (fabsf(x) + fabsf(y));
+                    // What a group's value is off by: `off` for its scores; a rounding of each of its values and of their sum, which go with
+                    // the values' sizes where these cancel, and of what stands here.  (Sums beyond the largest number are anything.)
+                    const float error = off + 4e-7f * (sums && two ? fabsf(a) + fabsf(b) : fabsf(a));
+                    const uint32_t low = ~most_of<L>(kept ? ~ordered(fmaxf(total - error, -FLT_MAX)) : 0u), high = most_of<L>(!kept && any ? ordered(fminf(total + error, FLT_MAX)) : 0u);
+                    const bool near = !bad && low <= high;
                     if (__any_sync(~0u, near)) kept = route_groups<T, L>(p, here ? row : 0, first, n, group);
                 }
                 if (!kept)
