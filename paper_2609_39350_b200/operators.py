@@ -73,6 +73,8 @@ def _here(name, t, here, dtypes, dims):
     """Checks what every tensor argument has to be."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name}: must be a CUDA tensor")
+    if t.layout != torch.strided:
+        _refuse(f"{name}: must be a strided tensor")
     if t.get_device() != here:
         _refuse(f"{name}: must live on the current CUDA device")
     if t.dtype not in dtypes:
@@ -90,7 +92,7 @@ def _matrix(name, t, here, dtypes, rows=None, cols=None):
                 return t.data_ptr(), (c + 7) & ~7
             if ld >= c:
                 return t.data_ptr(), ld
-    except (AttributeError, TypeError, ValueError):
+    except (AttributeError, TypeError, ValueError, RuntimeError):
         pass
     _here(name, t, here, dtypes, 2)
     (r, c), (ld, one) = t.shape, t.stride()
@@ -125,7 +127,7 @@ def _vector(name, t, here, dtype, n=None):
         (m,), (one,) = t.shape, t.stride()
         if t.get_device() == here and t.dtype == dtype and one == 1 and (n is None or m == n):
             return t.data_ptr()
-    except (AttributeError, TypeError, ValueError):
+    except (AttributeError, TypeError, ValueError, RuntimeError):
         pass
     _here(name, t, here, (dtype,), 1)
     if n is not None and t.numel() != n:

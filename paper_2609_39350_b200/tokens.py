@@ -60,7 +60,7 @@ def _table(name, t, here, dtype, rows=None, cols=None):
         r, c = t.shape
         if t.get_device() == here and t.dtype == dtype and (rows is None or r == rows) and (cols is None or c == cols) and t.is_contiguous():
             return t.data_ptr()
-    except (AttributeError, TypeError, ValueError):
+    except (AttributeError, TypeError, ValueError, RuntimeError):
         pass
     _here(name, t, here, (dtype,), 2)
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
