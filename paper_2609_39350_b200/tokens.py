@@ -272,7 +272,8 @@ def _params(x, here, H, named):
 @_on_stream
 def hap_layer_norm(x, w=None, b=None, eps=1e-5, centred=True, y=None, mean=None, rstd=None, keep=True):
     """(y, mean, rstd): y = (x - mean) rstd w + b over the rows of x; with centred false without the mean, which is None then.
-    w, b: of x's type or fp32.  mean, rstd: fp32 [rows], for the backward pass (None where keep is false)."""
+    w, b: of x's type or fp32.  mean, rstd: fp32 [rows], for the backward pass (None where keep is false).  A mean that is given with
+    centred false is not written."""
     here, stream = _now()
     px, ldx = _matrix("x", x, here, _FLOATS)
     rows, H = x.shape
@@ -287,7 +288,7 @@ def hap_layer_norm(x, w=None, b=None, eps=1e-5, centred=True, y=None, mean=None,
     pm = _vector("mean", mean, here, torch.float32, rows) if mean is not None else None
     pr = _vector("rstd", rstd, here, torch.float32, rows) if rstd is not None else None
     _check(_lib().hap_layer_norm(_TYPES[x.dtype], _TYPES[kind], bool(centred), rows, H, px, ldx, pw, pb, eps, py, ldy, pm, pr, stream), "hap_layer_norm")
-    return y, mean, rstd
+    return y, mean if centred else None, rstd
 
 
 def _norm_bytes(rows, H):
