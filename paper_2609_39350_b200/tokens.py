@@ -306,7 +306,8 @@ def hap_layer_norm_backward_workspace(x):
 @_on_stream
 def hap_layer_norm_backward(dy, x, w, rstd, mean=None, base=None, dx=None, dw=None, db=None, want_dx=True, want_dw=True, accumulate=False, workspace=None):
     """(dx, dw, db) of hap_layer_norm: centred where a mean is given.  base: added to dx.  dw and db are made, of w's type (fp32 without
-    one), where want_dw is set; given ones are of w's type or fp32, and added to with accumulate.  db is None without a mean."""
+    one), where want_dw is set; given ones are of w's type or fp32.  With accumulate they are added to, and none is made: those that
+    are wanted have to be given (one alone: with want_dw false).  db is None without a mean."""
     here, stream = _now()
     px, ldx = _matrix("x", x, here, _FLOATS)
     rows, H = x.shape
@@ -321,7 +322,7 @@ def hap_layer_norm_backward(dy, x, w, rstd, mean=None, base=None, dx=None, dw=No
     pdx, lddx = _matrix("dx", dx, here, same, rows, H) if dx is not None else (None, 0)
     given = dw if dw is not None else db
     grads = given.dtype if given is not None else kind if w is not None else torch.float32
-    if accumulate and want_dw and given is None:
+    if accumulate and want_dw and (dw is None or (db is None and mean is not None)):
         _refuse("dw, db: needed where sums are added to them")
     if want_dw and not accumulate:
         dw = torch.empty(H, dtype=grads, device=x.device) if dw is None else dw

@@ -17,3 +17,22 @@ def test_a_mean_without_centring_is_none():
     dx, dw, db = hap.hap_layer_norm_backward(y, x, None, rstd, mean=mean)
     assert db is None and torch.equal(dx, hap.hap_layer_norm_backward(y, x, None, rstd)[0])
     assert hap.hap_layer_norm(x, mean=given)[1] is given
+
+
+def test_sums_are_added_to_all_that_is_wanted():
+    """A gradient that is wanted is not left out because no tensor is given for it."""
+    x, dy = normal(40, 264), normal(40, 264, seed=1)
+    _, mean, rstd = hap.hap_layer_norm(x)
+    sums = lambda: torch.zeros(264, device="cuda")  # noqa: E731
+    for given in (dict(dw=sums()), dict(db=sums()), {}):
+        with pytest.raises(hap.HapError):
+            hap.hap_layer_norm_backward(dy, x, None, rstd, mean=mean, accumulate=True, **given)
+    with pytest.raises(hap.HapError):
+        hap.hap_layer_norm_backward(dy, x, None, rstd, accumulate=True)
+    _, dw, db = hap.hap_layer_norm_backward(dy, x, None, rstd, mean=mean)
+    for given in (dict(dw=sums(), db=sums()), dict(dw=sums(), want_dw=False), dict(db=sums(), want_dw=False)):
+        got = hap.hap_layer_norm_backward(dy, x, None, rstd, mean=mean, accumulate=True, **given)
+        for name, i, want in (("dw", 1, dw), ("db", 2, db)):
+            assert got[i] is given.get(name) and (got[i] is None or torch.equal(got[i], want))
+    only = sums()
+    assert torch.equal(hap.hap_layer_norm_backward(dy, x, None, rstd, dw=only, accumulate=True)[1], hap.hap_layer_norm_backward(dy, x, None, rstd)[1])
