@@ -504,7 +504,7 @@ hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *co
  * As the operators above: no handle, device pointers, asynchronous on `stream`, capturable, nothing allocated; and here element
  * types may be HAP_FP32 too.  Rows may be any distance apart (ld >= the row's length, in elements); where addresses and distances
  * are multiples of 16 bytes and rows are whole eights of values, memory is moved in such pieces, otherwise value by value at a
- * third to nine tenths of the speed.
+ * third to nine tenths of the speed.  An output may lie in an input's place only where it says so, with rows the same distance apart.
  *
  * Routing: the k of E experts that a row goes to, from its logits z [rows][E].  Scores s = softmax(z) (HAP_SOFTMAX) or
  * 1 / (1 + exp(-z)) (HAP_SIGMOID); values v = s + bias (fp32 [E], nullable: then experts are in the order of z).  With groups > 1
@@ -568,7 +568,7 @@ hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, int32_t accu
  * pass needs.  Statistics in fp32, the variance from differences to the mean.
  * Backward: dx = base + rstd (g - mean(g) - xh mean(g xh)) with g = dy w, xh = (x - mean) rstd (base nullable: the gradient of the
  * residual stream; with centred = 0 without mean(g)); dw = sum dy xh, db = sum dy over the rows, of grad_dtype (param_dtype or
- * HAP_FP32), added to what they hold with accumulate.  dx, dw, db nullable; dx may be dy or base.  H <= 16384.
+ * HAP_FP32), added to what they hold with accumulate.  dx, dw, db nullable; y may be x, dx may be x, dy or base.  H <= 16384.
  * Workspace: hap_layer_norm_backward_workspace bytes, 256-byte aligned, during the call; needed where dw or db is. */
 hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t centred, int64_t rows, int32_t H, const void *dev_x, int64_t ldx,
                           const void *dev_w, const void *dev_b, float eps, void *dev_y, int64_t ldy, float *dev_mean, float *dev_rstd,

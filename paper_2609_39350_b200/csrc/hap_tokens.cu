@@ -11,6 +11,8 @@ using namespace hapop;
 static bool dtype_fits(int32_t t) { return t == HAP_BF16 || t == HAP_FP16 || t == HAP_FP32; }
 // a matrix whose rows all begin at multiples of 16 bytes
 static bool wide(const void *p, int64_t ld, int32_t dtype) { return aligned(p, 16) && ld * size_of(dtype) % 16 == 0; }       // (beside H % 8 == 0)
+// an output in the place of an input whose rows are another distance apart: rows would be written before they are read
+static bool astray(const void *out, int64_t ldo, const void *in, int64_t ldi, int64_t rows) { return out && out == in && ldo != ldi && rows > 1; }
 static bool grid_fits(int64_t blocks) { return blocks <= INT32_MAX; }
 
 // f(T()) of an element type
@@ -183,7 +185,7 @@ extern "C" hap_status hap_expert_combine(int32_t dtype, int64_t rows, int32_t k,
 {
     const int64_t size = size_of(dtype);
     if (!dtype_fits(dtype) || !rows_sizes(rows, k, H, placed) || ldy < H || ldo < H || (base && ldbase < H) || !aligned(y, size) || !aligned(base, size) || !aligned(out, size) ||
-        !aligned(places, 4) || !aligned(weights, 4))
+        !aligned(places, 4) || !aligned(weights, 4) || astray(out, ldo, base, ldbase, rows))
         return HAP_E_INVALID;
     if (rows == 0) return HAP_OK;
     if ((!y && placed > 0) || !places || !out) return HAP_E_INVALID;
@@ -366,7 +368,8 @@ extern "C" hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t
                                      int64_t ldy, float *mean, float *rstd, void *stream)
 {
     if (!dtype_fits(dtype) || (param_dtype != dtype && param_dtype != HAP_FP32) || !norm_sizes(rows, H) || ldx < H || ldy < H || !(eps >= 0) || !aligned(x, size_of(dtype)) ||
-        !aligned(y, size_of(dtype)) || !aligned(w, size_of(param_dtype)) || !aligned(b, size_of(param_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4))
+        !aligned(y, size_of(dtype)) || !aligned(w, size_of(param_dtype)) || !aligned(b, size_of(param_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+        astray(y, ldy, x, ldx, rows))
         return HAP_E_INVALID;
     if (rows == 0) return HAP_OK;
     if (!x || !y) return HAP_E_INVALID;
@@ -412,7 +415,8 @@ extern "C" hap_status hap_layer_norm_backward(int32_t dtype, int32_t param_dtype
     const int64_t size = size_of(dtype), gsize = size_of(grad_dtype);
     if (!dtype_fits(dtype) || (param_dtype != dtype && param_dtype != HAP_FP32) || (grad_dtype != param_dtype && grad_dtype != HAP_FP32) || !norm_sizes(rows, H) || lddy < H || ldx < H ||
         (base && ldbase < H) || (dx && lddx < H) || !aligned(dy, size) || !aligned(x, size) || !aligned(base, size) || !aligned(dx, size) || !aligned(w, size_of(param_dtype)) ||
-        !aligned(dw, gsize) || !aligned(db, gsize) || !aligned(mean, 4) || !aligned(rstd, 4) || (db && !centred) || (dx && dx == dy && lddx != lddy) || (dx && dx == base && lddx != ldbase))
+        !aligned(dw, gsize) || !aligned(db, gsize) || !aligned(mean, 4) || !aligned(rstd, 4) || (db && !centred) || astray(dx, lddx, dy, lddy, rows) ||
+        astray(dx, lddx, x, ldx, rows) || astray(dx, lddx, base, ldbase, rows))
         return HAP_E_INVALID;
     if (rows > 0 && (!dy || !x || !rstd || (centred && !mean))) return HAP_E_INVALID;
     uint64_t need = 0;
