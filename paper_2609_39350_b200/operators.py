@@ -22,6 +22,7 @@ from .binding import HapError, load_library
 EXPERT_FORWARD, EXPERT_GRAD_INPUT, EXPERT_GRAD_WEIGHT = 0, 1, 2
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _HALVES = (torch.bfloat16, torch.float16)
+_MOST = (1 << 31) - 1           # values of a row: row lengths are passed in 32 bits
 
 
 class _AdamWTensor(C.Structure):
@@ -88,9 +89,9 @@ def _matrix(name, t, here, dtypes, rows=None, cols=None):
     try:                                            # what is usual, asked for in as few steps as there are; the rest below
         (r, c), (ld, one) = t.shape, t.stride()
         if t.get_device() == here and t.dtype in dtypes and one == 1 and r > 0 and (rows is None or r == rows) and (cols is None or c == cols):
-            if r == 1:
+            if r == 1 and c <= _MOST:
                 return t.data_ptr(), (c + 7) & ~7
-            if ld >= c:
+            if _MOST >= c <= ld:
                 return t.data_ptr(), ld
     except (AttributeError, TypeError, ValueError, RuntimeError):
         pass
@@ -98,6 +99,8 @@ def _matrix(name, t, here, dtypes, rows=None, cols=None):
     (r, c), (ld, one) = t.shape, t.stride()
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         _refuse(f"{name}: shape {tuple(t.shape)} where {(rows, cols)} is needed")
+    if c > _MOST:
+        _refuse(f"{name}: rows of {c} values")
     if one != 1 and c > 1:
         _refuse(f"{name}: elements of a row must lie side by side")
     if r < 2:
@@ -113,6 +116,8 @@ def _matrices(name, t, here, dtypes, batch, rows=None, cols=None):
     (n, r, c), (far, ld, one) = t.shape, t.stride()
     if n != batch or (rows is not None and r != rows) or (cols is not None and c != cols):
         _refuse(f"{name}: shape {tuple(t.shape)} where {(batch, rows, cols)} is needed")
+    if max(r, c) > _MOST:
+        _refuse(f"{name}: matrices of {r} rows of {c} values")
     if one != 1 and c > 1:
         _refuse(f"{name}: elements of a row must lie side by side")
     if r < 2:
@@ -152,6 +157,8 @@ def _offsets(offsets, here):
     at = _vector("offsets", offsets, here, torch.int64)
     if offsets.numel() < 2:
         _refuse("offsets: one more than there are experts are needed")
+    if offsets.numel() > _MOST:
+        _refuse(f"offsets: of {offsets.numel() - 1} experts")
     return at, offsets.numel() - 1
 
 

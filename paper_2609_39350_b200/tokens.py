@@ -19,7 +19,7 @@ import numpy as np
 import torch
 
 from . import operators
-from .operators import _HALVES, _TYPES, _check, _here, _matrix, _now, _on_stream, _refuse, _vector
+from .operators import _HALVES, _MOST, _TYPES, _check, _here, _matrix, _now, _on_stream, _refuse, _vector
 
 SOFTMAX, SIGMOID = 0, 1
 _FLOATS = (torch.float32, *_HALVES)
@@ -58,13 +58,15 @@ def _table(name, t, here, dtype, rows=None, cols=None):
     """Address of a table [rows][cols] whose rows follow one another."""
     try:
         r, c = t.shape
-        if t.get_device() == here and t.dtype == dtype and (rows is None or r == rows) and (cols is None or c == cols) and t.is_contiguous():
+        if t.get_device() == here and t.dtype == dtype and c <= _MOST and (rows is None or r == rows) and (cols is None or c == cols) and t.is_contiguous():
             return t.data_ptr()
     except (AttributeError, TypeError, ValueError, RuntimeError):
         pass
     _here(name, t, here, (dtype,), 2)
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
         _refuse(f"{name}: shape {tuple(t.shape)} where {(rows, cols)} is needed")
+    if t.shape[1] > _MOST:
+        _refuse(f"{name}: rows of {t.shape[1]} values")
     if not t.is_contiguous():
         _refuse(f"{name}: rows must follow one another")
     return t.data_ptr()
@@ -130,6 +132,8 @@ def hap_route_backward(routing: HapRouting, logits, experts, dweights, dlogits=N
 
 
 def _order_bytes(rows, k, E):
+    if not 1 <= E <= 1024:
+        _refuse(f"E: {E} experts")
     n = C.c_uint64()
     _check(_lib().hap_expert_order_workspace(rows, k, E, C.byref(n)), "hap_expert_order_workspace")
     return n.value
@@ -230,6 +234,8 @@ def hap_embedding(tokens, w, first=0, scale=1.0, out=None):
 
 
 def _embedding_bytes(n, H, V):
+    if H > _MOST:
+        _refuse(f"dw: rows of {H} values")
     b = C.c_uint64()
     _check(_lib().hap_embedding_backward_workspace(n, H, V, C.byref(b)), "hap_embedding_backward_workspace")
     return b.value
