@@ -390,7 +390,6 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
         int j = 0;
         if (sizeof(T) == 2)
             for (; j + 8 <= n; j += 8) add(j, Count<8>());
-        if (sizeof(T) == 2 && n - j >= 6) add(j, Count<6>()), j += 6;
         for (; j + 4 <= n; j += 4) add(j, Count<4>());
         if (n - j >= 2) add(j, Count<2>()), j += 2;
         if (n - j) add(j, Count<1>());
@@ -399,8 +398,9 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_
 }
 
 // dy[place_j] = weight_j dout[row] and dweight_j = <dout[row], y[place_j]>, a block for each row: dout is read once, y once.  Up to
-// eight rows of y are on their way at once; with more than eight dout is read again, from L1.  Bound by memory: 4001 rows of 5120 with
-// six places each 96 us, 5.6 TB/s.
+// eight rows of y are on their way at once; with more than eight dout is read again, from L1.  Six at once, since four and two are two
+// passes over the row: 16384 rows of 5120 with six places 373 us, without 424 (with seven 479 and 530; in 32 bits four
+// rows are as many bytes as eight).  Bound by memory: 4001 rows of 5120 with six places each 96 us, 5.6 TB/s.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256) combine_backward_kernel(const RowsArgs p)
 {
     __shared__ float parts[8][MOST_CHOSEN];
