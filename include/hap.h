@@ -515,6 +515,8 @@ hap_status hap_adamw_state(const hap_adamw_tensor *tensors, int32_t n, float *co
  * An expert whose logit or bias is -inf is never chosen, nor is a group that has no others; where fewer than k experts are left
  * the rest of a row's are -1 with weight 0.  A row with a NaN, with a logit +inf under HAP_SOFTMAX, or under a bias that is NaN or
  * +inf, has no order: its experts are 0 .. k-1 and its weights NaN.
+ * Layouts of groups with group_best > 2, and those that would hold more than 1024 experts with the number of their groups rounded up to
+ * a power of two, are computed in 64 bits throughout, four to seven times slower.
  * experts int32 [rows][k], weights fp32 [rows][k].  1 <= E <= 1024, 1 <= k <= min(E, 32), 1 <= groups <= 32 dividing E,
  * 1 <= kept_groups <= groups, 1 <= group_best.
  * The backward pass gives dlogits [rows][E] (of the logits' type; may not overlap them) from dweights; the bias and the choice have no gradient.
@@ -568,7 +570,8 @@ hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, int32_t accu
  * pass needs.  Statistics in fp32, the variance from differences to the mean.
  * Backward: dx = base + rstd (g - mean(g) - xh mean(g xh)) with g = dy w, xh = (x - mean) rstd (base nullable: the gradient of the
  * residual stream; with centred = 0 without mean(g)); dw = sum dy xh, db = sum dy over the rows, of grad_dtype (param_dtype or
- * HAP_FP32), added to what they hold with accumulate.  dx, dw, db nullable; y may be x, dx may be x, dy or base.  H <= 16384.
+ * HAP_FP32), added to what they hold with accumulate.  dx, dw, db nullable, db with centred = 0 not computed (it is the sum of dy over
+ * the rows) and refused; y may be x, dx may be x, dy or base.  H <= 16384.
  * Workspace: hap_layer_norm_backward_workspace bytes, 256-byte aligned, during the call; needed where dw or db is. */
 hap_status hap_layer_norm(int32_t dtype, int32_t param_dtype, int32_t centred, int64_t rows, int32_t H, const void *dev_x, int64_t ldx,
                           const void *dev_w, const void *dev_b, float eps, void *dev_y, int64_t ldy, float *dev_mean, float *dev_rstd,

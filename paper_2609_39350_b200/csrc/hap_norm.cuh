@@ -13,7 +13,7 @@ struct NormArgs {
     int64_t rows;
     int H, blocks, add;             // blocks: of the backward pass, each with partial sums of its own; add: to what dw and db hold
     int ahead;                      // backwards: 1 where the next row is brought while one is worked on
-    float eps, inverse;             // inverse: 1 / H
+    float eps, inverse;             // inverse: 1 / H, rounded: a product is off by a unit more than a quotient and takes one instruction
     const void *x, *w, *b, *dy, *base;
     int64_t ldx, ldy, lddy, ldbase, lddx;
     void *y, *dx, *dw, *db;
@@ -195,7 +195,10 @@ template <typename T, typename P, int EIGHTS, bool RING, bool WIDE, bool CENTRED
 
 // Backwards: a row's threads take rows one after the other, the next one on its way meanwhile, and hold their columns' sums of dw and
 // db in registers, in 32 bits.  What has arrived is read twice, for the sums and for dx.  32760 rows of 5120 in 16 bits with base: 240 us,
-// 5.6 TB/s (rows read into registers when their turn comes: 640).
+// 5.6 TB/s (rows read into registers when their turn comes: 640).  Up to 5120 columns two blocks or more share a multiprocessor and
+// hide each other's barriers; above one is alone there, and above 7680 in 32 bits the next row is not brought ahead.  Without base, with
+// a mean, 8192 rows in 16 bits: of 5120 72 us, 6144 88, 7168 and 8192 107; 4096 of 12288 152, of 16384 186 (1024 threads with 64
+// registers, which spill); in 32 bits 8192 of 5120 166, 4096 of 8192 139, of 16384 297.
 template <typename T, typename P, int EIGHTS, int MOST, bool WIDE, bool CENTRED> __global__ void __launch_bounds__(MOST) norm_backward_kernel(const NormArgs p)
 {
     extern __shared__ __align__(16) char ring[];            // w; [blockDim.y][1 + ahead][x, dy, base where it fits][8 EIGHTS threads]

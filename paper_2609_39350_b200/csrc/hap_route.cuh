@@ -64,8 +64,9 @@ template <int L> __device__ __forceinline__ unsigned lanes_of(int lane) { return
 // the scores are.
 __device__ __forceinline__ float sigmoid_score(float z, float m) { return z <= 0.0f ? expf(z - m) / (1.0f + expf(z)) : 1.0f / (1.0f + expf(-z)); }
 
-// One row by a whole warp with values in 64 bits: for rows whose values 32 bits cannot tell apart, and for layouts of groups that do
-// not fit the lanes.  space: E doubles of this warp's own.
+// One row by a whole warp with values in 64 bits: for rows whose values 32 bits cannot tell apart, for layouts of groups that do not fit
+// the lanes, and for groups that are judged by more than two values.  Such layouts are four to seven times slower: 32768 rows of 256 in
+// eight groups by their best three 220 to 244 us (by their best two 51), of 1020 in 17 groups 952 us (rows of 1024 alone 145).  space: E doubles of this warp's own.
 struct RowStart { float m, sum; bool bad; };
 template <typename T> __device__ __noinline__ RowStart route_slowly(const RouteArgs &p, int64_t row, double *space, int *ce)
 {
@@ -230,10 +231,13 @@ template <int LO, int N, int ALL> __device__ __forceinline__ void in_order(uint3
 // L lanes for a row, up to PER experts each.  Values are in 32 bits, without the last few, where an expert's place in its lane stands;
 // the choice is the same as in exact arithmetic where neighbours in the order are further apart than both are off; where they are not,
 // groups and chosen are settled by their values in 64 bits, and hardly ever the row is done once more (settled by whole rows, one row
-// in 300 made the kernel a third longer: those that wait for it are few, but they are the last).  Bound by instructions: a lane's
-// values are put in order once, so that taking the largest k of a row is one maximum over the lanes and one read in one of them each.
-// 32768 rows of 256 with a bias and groups: 790 instructions a row, 53 us (every lane's maximum found anew for each: 1730, 91 us), of
-// which the ALU pipe is busy 20; logits alone 35 us; 5 us would be the bytes.
+// in 300 made the kernel a third longer: those that wait for it are few, but they are the last).  A lane's values are put in order
+// once, so that taking the largest k of a row is one maximum over the lanes and one read in one of them each.  Bound by latency with
+// few warps: 32768 rows of 256 with a bias and groups, 782 instructions a row, 53 us (every lane's maximum found anew for each: 1730,
+// 91 us); logits alone in 16 bits 29 us; 5 and 3 us would be the bytes.  A scheduler has 4.8 warps (96 registers a thread) and issues
+// in 55 % of its cycles, the ALU pipe is busy in half of them; of the 8.7 cycles between two instructions of a warp 2.3 are the first's
+// own, 1.6 wait for shuffles and shared memory (the k + 2 rounds, one behind the other), 1.3 for memory.  Rows of 1024: 145 us, 21
+// would be the bytes; 3.1 warps a scheduler (128 registers).
 template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROUTE_WARPS, PER == 32 ? 4 : ROUTE_BLOCKS) route_kernel(const RouteArgs p)
 {
     extern __shared__ double space[];                       // `room` for each warp, then for each row the chosen and their keys, two more
@@ -435,7 +439,8 @@ template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROU
 //   sigmoid, renormalised   dz_j = scale p_j (1 - s_j) (g_j - G)
 //   sigmoid                 dz_j = scale g_j s_j (1 - s_j)
 //   softmax                 dz_e = scale s_e (g_e - sum_j g_j s_j) over all e, g_e = 0 where e is not chosen
-// All but the last are 0 beside the chosen: their logits alone are read.  (32768 rows of 256: 17 us, 34 MB written.)
+// All but the last are 0 beside the chosen: their logits alone are read.  32768 rows of 256 in 32 bits:
+// 17 us, 34 MB written (8 would be the bytes), and 20 us over all e (11): a warp has one chain of reads and ends.
 template <typename T, int L, int PER> __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const RouteArgs p)
 {
     constexpr int ROWS = 32 / L;

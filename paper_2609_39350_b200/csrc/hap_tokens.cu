@@ -52,7 +52,9 @@ template <typename T, int L, int PER> static hap_status launch_route(const Route
     if (backward) return launch_next(route_backward_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, 0, 1, s, p);
     RouteArgs a = p;
     a.room = p.E > 16 * (PER + 1) ? p.E : 16 * (PER + 1);   // (a lane's keys and a 0 behind them)
-    if (blocks > 148 * ROUTE_BLOCKS) blocks = 148 * ROUTE_BLOCKS;       // (as many as run at once: warps go from row to row)
+    // warps go from row to row: as many blocks as run at once on 148 multiprocessors (of 32 experts a lane, whose threads have 128
+    // registers, four fifths do; the rest follow)
+    if (blocks > 148 * ROUTE_BLOCKS) blocks = 148 * ROUTE_BLOCKS;
     return launch_next(route_kernel<T, L, PER>, blocks, 32 * ROUTE_WARPS, ROUTE_WARPS * (a.room + 32 / L * (p.k + 2)) * 8, 1, s, a);
 }
 
@@ -302,7 +304,8 @@ extern "C" hap_status hap_embedding_backward(int32_t dtype, int32_t out_dtype, i
     const int threads = (int)(ceil_div(H, 8) < 256 ? ceil_div(ceil_div(H, 8), 32) * 32 : 256);
     const int64_t chunks = ceil_div(n, EMBEDDING_CHUNK), columns = ceil_div(H, 8 * threads), tasks = chunks * columns;
     if (!grid_fits(tasks)) return HAP_E_RANGE;
-    // blocks that sum: as many as run at once; behind them those that clear
+    // blocks that sum: three a multiprocessor, which run at once (but two do, by their registers, where dy is in 32 bits or rows are not
+    // whole sixteen bytes, and the third follows); behind them those that clear
     const int64_t most = 148 * 3, rows = ceil_div(V, threads / 32), clear = accumulate ? 0 : rows < 148 * 8 ? rows : 148 * 8;
     p.columns = (int)columns, p.sums = (int)(tasks < most ? tasks : most);
     const int64_t grid = p.sums + clear;
